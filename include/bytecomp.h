@@ -63,7 +63,9 @@ extern "C" {
 
 enum bc_kind { BC_TOPK = 0, BC_TOPK_SAMPLED = 1, BC_RANDK = 2, BC_SIGN1 = 3,
                BC_TERNGRAD = 4, BC_QSGD4 = 5, BC_QSGD8 = 6 };
-enum bc_dtype { BC_F32 = 0, BC_F16 = 1 };
+/* BC_BF16 (bfloat16) is an element type of the layer and optimizer calls
+ * at the end of this file only; gradients to compress are fp32 or fp16. */
+enum bc_dtype { BC_F32 = 0, BC_F16 = 1, BC_BF16 = 2 };
 
 enum bc_status {
     BC_OK = 0,
@@ -77,7 +79,8 @@ enum bc_status {
     BC_E_WORKSPACE = -7,  /* workspace NULL or smaller than required          */
     BC_E_HIP = -8,        /* a HIP runtime call failed                        */
     BC_E_ALIGN = -9,      /* a dense buffer violates the alignment rule       */
-    BC_E_DEVICE = -10     /* a kernel reported a failure (see bytecomp_device_status) */
+    BC_E_DEVICE = -10,    /* a kernel reported a failure (see bytecomp_device_status) */
+    BC_E_VALUE = -11      /* a number argument is outside its range           */
 };
 
 /* One gradient tensor to compress.
@@ -428,6 +431,55 @@ int bytecomp_set_topk_few_chunks(uint32_t chunks);
  * request), 0 otherwise.  BC_E_KIND for an unknown name.  One request is
  * held at a time, process-wide. */
 int bytecomp_time_next_launch(const char* kernel, void* start_event, void* stop_event);
+
+/* ------------------------------------------------------------------------
+ * Layers and optimizer around the compression path: the layers whose
+ * parameter gradients a data-parallel step compresses (layer norm and the
+ * linear layer, forward and backward), and the optimizer step that takes the
+ * aggregate.  They follow the conventions above (arguments checked on the
+ * host before anything is enqueued, all work on `stream`, the caller owns
+ * every buffer, no synchronisation), with these differences:
+ *   - Element types are BC_F32, BC_F16 and BC_BF16.
+ *   - Matrices are row-major with a row stride in elements (at least their
+ *     column count): rows may be slices of wider tensors.  Pointers need no
+ *     more than their element's alignment (BC_E_ALIGN otherwise).
+ *   - Arithmetic is fp32 (sums, statistics and products included) unless
+ *     said otherwise; each result is rounded once (nearest even) to its type.
+ *   - A workspace needs no initialisation and keeps nothing between calls.
+ *   - Outputs must not overlap inputs or each other, except where said.
+ *   - NaN and infinities in inputs go where the formulas send them.
+ * Results are deterministic. */
+
+/* Layer norm over the last axis.  For each of `rows` rows of `cols` values:
+ *   mean = sum(x) / cols, var = sum((x - mean)^2) / cols,
+ *   rstd = 1 / sqrt(var + eps), y = (x - mean) rstd weight + bias.
+ *   dtype      element type of x and y
+ *   wdtype     of weight and bias: dtype or BC_F32 (BC_E_DTYPE otherwise)
+ *   weight, bias  cols values each; NULL: 1 and 0
+ *   mean, rstd  rows fp32 values each, for the backward pass; NULL: not kept
+ *   eps        finite and >= 0 (BC_E_VALUE)
+ * y may be x itself (same stride).  rows < 2^31, cols < 2^24 (BC_E_SIZE);
+ * zero rows or columns: nothing to do. */
+int bytecomp_layernorm_forward(int dtype, int wdtype, uint64_t rows, uint64_t cols, const void* x, uint64_t ldx,
+                               const void* weight, const void* bias, double eps, void* y, uint64_t ldy,
+                               float* mean, float* rstd, void* stream);
+
+/* Bytes of workspace that bytecomp_layernorm_backward needs to compute
+ * dweight or dbias (any element type); host only. */
+int bytecomp_layernorm_workspace_size(uint64_t rows, uint64_t cols, size_t* bytes);
+
+/* The gradients, with xhat = (x - mean) rstd and h = dy weight:
+ *   dx = rstd (h - mean(h) - xhat mean(h xhat)), the means over the row,
+ *   dweight = sum over rows of dy xhat, dbias = sum over rows of dy.
+ *   mean, rstd  of the forward pass
+ *   dx         element type dtype; NULL: not wanted
+ *   dweight, dbias  cols values of wdtype, overwritten; NULL: not wanted
+ *   ws         NULL is fine when neither dweight nor dbias is wanted
+ * Zero rows: dweight and dbias become zero. */
+int bytecomp_layernorm_backward(int dtype, int wdtype, uint64_t rows, uint64_t cols, const void* dy, uint64_t lddy,
+                                const void* x, uint64_t ldx, const void* weight, const float* mean,
+                                const float* rstd, void* dx, uint64_t lddx, void* dweight, void* dbias, void* ws,
+                                size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,14 +17,14 @@ LIB_PATH = os.path.join(HERE, "libbytecomp.so")
 
 BC_TOPK, BC_TOPK_SAMPLED, BC_RANDK, BC_SIGN1 = 0, 1, 2, 3
 BC_TERNGRAD, BC_QSGD4, BC_QSGD8 = 4, 5, 6
-BC_F32, BC_F16 = 0, 1
+BC_F32, BC_F16, BC_BF16 = 0, 1, 2
 KIND = {"topk": BC_TOPK, "topk_sampled": BC_TOPK_SAMPLED, "randk": BC_RANDK, "sign": BC_SIGN1,
         "terngrad": BC_TERNGRAD, "qsgd4": BC_QSGD4, "qsgd8": BC_QSGD8}
 # kinds whose payload is packed words plus one scale per tensor
 WORD_KINDS = (BC_SIGN1, BC_TERNGRAD, BC_QSGD4, BC_QSGD8)
 STATUS = {0: "BC_OK", -1: "BC_E_NULL", -2: "BC_E_KIND", -3: "BC_E_DTYPE", -4: "BC_E_RATIO",
           -5: "BC_E_SIZE", -6: "BC_E_COUNT", -7: "BC_E_WORKSPACE", -8: "BC_E_HIP",
-          -9: "BC_E_ALIGN", -10: "BC_E_DEVICE"}
+          -9: "BC_E_ALIGN", -10: "BC_E_DEVICE", -11: "BC_E_VALUE"}
 
 
 class bc_tensor(ctypes.Structure):
@@ -109,6 +109,13 @@ def lib():
         L.bytecomp_set_wait_limit.argtypes = [ctypes.c_uint32]
         L.bytecomp_set_topk_few_chunks.restype = i32
         L.bytecomp_set_topk_few_chunks.argtypes = [ctypes.c_uint32]
+        L.bytecomp_layernorm_forward.restype = i32
+        L.bytecomp_layernorm_forward.argtypes = [i32, i32, u64, u64, vp, u64, vp, vp, dbl, vp, u64, vp, vp, vp]
+        L.bytecomp_layernorm_workspace_size.restype = i32
+        L.bytecomp_layernorm_workspace_size.argtypes = [u64, u64, ctypes.POINTER(sz)]
+        L.bytecomp_layernorm_backward.restype = i32
+        L.bytecomp_layernorm_backward.argtypes = [i32, i32, u64, u64, vp, u64, vp, u64, vp, vp, vp, vp, u64, vp, vp,
+                                                  vp, sz, vp]
         _lib = L
     return _lib
 
@@ -548,3 +555,122 @@ def alloc_payload(kind, ratio, ns, device="cuda"):
 def alloc_workspace(kind, ratio, ns, W=1, device="cuda"):
     import torch
     return torch.zeros(bytecomp_workspace_size(kind, ratio, ns, W), dtype=torch.uint8, device=device)
+
+
+# ------------------------------------------------ layers and optimizer step
+# Matrices are two-dimensional tensors whose last axis is contiguous (rows
+# may be slices of wider tensors); vectors are contiguous.  A wrong shape,
+# layout, device or mix of types raises ValueError here, everything else is the
+# library's to refuse.
+
+def _dtype(t):
+    import torch
+    return {torch.float32: BC_F32, torch.float16: BC_F16, torch.bfloat16: BC_BF16}.get(t.dtype, 99)
+
+
+def _matrix(name, t, rows, cols, dtype):
+    """(pointer, row stride) of a rows x cols matrix, (None, cols) for None."""
+    if t is None:
+        return None, cols
+    if tuple(t.shape) != (rows, cols) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: expected a {rows} x {cols} {dtype} device tensor, got {tuple(t.shape)} {t.dtype} "
+                         f"on {t.device}")
+    if cols > 1 and t.stride(1) != 1 and t.numel():
+        raise ValueError(f"{name}: columns must be contiguous")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name}: row stride {ld} below {cols} columns")
+    return (t.data_ptr() if t.numel() else None), ld
+
+
+def _vector(name, t, n, dtype):
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or t.dtype != dtype or not t.is_cuda or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: expected {n} contiguous {dtype} values on the device, got {tuple(t.shape)} {t.dtype} "
+                         f"on {t.device}")
+    return t.data_ptr() if n else None
+
+
+def _ws(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def _alloc_bytes(n, device):
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def bytecomp_layernorm_workspace_size(rows, cols):
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_layernorm_workspace_size",
+           lib().bytecomp_layernorm_workspace_size(int(rows), int(cols), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_layernorm_workspace(rows, cols, device="cuda"):
+    return _alloc_bytes(bytecomp_layernorm_workspace_size(rows, cols), device)
+
+
+class _Call:
+    """A library call with its arguments marshalled once; `_keep` holds the
+    tensors that the pointers belong to."""
+
+    def __init__(self, fn, args, keep):
+        self._fn, self._args, self._keep = fn, args, keep
+        self._entry = getattr(lib(), fn)
+
+    def __call__(self):
+        code = self._entry(*self._args)
+        if code:
+            _check(self._fn, code)
+
+
+class LayerNormCall(_Call):
+    """bytecomp_layernorm_forward: x [rows, cols] to y, with weight and bias
+    [cols] of x's type or fp32 (None: 1 and 0) and the rows' fp32 mean and
+    rstd (None: not kept)."""
+
+    def __init__(self, x, weight, bias, eps, y, mean=None, rstd=None, stream=None):
+        import torch
+        rows, cols = x.shape
+        wd = next((t.dtype for t in (weight, bias) if t is not None), x.dtype)
+        px, ldx = _matrix("x", x, rows, cols, x.dtype)
+        py, ldy = _matrix("y", y, rows, cols, x.dtype)
+        wdt = _dtype(weight if weight is not None else bias if bias is not None else x)
+        super().__init__("bytecomp_layernorm_forward",
+                         (_dtype(x), wdt, rows, cols, px, ldx, _vector("weight", weight, cols, wd),
+                          _vector("bias", bias, cols, wd), float(eps), py, ldy,
+                          _vector("mean", mean, rows, torch.float32), _vector("rstd", rstd, rows, torch.float32),
+                          _stream_handle(stream)), (x, weight, bias, y, mean, rstd))
+
+
+class LayerNormGradCall(_Call):
+    """bytecomp_layernorm_backward: dx, dweight and dbias (None: not wanted)
+    from dy, x, weight (None: 1) and the forward pass's mean and rstd; ws
+    from alloc_layernorm_workspace."""
+
+    def __init__(self, dy, x, weight, mean, rstd, dx, dweight, dbias, ws, stream=None):
+        import torch
+        rows, cols = x.shape
+        wd = next((t.dtype for t in (weight, dweight, dbias) if t is not None), x.dtype)
+        wdt = _dtype(next((t for t in (weight, dweight, dbias) if t is not None), x))
+        pdy, lddy = _matrix("dy", dy, rows, cols, x.dtype)
+        px, ldx = _matrix("x", x, rows, cols, x.dtype)
+        pdx, lddx = _matrix("dx", dx, rows, cols, x.dtype)
+        pw, nw = _ws(ws)
+        super().__init__("bytecomp_layernorm_backward",
+                         (_dtype(x), wdt, rows, cols, pdy, lddy, px, ldx, _vector("weight", weight, cols, wd),
+                          _vector("mean", mean, rows, torch.float32), _vector("rstd", rstd, rows, torch.float32), pdx,
+                          lddx, _vector("dweight", dweight, cols, wd), _vector("dbias", dbias, cols, wd), pw, nw,
+                          _stream_handle(stream)), (dy, x, weight, mean, rstd, dx, dweight, dbias, ws))
+
+
+def bytecomp_layernorm_forward(x, weight, bias, eps, y, mean=None, rstd=None, stream=None):
+    """y = layer norm of x's rows; see LayerNormCall."""
+    LayerNormCall(x, weight, bias, eps, y, mean, rstd, stream)()
+
+
+def bytecomp_layernorm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, ws, stream=None):
+    """The gradients of bytecomp_layernorm_forward; see LayerNormGradCall."""
+    LayerNormGradCall(dy, x, weight, mean, rstd, dx, dweight, dbias, ws, stream)()

@@ -335,15 +335,7 @@ Ws carve_workspace(void* base, const WsPlan& p) {
 
 hipError_t launch_zero_header(uint32_t* flags, hipStream_t s);
 
-}  // namespace bc
-
-using namespace bc;
-
-namespace {
-
-int hip_status(hipError_t e) { return e == hipSuccess ? BC_OK : BC_E_HIP; }
-
-int finish(int rc, hipStream_t s, void* ws) {
+int finish_call(int rc, hipStream_t s, void* ws) {
     if (rc != BC_OK || !debug_mode()) return rc;
     if (hipStreamSynchronize(s) != hipSuccess) return BC_E_HIP;
     if (ws) {
@@ -353,6 +345,26 @@ int finish(int rc, hipStream_t s, void* ws) {
     }
     return BC_OK;
 }
+
+hipError_t with_table(const void* bytes, size_t len, hipStream_t s, TableLaunch launch, void* ctx) {
+    std::lock_guard<std::mutex> lk(g_mu);
+    Entry* en = nullptr;
+    hipError_t e = cache_get(bytes, len, 0, [](void*) {}, s, &en);
+    if (e != hipSuccess) return e;
+    e = launch(ctx, en->dev);
+    cache_mark_used(en, s);
+    return e;
+}
+
+}  // namespace bc
+
+using namespace bc;
+
+namespace {
+
+int hip_status(hipError_t e) { return e == hipSuccess ? BC_OK : BC_E_HIP; }
+
+int finish(int rc, hipStream_t s, void* ws) { return finish_call(rc, s, ws); }
 
 // Validate a tensor list and build its descriptor table.
 int build_tdesc(int kind, uint64_t ppm, const bc_tensor* t, int T, bool need_resid,
@@ -492,6 +504,7 @@ const char* bytecomp_strerror(int status) {
         case BC_E_HIP: return "HIP runtime error";
         case BC_E_ALIGN: return "dense buffer not aligned (fp32 and outputs 16 B, fp16 8 B)";
         case BC_E_DEVICE: return "a kernel reported a failure";
+        case BC_E_VALUE: return "a number argument is outside its range";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,63 @@
+// elem.hpp -- element types of the layer operators (layer norm, linear layer,
+// orthogonalised updates): fp32, fp16 and bfloat16 in memory, fp32 in
+// registers.  Rows may start at any element, so vector accesses assume no more
+// than an element's alignment; gfx950 takes such global loads and stores whole.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/bytecomp.h"
+
+namespace bc {
+
+typedef _Float16 f16_t;
+typedef __bf16 bf16_t;
+
+inline size_t dtype_bytes(int dtype) { return dtype == BC_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == BC_F32 || dtype == BC_F16 || dtype == BC_BF16; }
+
+// Elements of one 16-byte access.
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+// V consecutive elements widened to fp32; the first `left` of them when
+// fewer are left (the others 0, not read).
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(const T* p, int left, float (&f)[V]) {
+    if (left >= V) {
+        typedef T vec __attribute__((ext_vector_type(V)));
+        vec v;
+        __builtin_memcpy(&v, p, sizeof(v));
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = (float)v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+
+// The same, rounded once (nearest, ties to even) and written.
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T* p, int left, const float (&f)[V]) {
+    if (left >= V) {
+        typedef T vec __attribute__((ext_vector_type(V)));
+        vec v;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (T)f[i];
+        __builtin_memcpy(p, &v, sizeof(v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < left) p[i] = (T)f[i];
+    }
+}
+
+// Sum over the 64 lanes of a wave, in every lane.
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+
+}  // namespace bc

@@ -102,6 +102,14 @@ int compress_prepare(int kind, double ratio, const bc_tensor* t, int T, const bc
 hipError_t compress_launch(int kind, double ratio, uint64_t seed, const CompressPrep& p, const TDesc* dd,
                            const bc_payload& out, const Ws& w, hipStream_t s);
 
+// rc, after a synchronisation and a look at the workspace's failure flags
+// (ws NULL: none) where BYTECOMP_DEBUG=1 asks for them.
+int finish_call(int rc, hipStream_t s, void* ws);
+// Runs launch(device copy of bytes) with the descriptor cache's copy, marked
+// as in use by stream s.
+typedef hipError_t (*TableLaunch)(void* ctx, const void* table);
+hipError_t with_table(const void* bytes, size_t len, hipStream_t s, TableLaunch launch, void* ctx);
+
 struct DevInfo {
     int cus;
     bool any_empty;      // per call: some tensor has no elements
