@@ -481,6 +481,49 @@ int bytecomp_layernorm_backward(int dtype, int wdtype, uint64_t rows, uint64_t c
                                 const float* rstd, void* dx, uint64_t lddx, void* dweight, void* dbias, void* ws,
                                 size_t ws_bytes, void* stream);
 
+/* Activations of the linear layer: z, max(z, 0), z Phi(z) with the normal
+ * distribution function Phi, its approximation
+ * 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), and z / (1 + exp(-z)). */
+enum bc_act { BC_ACT_NONE = 0, BC_ACT_RELU = 1, BC_ACT_GELU = 2, BC_ACT_GELU_TANH = 3, BC_ACT_SILU = 4 };
+
+/* Linear layer: z = x w^T + bias, y = act(z) + residual, with bias,
+ * activation and residual in the product's epilogue.
+ *   dtype     of every tensor
+ *   x [rows, inner], w [cols, inner], y [rows, cols]
+ *   bias      cols values, or NULL: 0
+ *   residual  [rows, cols], or NULL: 0; may be y itself (same stride)
+ *   z         [rows, cols], the sum before the activation, kept for the
+ *             backward pass; NULL: not kept.  y comes from the unrounded z.
+ *   ws        at least bytecomp_linear_workspace_size bytes, 16-byte aligned;
+ *             NULL is fine where that is 0
+ * fp32 products are sums of bfloat16 products of the operands' three parts
+ * (24 bits) and as exact as fp32 ones; with an infinite operand such a
+ * product is NaN, and parts under the smallest normal number may be lost.
+ * rows, inner and cols < 2^22 (BC_E_SIZE).  Zero rows or columns: nothing to
+ * do; zero inner: the product is zero. */
+int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* x, uint64_t ldx,
+                            const void* w, uint64_t ldw, const void* bias, int act, const void* residual,
+                            uint64_t ld_residual, void* y, uint64_t ldy, void* z, uint64_t ldz, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* Bytes of workspace that the forward (backward = 0) or backward pass of
+ * this shape needs at most, whatever the strides and alignment (host only). */
+int bytecomp_linear_workspace_size(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, int backward,
+                                   size_t* bytes);
+
+/* The gradients, with dz = dy act'(z) (relu's slope at 0 is 0):
+ *   dx = dz w, dw = dz^T x, dbias = sum over rows of dz;
+ * the residual's gradient is dy.
+ *   gdtype  element type of dw and dbias: dtype or BC_F32
+ *   z       of the forward pass; may be NULL with BC_ACT_NONE
+ *   dx, dw, dbias  overwritten; NULL: not wanted
+ * In fp16 and bfloat16, dz is rounded to dtype for the products (dbias sums
+ * it unrounded).  Zero rows: dw and dbias become zero. */
+int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* dy,
+                             uint64_t lddy, const void* z, uint64_t ldz, int act, const void* x, uint64_t ldx,
+                             const void* w, uint64_t ldw, void* dx, uint64_t lddx, void* dw, uint64_t lddw,
+                             void* dbias, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(HERE, "libbytecomp.so")
 BC_TOPK, BC_TOPK_SAMPLED, BC_RANDK, BC_SIGN1 = 0, 1, 2, 3
 BC_TERNGRAD, BC_QSGD4, BC_QSGD8 = 4, 5, 6
 BC_F32, BC_F16, BC_BF16 = 0, 1, 2
+ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 KIND = {"topk": BC_TOPK, "topk_sampled": BC_TOPK_SAMPLED, "randk": BC_RANDK, "sign": BC_SIGN1,
         "terngrad": BC_TERNGRAD, "qsgd4": BC_QSGD4, "qsgd8": BC_QSGD8}
 # kinds whose payload is packed words plus one scale per tensor
@@ -116,6 +117,14 @@ def lib():
         L.bytecomp_layernorm_backward.restype = i32
         L.bytecomp_layernorm_backward.argtypes = [i32, i32, u64, u64, vp, u64, vp, u64, vp, vp, vp, vp, u64, vp, vp,
                                                   vp, sz, vp]
+        L.bytecomp_linear_workspace_size.restype = i32
+        L.bytecomp_linear_workspace_size.argtypes = [i32, u64, u64, u64, i32, ctypes.POINTER(sz)]
+        L.bytecomp_linear_forward.restype = i32
+        L.bytecomp_linear_forward.argtypes = [i32, u64, u64, u64, vp, u64, vp, u64, vp, i32, vp, u64, vp, u64, vp,
+                                              u64, vp, sz, vp]
+        L.bytecomp_linear_backward.restype = i32
+        L.bytecomp_linear_backward.argtypes = [i32, i32, u64, u64, u64, vp, u64, vp, u64, i32, vp, u64, vp, u64, vp,
+                                               u64, vp, u64, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -674,3 +683,77 @@ def bytecomp_layernorm_forward(x, weight, bias, eps, y, mean=None, rstd=None, st
 def bytecomp_layernorm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, ws, stream=None):
     """The gradients of bytecomp_layernorm_forward; see LayerNormGradCall."""
     LayerNormGradCall(dy, x, weight, mean, rstd, dx, dweight, dbias, ws, stream)()
+
+
+def bytecomp_linear_workspace_size(dtype, rows, inner, cols, backward=False):
+    """dtype: BC_F32, BC_F16 or BC_BF16."""
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_linear_workspace_size",
+           lib().bytecomp_linear_workspace_size(int(dtype), int(rows), int(inner), int(cols), int(bool(backward)),
+                                                ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_linear_workspace(x, w, backward=False):
+    """Workspace for the layer's forward or backward pass on x [rows, inner] and w [cols, inner]."""
+    return _alloc_bytes(bytecomp_linear_workspace_size(_dtype(x), x.shape[0], x.shape[1], w.shape[0], backward),
+                        x.device)
+
+
+def _activation(name):
+    if name not in ACTIVATION:
+        raise ValueError(f"activation {name!r}: one of {', '.join(ACTIVATION)}")
+    return ACTIVATION[name]
+
+
+class LinearCall(_Call):
+    """bytecomp_linear_forward: y = act(x w^T + bias) + residual, z the sum
+    before the activation; bias, residual and z may be None.  activation: a
+    key of ACTIVATION; ws from alloc_linear_workspace (None for at most 64
+    rows)."""
+
+    def __init__(self, x, w, bias, residual, activation, y, z=None, ws=None, stream=None):
+        rows, inner = x.shape
+        cols, dt = w.shape[0], x.dtype
+        px, ldx = _matrix("x", x, rows, inner, dt)
+        pwt, ldw = _matrix("w", w, cols, inner, dt)
+        pr, ldr = _matrix("residual", residual, rows, cols, dt)
+        py, ldy = _matrix("y", y, rows, cols, dt)
+        pz, ldz = _matrix("z", z, rows, cols, dt)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_linear_forward",
+                         (_dtype(x), rows, inner, cols, px, ldx, pwt, ldw, _vector("bias", bias, cols, dt),
+                          _activation(activation), pr, ldr, py, ldy, pz, ldz, p, n, _stream_handle(stream)),
+                         (x, w, bias, residual, y, z, ws))
+
+
+class LinearGradCall(_Call):
+    """bytecomp_linear_backward: dx, dw and dbias (None: not wanted) of a
+    LinearCall with this x, w, activation and z.  dw and dbias in x's type or
+    fp32; ws from alloc_linear_workspace(x, w, backward=True)."""
+
+    def __init__(self, dy, z, x, w, activation, dx, dw, dbias, ws, stream=None):
+        rows, inner = x.shape
+        cols, dt = w.shape[0], x.dtype
+        pdy, lddy = _matrix("dy", dy, rows, cols, dt)
+        pz, ldz = _matrix("z", z, rows, cols, dt)
+        px, ldx = _matrix("x", x, rows, inner, dt)
+        pwt, ldw = _matrix("w", w, cols, inner, dt)
+        pdx, lddx = _matrix("dx", dx, rows, inner, dt)
+        gd = next((t for t in (dw, dbias) if t is not None), x)
+        pdw, lddw = _matrix("dw", dw, cols, inner, gd.dtype)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_linear_backward",
+                         (_dtype(x), _dtype(gd), rows, inner, cols, pdy, lddy, pz, ldz, _activation(activation), px,
+                          ldx, pwt, ldw, pdx, lddx, pdw, lddw, _vector("dbias", dbias, cols, gd.dtype), p, n,
+                          _stream_handle(stream)), (dy, z, x, w, dx, dw, dbias, ws))
+
+
+def bytecomp_linear_forward(x, w, bias, residual, activation, y, z=None, ws=None, stream=None):
+    """y = act(x w^T + bias) + residual; see LinearCall."""
+    LinearCall(x, w, bias, residual, activation, y, z, ws, stream)()
+
+
+def bytecomp_linear_backward(dy, z, x, w, activation, dx, dw, dbias, ws, stream=None):
+    """The gradients of bytecomp_linear_forward; see LinearGradCall."""
+    LinearGradCall(dy, z, x, w, activation, dx, dw, dbias, ws, stream)()

@@ -34,6 +34,58 @@ size_t layernorm_ws(uint64_t rows, uint64_t cols) {
     return (size_t)(a > b ? a : b) * 2 * cols * sizeof(float);
 }
 
+// ------------------------------------------------------------ linear layer
+constexpr uint64_t kMaxDim = 1ull << 22;
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+int check_linear(int dtype, uint64_t rows, uint64_t inner, uint64_t cols) {
+    if (!dtype_ok(dtype)) return BC_E_DTYPE;
+    if (rows >= kMaxDim || inner >= kMaxDim || cols >= kMaxDim) return BC_E_SIZE;
+    return BC_OK;
+}
+
+// Bytes of an operand of `rows` rows and k columns laid out as planes.
+size_t planes_bytes(int dtype, uint64_t rows, uint64_t k) {
+    return align256((size_t)(rows * plane_cols(k) * 2 * (uint64_t)planes_of(dtype)));
+}
+
+size_t linear_ws(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, bool backward) {
+    if (!backward) return rows <= kFewRows ? 0 : planes_bytes(dtype, rows, inner) + planes_bytes(dtype, cols, inner);
+    return planes_bytes(dtype, rows, cols) + planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows) +
+           planes_bytes(dtype, inner, cols) + align256((size_t)((rows + 63) / 64 * cols * sizeof(float)));
+}
+
+// Hands out the workspace piece by piece.
+struct Carver {
+    char* at;
+    void* take(size_t bytes) {
+        char* p = at;
+        at += align256(bytes);
+        return p;
+    }
+};
+
+// Whether the product kernels can read an operand of k columns where it lies:
+// 16-bit elements, whole steps, 16-byte pieces, offsets within 32 bits.
+bool readable(int dtype, const void* p, uint64_t ld, uint64_t k) {
+    return dtype != BC_F32 && k % kPlaneCols == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1ull << 23);
+}
+
+// An operand of `rows` rows and k columns for the product kernels: where it
+// lies, or laid out at `c`.
+hipError_t operand(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t k, Carver& c, Planes& out,
+                   hipStream_t s) {
+    if (readable(dtype, p, ld, k)) {
+        out = Planes{p, ld, 0};
+        return hipSuccess;
+    }
+    void* to = c.take(planes_bytes(dtype, rows, k));
+    out = Planes{to, plane_cols(k), rows * plane_cols(k)};
+    const LayOut a{p, nullptr, ld, 0, (uint32_t)rows, (uint32_t)k, to, nullptr, nullptr, BC_ACT_NONE};
+    return launch_lay_out(dtype, a, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -82,6 +134,128 @@ int bytecomp_layernorm_backward(int dtype, int wdtype, uint64_t rows, uint64_t c
                        (uint32_t)cols, ln_parts(rows, (uint32_t)cols, dtype), (float)(1.0 / (double)cols)};
     hipStream_t s = (hipStream_t)stream;
     return finish_call(status_of(launch_ln_backward(dtype, wdtype, a, dweight, dbias, s)), s, nullptr);
+}
+
+int bytecomp_linear_workspace_size(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, int backward,
+                                   size_t* bytes) {
+    if (!bytes) return BC_E_NULL;
+    if (const int rc = check_linear(dtype, rows, inner, cols)) return rc;
+    *bytes = linear_ws(dtype, rows, inner, cols, backward != 0);
+    return BC_OK;
+}
+
+int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* x, uint64_t ldx,
+                            const void* w, uint64_t ldw, const void* bias, int act, const void* residual,
+                            uint64_t ld_residual, void* y, uint64_t ldy, void* z, uint64_t ldz, void* ws,
+                            size_t ws_bytes, void* stream) {
+    const CallRange range("bytecomp_linear_forward");
+    if (const int rc = check_linear(dtype, rows, inner, cols)) return rc;
+    if (act < BC_ACT_NONE || act > BC_ACT_SILU) return BC_E_KIND;
+    if (rows == 0 || cols == 0) return BC_OK;
+    if (!y || (inner > 0 && (!x || !w))) return BC_E_NULL;
+    if (ldx < inner || ldw < inner || ldy < cols || (residual && ld_residual < cols) || (z && ldz < cols))
+        return BC_E_SIZE;
+    if (misaligned(x, dtype) || misaligned(w, dtype) || misaligned(bias, dtype) || misaligned(residual, dtype) ||
+        misaligned(y, dtype) || misaligned(z, dtype) || ((uintptr_t)ws & 15))
+        return BC_E_ALIGN;
+    hipStream_t s = (hipStream_t)stream;
+    if (rows <= kFewRows) {
+        const FewRows a{x, w, bias, residual, y, z, ldx, ldw, ld_residual, ldy, ldz, (uint32_t)rows, (uint32_t)inner,
+                        (uint32_t)cols, act};
+        return finish_call(status_of(launch_few_rows(dtype, a, s)), s, nullptr);
+    }
+    size_t need = 0;
+    if (!readable(dtype, x, ldx, inner)) need += planes_bytes(dtype, rows, inner);
+    if (!readable(dtype, w, ldw, inner)) need += planes_bytes(dtype, cols, inner);
+    if (need > 0 && (!ws || ws_bytes < need)) return BC_E_WORKSPACE;
+    Carver c{(char*)ws};
+    Product p{};
+    hipError_t e = operand(dtype, x, ldx, rows, inner, c, p.a, s);
+    if (e == hipSuccess) e = operand(dtype, w, ldw, cols, inner, c, p.b, s);
+    if (e == hipSuccess) {
+        p.rows = (uint32_t)rows;
+        p.cols = (uint32_t)cols;
+        p.steps = (uint32_t)(plane_cols(inner) / kPlaneCols);
+        p.out = y;
+        p.ld_out = ldy;
+        p.bias = bias;
+        p.residual = residual;
+        p.z = z;
+        p.ld_residual = ld_residual;
+        p.ld_z = ldz;
+        p.act = act;
+        e = launch_product(dtype, dtype, true, p, s);
+    }
+    return finish_call(status_of(e), s, nullptr);
+}
+
+int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* dy,
+                             uint64_t lddy, const void* z, uint64_t ldz, int act, const void* x, uint64_t ldx,
+                             const void* w, uint64_t ldw, void* dx, uint64_t lddx, void* dw, uint64_t lddw,
+                             void* dbias, void* ws, size_t ws_bytes, void* stream) {
+    const CallRange range("bytecomp_linear_backward");
+    if (const int rc = check_linear(dtype, rows, inner, cols)) return rc;
+    if (gdtype != dtype && gdtype != BC_F32) return BC_E_DTYPE;
+    if (act < BC_ACT_NONE || act > BC_ACT_SILU) return BC_E_KIND;
+    if (!dx && !dw && !dbias) return BC_OK;
+    const bool product = rows > 0 && cols > 0 && inner > 0;
+    if (rows > 0 && cols > 0 && (!dy || (act != BC_ACT_NONE && !z))) return BC_E_NULL;
+    if (product && ((dw && !x) || (dx && !w))) return BC_E_NULL;
+    if (lddy < cols || (act != BC_ACT_NONE && ldz < cols) || (dw && (ldx < inner || lddw < inner)) ||
+        (dx && (ldw < inner || lddx < inner)))
+        return BC_E_SIZE;
+    if (misaligned(dy, dtype) || misaligned(z, dtype) || misaligned(x, dtype) || misaligned(w, dtype) ||
+        misaligned(dx, dtype) || misaligned(dw, gdtype) || misaligned(dbias, gdtype) || ((uintptr_t)ws & 15))
+        return BC_E_ALIGN;
+    const bool same = act == BC_ACT_NONE && readable(dtype, dy, lddy, cols);  // dz can be read as dy
+    const bool flat = dx && !same;
+    size_t need = 0;
+    if (flat) need += planes_bytes(dtype, rows, cols);
+    if (dx) need += planes_bytes(dtype, inner, cols);
+    if (dw) need += planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows);
+    const size_t part_bytes = align256((size_t)((rows + 63) / 64 * cols * sizeof(float)));
+    if (dbias) need += part_bytes;
+    if (need > 0 && (!ws || ws_bytes < need)) return BC_E_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    Carver c{(char*)ws};
+    hipError_t e = hipSuccess;
+    LayOut l{dy, act != BC_ACT_NONE ? z : nullptr, lddy, ldz, (uint32_t)rows, (uint32_t)cols, nullptr, nullptr,
+             nullptr, act};
+    if (flat) l.flat = c.take(planes_bytes(dtype, rows, cols));
+    if (dw) l.turned = c.take(planes_bytes(dtype, cols, rows));
+    if (dbias) l.part = (float*)c.take(part_bytes);
+    if (flat || dw || dbias) e = launch_lay_out(dtype, l, s);
+    if (e == hipSuccess && dbias)
+        e = launch_sum_parts(gdtype, l.part, (uint32_t)((rows + 63) / 64), cols, (uint32_t)cols, dbias, nullptr, s);
+    if (e == hipSuccess && dx) {
+        Product p{};
+        p.a = flat ? Planes{l.flat, plane_cols(cols), rows * plane_cols(cols)} : Planes{dy, lddy, 0};
+        void* turned = c.take(planes_bytes(dtype, inner, cols));
+        p.b = Planes{turned, plane_cols(cols), inner * plane_cols(cols)};
+        const LayOut t{w, nullptr, ldw, 0, (uint32_t)cols, (uint32_t)inner, nullptr, turned, nullptr, BC_ACT_NONE};
+        e = launch_lay_out(dtype, t, s);
+        p.rows = (uint32_t)rows;
+        p.cols = (uint32_t)inner;
+        p.steps = (uint32_t)(plane_cols(cols) / kPlaneCols);
+        p.out = dx;
+        p.ld_out = lddx;
+        if (e == hipSuccess) e = launch_product(dtype, dtype, false, p, s);
+    }
+    if (e == hipSuccess && dw) {
+        Product p{};
+        p.a = Planes{l.turned, plane_cols(rows), cols * plane_cols(rows)};
+        void* turned = c.take(planes_bytes(dtype, inner, rows));
+        p.b = Planes{turned, plane_cols(rows), inner * plane_cols(rows)};
+        const LayOut t{x, nullptr, ldx, 0, (uint32_t)rows, (uint32_t)inner, nullptr, turned, nullptr, BC_ACT_NONE};
+        e = launch_lay_out(dtype, t, s);
+        p.rows = (uint32_t)cols;
+        p.cols = (uint32_t)inner;
+        p.steps = (uint32_t)(plane_cols(rows) / kPlaneCols);
+        p.out = dw;
+        p.ld_out = lddw;
+        if (e == hipSuccess) e = launch_product(dtype, gdtype, false, p, s);
+    }
+    return finish_call(status_of(e), s, nullptr);
 }
 
 }  // extern "C"

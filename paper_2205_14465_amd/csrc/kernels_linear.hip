@@ -1,0 +1,374 @@
+// kernels_linear.hip -- the linear layer on the matrix cores: forward
+//   z = x w^T + bias,  y = act(z) + residual
+// and backward, with dz = dy act'(z),
+//   dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz.
+//
+// The products run in the tiles of gemm.hpp, which want both operands with the
+// contracted axis contiguous, 16-byte pieces and whole steps of it.  The
+// forward pass's fp16 and bfloat16 operands are usually so and are read where
+// they lie; lay_out copies the others into the workspace (padding with zeros,
+// turning for the backward pass, splitting fp32 into three bfloat16 planes, whose
+// six leading products reach fp32's last places at more than twice the rate of
+// the fp32 matrix instructions).  dz is formed in that pass from dy and z and,
+// for fp16 and bfloat16, rounded to their type: each of its roundings is half a
+// unit in the last place of one term of dx and dw, whose own results are
+// rounded once to the same type.  dbias is the fp32 sum of the unrounded dz.
+#include "gemm.hpp"
+#include "launch.hpp"
+#include "layers.hpp"
+
+namespace bc {
+
+namespace {
+
+// ------------------------------------------------------------- activations
+// Both in fp32; `exact` keeps fp32's last places (fp32 tensors), otherwise the
+// hardware's exponential and reciprocal do (1 unit of fp32, far below a unit of
+// fp16 or bfloat16).
+constexpr float kSqrtHalf = 0.70710678118654752f;
+constexpr float kTanhScale = 0.79788456080286536f;      // sqrt(2 / pi)
+constexpr float kTanhCubic = 0.044715f;
+
+// 1 / (1 + exp(-t))
+template <bool exact>
+__device__ __forceinline__ float logistic(float t) {
+    if constexpr (exact) return 1.0f / (1.0f + expf(-t));
+    else return __builtin_amdgcn_rcpf(1.0f + __expf(-t));
+}
+
+template <bool exact>
+__device__ __forceinline__ float activate(int act, float z) {
+    switch (act) {
+        case BC_ACT_RELU: return z < 0.0f ? 0.0f : z;  // NaN stays
+        case BC_ACT_GELU: return 0.5f * z * erfcf(-z * kSqrtHalf);
+        // 0.5 (1 + tanh t) is the logistic function of 2 t
+        case BC_ACT_GELU_TANH: return z * logistic<exact>(2.0f * kTanhScale * (z + kTanhCubic * z * z * z));
+        case BC_ACT_SILU: return z * logistic<exact>(z);
+        default: return z;
+    }
+}
+
+template <bool exact>
+__device__ __forceinline__ float act_slope(int act, float z) {
+    switch (act) {
+        case BC_ACT_RELU: return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+        case BC_ACT_GELU:
+            return 0.5f * erfcf(-z * kSqrtHalf) +
+                   z * (0.5f * kTanhScale) * (exact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
+        case BC_ACT_GELU_TANH: {
+            const float p = logistic<exact>(2.0f * kTanhScale * (z + kTanhCubic * z * z * z));
+            return p + z * p * (1.0f - p) * (2.0f * kTanhScale) * (1.0f + 3.0f * kTanhCubic * z * z);
+        }
+        case BC_ACT_SILU: {
+            const float p = logistic<exact>(z);
+            return p + z * p * (1.0f - p);
+        }
+        default: return 1.0f;
+    }
+}
+
+// ------------------------------------------------------------------ lay_out
+// A workgroup 64 rows x 64 columns: read once, written flat from registers and
+// turned through LDS, eight elements (16 bytes) of a plane at a time.
+template <typename T>
+struct PlaneOf {
+    typedef T type;
+    static constexpr int P = 1;
+};
+template <>
+struct PlaneOf<float> {
+    typedef bf16_t type;
+    static constexpr int P = 3;
+};
+
+// v as P planes of eight elements at p, p + plane, ...
+template <typename T>
+__device__ __forceinline__ void store_planes(typename PlaneOf<T>::type* p, uint64_t plane, const float (&v)[8]) {
+    typedef typename PlaneOf<T>::type E;
+    typedef E vec __attribute__((ext_vector_type(8)));
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = v[i];
+#pragma unroll
+    for (int q = 0; q < PlaneOf<T>::P; ++q) {
+        vec w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[i] = (E)rest[i];
+            rest[i] -= (float)w[i];  // exact
+        }
+        *(vec*)(p + q * plane) = w;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void lay_out(LayOut a) {
+    typedef typename PlaneOf<T>::type E;
+    __shared__ float tile[64][65];
+    __shared__ float sums[4][64];
+    const uint64_t flat_ld = plane_cols(a.cols), turned_ld = plane_cols(a.rows);
+    const uint32_t across = (uint32_t)(flat_ld / 64), by = blockIdx.x / across;
+    const uint32_t r0 = by * 64, c0 = blockIdx.x % across * 64;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lr = threadIdx.x / 8 + 32 * i, lc = threadIdx.x % 8 * 8;
+        const uint32_t r = r0 + lr, c = c0 + lc;
+        const int left = r < a.rows && c < a.cols ? (int)(a.cols - c) : 0;
+        float v[8];
+        load_vec((const T*)a.in + (left ? r * a.ld_in + c : 0), left, v);
+        if (a.z) {
+            float z[8];
+            load_vec((const T*)a.z + (left ? r * a.ld_z + c : 0), left, z);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] * act_slope<sizeof(T) == 4>(a.act, z[j]) : 0.0f;
+        }
+        if (a.flat && r < a.rows && c < flat_ld)
+            store_planes<T>((E*)a.flat + r * flat_ld + c, (uint64_t)a.rows * flat_ld, v);
+        if (a.turned || a.part)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];
+    }
+    if (!a.turned && !a.part) return;
+    __syncthreads();
+    if (a.turned)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t lc = threadIdx.x / 8 + 32 * i, lr = threadIdx.x % 8 * 8;
+            const uint32_t c = c0 + lc, r = r0 + lr;
+            if (c < a.cols && r < turned_ld) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = tile[lr + j][lc];
+                store_planes<T>((E*)a.turned + c * turned_ld + r, (uint64_t)a.cols * turned_ld, v);
+            }
+        }
+    if (a.part) {
+        const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += tile[g * 16 + r][c];
+        sums[g][c] = s;
+        __syncthreads();
+        if (g == 0 && c0 + c < a.cols)
+            a.part[(uint64_t)by * a.cols + c0 + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+    }
+}
+
+// ----------------------------------------------------------------- products
+template <typename G, typename TO, bool forward>
+__global__ __launch_bounds__(G::kThreads) void product(Product p) {
+    typedef typename G::T T;
+    extern __shared__ char lds[];
+    uint32_t tm, tn;
+    tile_of<8>(blockIdx.x, (p.rows + G::kBM - 1) / G::kBM, (p.cols + G::kBN - 1) / G::kBN, tm, tn);
+    const uint32_t m0 = tm * G::kBM, n0 = tn * G::kBN;
+    const Operand<T> a{(const T*)p.a.p + m0 * p.a.ld, (uint32_t)p.a.ld, p.a.plane, p.rows - m0};
+    const Operand<T> b{(const T*)p.b.p + n0 * p.b.ld, (uint32_t)p.b.ld, p.b.plane, p.cols - n0};
+    G g;
+    g.multiply(a, b, p.steps * (kPlaneCols / G::kBK), lds);
+    constexpr bool exact = sizeof(TO) == 4;
+    g.finish(lds, [&](int row, int col, float (&v)[8]) {
+        const uint64_t m = m0 + row;
+        const uint32_t n = n0 + col;
+        if (m >= p.rows || n >= p.cols) return;
+        const int left = (int)(p.cols - n);
+        if constexpr (forward) {
+            float t[8];
+            if (p.bias) {
+                load_vec((const TO*)p.bias + n, left, t);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += t[i];
+            }
+            if (p.z) store_vec((TO*)p.z + m * p.ld_z + n, left, v);
+            if (p.act != BC_ACT_NONE)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate<exact>(p.act, v[i]);
+            if (p.residual) {
+                load_vec((const TO*)p.residual + m * p.ld_residual + n, left, t);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += t[i];
+            }
+        }
+        store_vec((TO*)p.out + m * p.ld_out + n, left, v);
+    });
+}
+
+template <typename G, typename TO, bool forward>
+hipError_t launch_tiles(const Product& p, hipStream_t s) {
+    // more LDS than a kernel may use by default; the attribute is per device
+    // and setting it again costs next to nothing
+    const hipError_t e = hipFuncSetAttribute((const void*)product<G, TO, forward>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+    if (e != hipSuccess) return e;
+    const uint32_t tiles = ((p.rows + G::kBM - 1) / G::kBM) * ((p.cols + G::kBN - 1) / G::kBN);
+    hipLaunchKernelGGL((product<G, TO, forward>), dim3(tiles), dim3(G::kThreads), G::kLdsBytes, s, p);
+    return hipGetLastError();
+}
+
+template <typename T, typename TO, bool forward>
+hipError_t pick_tiles(const Product& p, hipStream_t s) {
+    if constexpr (PlaneOf<T>::P == 3) {
+        return launch_tiles<GemmTile<bf16_t, 3, 128, 128, 32, 2, 2, 2>, TO, forward>(p, s);
+    } else {
+        const uint64_t big = (uint64_t)((p.rows + 255) / 256) * ((p.cols + 255) / 256);
+        if (big >= 160) return launch_tiles<GemmTile<T, 1, 256, 256, 64, 2, 4, 2>, TO, forward>(p, s);
+        return launch_tiles<GemmTile<T, 1, 128, 128, 64, 2, 2, 2>, TO, forward>(p, s);
+    }
+}
+
+// ----------------------------------------------------------------- few rows
+// At most 64 rows of x: the weight's bytes are the cost, and every workgroup
+// reads its 16 rows of w once, straight into the first operand of the
+// 16x16x32 matrix instruction; its waves share out the inner axis and meet in
+// LDS.  The second operand holds kGroups groups of 16 rows of x.
+constexpr int kFewWaves = 8;
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct FewFrag {
+    typedef typename Frag<T>::type type;
+    static constexpr int kStep = 32;
+    static __device__ __forceinline__ void load(const T* p, int left, type& f) {
+        if (left >= 8) {
+            __builtin_memcpy(&f, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = i < left ? p[i] : (T)0.0f;
+        }
+    }
+    static __device__ __forceinline__ f32x4_t mma(type a, type b, f32x4_t c) {
+        if constexpr (__is_same(T, f16_t)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+// fp32: four 16x16x4 instructions, the k of lane group g's element i being
+// 4 g + i in both operands.
+template <>
+struct FewFrag<float> {
+    typedef f32x4_t type;
+    static constexpr int kStep = 16;
+    static __device__ __forceinline__ void load(const float* p, int left, type& f) {
+        if (left >= 4) {
+            __builtin_memcpy(&f, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = i < left ? p[i] : 0.0f;
+        }
+    }
+    static __device__ __forceinline__ f32x4_t mma(type a, type b, f32x4_t c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <typename T, int kGroups>
+__global__ __launch_bounds__(64 * kFewWaves) void few_rows(FewRows a) {
+    typedef FewFrag<T> F;
+    constexpr int kEach = F::kStep / 4;         // elements of a lane and step
+    __shared__ float meet[kFewWaves][kGroups][16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t n0 = blockIdx.x * 16;
+    const uint32_t n = n0 + (lane & 15), kl = (lane >> 4) * kEach;
+    const T* w = (const T*)a.w + (uint64_t)(n < a.cols ? n : a.cols - 1) * a.ldw;
+    const T* x[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const uint32_t m = g * 16 + (lane & 15);
+        x[g] = (const T*)a.x + (uint64_t)(m < a.rows ? m : a.rows - 1) * a.ldx;
+    }
+    f32x4_t acc[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) acc[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t steps = (a.inner + F::kStep - 1) / F::kStep;
+    const uint32_t whole = a.inner / F::kStep;
+    constexpr int kAhead = kGroups > 2 ? 2 : 4;
+    uint32_t s = wave;
+    // kAhead steps of loads go out before the first is used
+    for (; s + (kAhead - 1) * kFewWaves < whole; s += kAhead * kFewWaves) {
+        typename F::type fw[kAhead], fx[kAhead][kGroups];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t k = (s + u * kFewWaves) * F::kStep + kl;
+            F::load(w + k, kEach, fw[u]);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) F::load(x[g] + k, kEach, fx[u][g]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) acc[g] = F::mma(fw[u], fx[u][g], acc[g]);
+    }
+    for (; s < steps; s += kFewWaves) {
+        const uint32_t k = s * F::kStep + kl;
+        const int left = k < a.inner ? (int)(a.inner - k) : 0;
+        typename F::type fw, fx;
+        F::load(w + (left ? k : 0), left, fw);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            F::load(x[g] + (left ? k : 0), left, fx);
+            acc[g] = F::mma(fw, fx, acc[g]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) meet[wave][g][lane & 15][(lane >> 4) * 4 + r] = acc[g][r];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 16 * 16 * kGroups; i += 64 * kFewWaves) {
+        const uint32_t m = i / 16, c = n0 + i % 16;
+        if (m >= a.rows || c >= a.cols) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kFewWaves; ++q) v += meet[q][m / 16][m % 16][i % 16];
+        if (a.bias) v += (float)((const T*)a.bias)[c];
+        if (a.z) ((T*)a.z)[m * a.ldz + c] = (T)v;
+        v = activate<sizeof(T) == 4>(a.act, v);
+        if (a.residual) v += (float)((const T*)a.residual)[m * a.ld_residual + c];
+        ((T*)a.y)[m * a.ldy + c] = (T)v;
+    }
+}
+
+template <typename T>
+void few_rows_launch(const FewRows& a, hipStream_t s) {
+    const dim3 grid((a.cols + 15) / 16), block(64 * kFewWaves);
+    if (a.rows <= 16) hipLaunchKernelGGL((few_rows<T, 1>), grid, block, 0, s, a);
+    else if (a.rows <= 32) hipLaunchKernelGGL((few_rows<T, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_rows<T, 4>), grid, block, 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_lay_out(int dtype, const LayOut& a, hipStream_t s) {
+    const dim3 grid((uint32_t)(plane_cols(a.cols) / 64 * (plane_cols(a.rows) / 64))), block(256);
+    if (grid.x == 0) return hipSuccess;
+    if (dtype == BC_F32) hipLaunchKernelGGL(lay_out<float>, grid, block, 0, s, a);
+    else if (dtype == BC_F16) hipLaunchKernelGGL(lay_out<f16_t>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(lay_out<bf16_t>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_product(int dtype, int out_dtype, bool forward, const Product& p, hipStream_t s) {
+    if (p.rows == 0 || p.cols == 0) return hipSuccess;
+    if (forward) {
+        if (dtype == BC_F32) return pick_tiles<float, float, true>(p, s);
+        if (dtype == BC_F16) return pick_tiles<f16_t, f16_t, true>(p, s);
+        return pick_tiles<bf16_t, bf16_t, true>(p, s);
+    }
+    if (dtype == BC_F32) return pick_tiles<float, float, false>(p, s);
+    if (dtype == BC_F16) {
+        if (out_dtype == BC_F32) return pick_tiles<f16_t, float, false>(p, s);
+        return pick_tiles<f16_t, f16_t, false>(p, s);
+    }
+    if (out_dtype == BC_F32) return pick_tiles<bf16_t, float, false>(p, s);
+    return pick_tiles<bf16_t, bf16_t, false>(p, s);
+}
+
+hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s) {
+    if (dtype == BC_F32) few_rows_launch<float>(a, s);
+    else if (dtype == BC_F16) few_rows_launch<f16_t>(a, s);
+    else few_rows_launch<bf16_t>(a, s);
+    return hipGetLastError();
+}
+
+}  // namespace bc

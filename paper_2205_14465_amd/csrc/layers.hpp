@@ -35,4 +35,55 @@ hipError_t launch_ln_backward(int dtype, int wdtype, const LnBackward& a, void* 
 hipError_t launch_sum_parts(int dtype, const float* part, uint32_t parts, uint64_t stride, uint32_t cols, void* out0,
                             void* out1, hipStream_t s);
 
+// ---------------------------------------------------------- linear layer
+// Operand planes of the product kernels (gemm.hpp): 16-bit elements, rows
+// `ld` apart, a multiple of kPlaneCols long and zero past the operand's end.
+constexpr uint32_t kPlaneCols = 64;
+__host__ __device__ constexpr uint64_t plane_cols(uint64_t k) { return (k + kPlaneCols - 1) / kPlaneCols * kPlaneCols; }
+// Planes of an element type: fp32 as three bfloat16 parts.
+inline int planes_of(int dtype) { return dtype == BC_F32 ? 3 : 1; }
+
+// An operand for the product kernels: planes in memory.
+struct Planes {
+    const void* p;
+    uint64_t ld, plane;      // elements from row to row, from plane to plane
+};
+
+// A matrix laid out as planes: v = in, or in * act'(z) where z is given.
+struct LayOut {
+    const void *in, *z;
+    uint64_t ld_in, ld_z;
+    uint32_t rows, cols;
+    void* flat;              // [P][rows][plane_cols(cols)], or NULL
+    void* turned;            // [P][cols][plane_cols(rows)], or NULL
+    float* part;             // [ceil(rows / 64)][cols] column sums of v, or NULL
+    int act;
+};
+hipError_t launch_lay_out(int dtype, const LayOut& a, hipStream_t s);
+
+// out [rows, cols] = epilogue(A B^T), A [rows, k], B [cols, k] as planes.
+struct Product {
+    Planes a, b;
+    uint32_t rows, cols, steps;   // steps of kPlaneCols along k
+    void* out;
+    uint64_t ld_out;
+    // forward only: z = product + bias, out = act(z) + residual
+    const void *bias, *residual;
+    void* z;
+    uint64_t ld_residual, ld_z;
+    int act;
+};
+hipError_t launch_product(int dtype, int out_dtype, bool forward, const Product& p, hipStream_t s);
+
+// The forward pass for few rows: x and w as the caller has them.
+struct FewRows {
+    const void *x, *w, *bias, *residual;
+    void *y, *z;
+    uint64_t ldx, ldw, ld_residual, ldy, ldz;
+    uint32_t rows, inner, cols;
+    int act;
+};
+constexpr uint32_t kFewRows = 64;
+hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s);
+
 }  // namespace bc

@@ -47,3 +47,41 @@ def test_layernorm_refusals():
 
 def test_status_text():
     assert B.lib().bytecomp_strerror(-11) not in (b"", b"unknown status")
+
+
+def test_linear_refusals():
+    L = B.lib()
+
+    def fwd(dtype=1, rows=70, inner=64, cols=32, x=X, ldx=64, w=W, ldw=64, b=None, act=0, r=None, ldr=0, y=Y, ldy=32,
+            z=None, ldz=0, ws=None, n=0):
+        return L.bytecomp_linear_forward(dtype, rows, inner, cols, x, ldx, w, ldw, b, act, r, ldr, y, ldy, z, ldz, ws, n,
+                                         None)
+
+    assert fwd(dtype=3) == -3 and fwd(act=5) == -2 and fwd(act=-1) == -2
+    assert fwd(rows=1 << 22) == -5 and fwd(inner=1 << 22) == -5 and fwd(cols=1 << 22) == -5
+    assert fwd(ldx=63) == -5 and fwd(ldw=63) == -5 and fwd(ldy=31) == -5
+    assert fwd(r=Y, ldr=31) == -5 and fwd(z=Y, ldz=31) == -5
+    assert fwd(x=None) == -1 and fwd(w=None) == -1 and fwd(y=None) == -1
+    assert fwd(x=P(0x10001)) == -9 and fwd(b=P(0x10001)) == -9 and fwd(ws=P(0x40008), n=1 << 30) == -9
+    assert fwd(rows=0) == 0 and fwd(cols=0) == 0
+    # fp32 and odd sizes are laid out first
+    need = B.bytecomp_linear_workspace_size(0, 70, 64, 32)
+    assert need > 0 and fwd(dtype=0) == -7 and fwd(dtype=0, ws=WS, n=need - 1) == -7
+    assert fwd(inner=63) == -7
+    assert B.bytecomp_linear_workspace_size(1, 64, 64, 32) == 0
+
+    def bwd(dtype=1, gdtype=1, dy=Y, lddy=32, z=Y, ldz=32, act=1, x=X, ldx=64, w=W, ldw=64, dx=X, lddx=64, dw=W,
+            lddw=64, db=W, ws=WS, n=1 << 30, rows=70):
+        return L.bytecomp_linear_backward(dtype, gdtype, rows, 64, 32, dy, lddy, z, ldz, act, x, ldx, w, ldw, dx, lddx,
+                                          dw, lddw, db, ws, n, None)
+
+    assert bwd(gdtype=2) == -3 and bwd(dtype=0, gdtype=1) == -3 and bwd(act=9) == -2
+    assert bwd(dy=None) == -1 and bwd(z=None) == -1 and bwd(x=None) == -1 and bwd(w=None) == -1
+    assert bwd(lddx=63) == -5 and bwd(lddw=63) == -5 and bwd(ldz=31) == -5
+    assert bwd(gdtype=0, dw=P(0x30002)) == -9
+    need = B.bytecomp_linear_workspace_size(1, 70, 64, 32, True)
+    assert bwd(n=need - 1) == -7 and bwd(ws=None) == -7
+    assert bwd(dx=None, dw=None, db=None) == 0
+    with pytest.raises(B.BytecompError) as e:
+        B.bytecomp_linear_workspace_size(7, 1, 1, 1)
+    assert e.value.code == -3
