@@ -524,6 +524,64 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
                              const void* w, uint64_t ldw, void* dx, uint64_t lddx, void* dw, uint64_t lddw,
                              void* dbias, void* ws, size_t ws_bytes, void* stream);
 
+/* Orthogonalised updates (the Muon optimiser's step): for each matrix U of
+ * the call, with X its shorter side as rows,
+ *   X = U / (|U| + eps), |U| the Frobenius norm,
+ *   `steps` times: A = X X^T, X <- a X + (b A + c A^2) X,
+ * which drives every singular value of X towards 1.
+ * Factors are kept as pairs of fp16 (22 bits), sums in fp32, the norm in
+ * fp64: the results are as close to the exact ones as fp32 arithmetic's. */
+
+/* One matrix: out [rows, cols] receives the orthogonalised update
+ * [rows, cols]; out may be update itself (same stride). */
+typedef struct bc_update {
+    const void* update;
+    void* out;
+    uint64_t ld_update, ld_out;
+    uint64_t rows, cols;
+} bc_update;
+
+/* One parameter of an optimizer step: weight, gradient and fp32 momentum
+ * [rows, cols]; scale multiplies the learning rate for this matrix (a
+ * usual choice is sqrt(max(1, rows / cols))). */
+typedef struct bc_param {
+    void* weight;
+    const void* grad;
+    float* momentum;
+    uint64_t ld_weight, ld_grad, ld_momentum;
+    uint64_t rows, cols;
+    double scale;
+} bc_param;
+
+/* Bytes of workspace that the two calls below need for matrices of these
+ * shapes (host arrays of T row and column counts; host only): 12 bytes an
+ * element and 8 for each of min(rows, cols)^2, rounded up to whole 64s. */
+int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* cols, int T, size_t* bytes);
+
+/* Orthogonalise T updates.
+ *   dtype  of every update and out
+ *   steps  1 to 64 (BC_E_VALUE)
+ *   coefficients  host, a, b and c; BC_E_VALUE when they are not finite or
+ *          take a singular value of at most 1 past 64 within the steps
+ *   eps    finite and >= 0 (BC_E_VALUE)
+ *   ws     256-byte aligned
+ * rows and cols < 2^22 (BC_E_SIZE); empty matrices are skipped.  A NaN or
+ * an infinity reaches its whole matrix and no other. */
+int bytecomp_orthogonalize(int dtype, const bc_update* t, int T, int steps, const double* coefficients, double eps,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/* One optimizer step on T parameters, in place, with g the gradient and m
+ * the momentum:
+ *   m <- fl32(fl32(momentum * m) + g)
+ *   U  = nesterov ? fl32(fl32(momentum * m) + g) : m, orthogonalised to O
+ *   w <- (1 - lr * weight_decay) w - lr * scale * O
+ *   wdtype, gdtype  of every weight and gradient
+ *   lr, momentum, weight_decay, scale  finite (BC_E_VALUE)
+ * Every other argument is bytecomp_orthogonalize's. */
+int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double lr, double momentum, int nesterov,
+                       double weight_decay, int steps, const double* coefficients, double eps, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

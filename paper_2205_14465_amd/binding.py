@@ -38,6 +38,17 @@ class bc_payload(ctypes.Structure):
                 ("scale", ctypes.c_void_p)]
 
 
+class bc_update(ctypes.Structure):
+    _fields_ = [("update", ctypes.c_void_p), ("out", ctypes.c_void_p), ("ld_update", ctypes.c_uint64),
+                ("ld_out", ctypes.c_uint64), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64)]
+
+
+class bc_param(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
+                ("ld_weight", ctypes.c_uint64), ("ld_grad", ctypes.c_uint64), ("ld_momentum", ctypes.c_uint64),
+                ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("scale", ctypes.c_double)]
+
+
 class BytecompError(RuntimeError):
     def __init__(self, fn, code):
         self.code = code
@@ -125,6 +136,13 @@ def lib():
         L.bytecomp_linear_backward.restype = i32
         L.bytecomp_linear_backward.argtypes = [i32, i32, u64, u64, u64, vp, u64, vp, u64, i32, vp, u64, vp, u64, vp,
                                                u64, vp, u64, vp, vp, sz, vp]
+        L.bytecomp_orthogonalize_workspace_size.restype = i32
+        L.bytecomp_orthogonalize_workspace_size.argtypes = [vp, vp, i32, ctypes.POINTER(sz)]
+        L.bytecomp_orthogonalize.restype = i32
+        L.bytecomp_orthogonalize.argtypes = [i32, ctypes.POINTER(bc_update), i32, i32, vp, dbl, vp, sz, vp]
+        L.bytecomp_muon_step.restype = i32
+        L.bytecomp_muon_step.argtypes = [i32, i32, ctypes.POINTER(bc_param), i32, dbl, dbl, i32, dbl, i32, vp, dbl, vp,
+                                         sz, vp]
         _lib = L
     return _lib
 
@@ -757,3 +775,104 @@ def bytecomp_linear_forward(x, w, bias, residual, activation, y, z=None, ws=None
 def bytecomp_linear_backward(dy, z, x, w, activation, dx, dw, dbias, ws, stream=None):
     """The gradients of bytecomp_linear_forward; see LinearGradCall."""
     LinearGradCall(dy, z, x, w, activation, dx, dw, dbias, ws, stream)()
+
+
+# Coefficients of the quintic that the Muon optimiser's five steps use: they
+# take every singular value from a thousandth to 1 to between 0.7 and 1.2.
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def bytecomp_orthogonalize_workspace_size(shapes):
+    """shapes: (rows, cols) of every matrix of the call."""
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_orthogonalize_workspace_size",
+           lib().bytecomp_orthogonalize_workspace_size(_u64_array([r for r, _ in shapes]),
+                                                       _u64_array([c for _, c in shapes]), len(shapes),
+                                                       ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_orthogonalize_workspace(shapes, device="cuda"):
+    return _alloc_bytes(bytecomp_orthogonalize_workspace_size(shapes), device)
+
+
+def _one_dtype(name, tensors):
+    """The dtype that all of a list's tensors share (fp32 for an empty list)."""
+    import torch
+    found = {t.dtype for t in tensors}
+    if len(found) > 1:
+        raise ValueError(f"{name}: one element type in a call, got {sorted(map(str, found))}")
+    return found.pop() if found else torch.float32
+
+
+def _dtype_code(dtype):
+    import torch
+    return {torch.float32: BC_F32, torch.float16: BC_F16, torch.bfloat16: BC_BF16}.get(dtype, 99)
+
+
+class OrthogonalizeCall(_Call):
+    """bytecomp_orthogonalize: outs[i] receives updates[i] orthogonalised
+    (lists of matrices of one type; outs may be the updates); ws from
+    alloc_orthogonalize_workspace of their shapes."""
+
+    def __init__(self, updates, outs, ws, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, stream=None):
+        T = len(updates)
+        if len(outs) != T:
+            raise ValueError(f"{T} updates, {len(outs)} outs")
+        dt = _one_dtype("updates", updates)
+        arr = (bc_update * max(T, 1))()
+        for i, (u, o) in enumerate(zip(updates, outs)):
+            r, c = u.shape
+            arr[i].update, arr[i].ld_update = _matrix(f"updates[{i}]", u, r, c, dt)
+            arr[i].out, arr[i].ld_out = _matrix(f"outs[{i}]", o, r, c, dt)
+            arr[i].rows, arr[i].cols = r, c
+        k = (ctypes.c_double * 3)(*coefficients)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_orthogonalize",
+                         (_dtype_code(dt), arr, T, int(steps), k, float(eps), p, n, _stream_handle(stream)),
+                         (updates, outs, ws))
+
+
+class MuonCall(_Call):
+    """bytecomp_muon_step on lists of matrices, in place: weights (one type),
+    grads (one type) and fp32 momenta; called with the step's learning rate.
+    scales: the learning rate's factor for each matrix (default
+    sqrt(max(1, rows / cols))); ws as for OrthogonalizeCall."""
+
+    def __init__(self, weights, grads, momenta, ws, momentum=0.95, nesterov=True, weight_decay=0.0, scales=None,
+                 steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, stream=None):
+        import torch
+        T = len(weights)
+        if len(grads) != T or len(momenta) != T or (scales is not None and len(scales) != T):
+            raise ValueError(f"{T} weights, {len(grads)} grads, {len(momenta)} momenta"
+                             + ("" if scales is None else f", {len(scales)} scales"))
+        wd, gd = _one_dtype("weights", weights), _one_dtype("grads", grads)
+        arr = (bc_param * max(T, 1))()
+        for i, (w, g, m) in enumerate(zip(weights, grads, momenta)):
+            r, c = w.shape
+            arr[i].weight, arr[i].ld_weight = _matrix(f"weights[{i}]", w, r, c, wd)
+            arr[i].grad, arr[i].ld_grad = _matrix(f"grads[{i}]", g, r, c, gd)
+            arr[i].momentum, arr[i].ld_momentum = _matrix(f"momenta[{i}]", m, r, c, torch.float32)
+            arr[i].rows, arr[i].cols = r, c
+            arr[i].scale = max(1.0, r / max(c, 1)) ** 0.5 if scales is None else float(scales[i])
+        k = (ctypes.c_double * 3)(*coefficients)
+        p, n = _ws(ws)
+        self._head = (_dtype_code(wd), _dtype_code(gd), arr, T)
+        self._tail = (float(momentum), int(bool(nesterov)), float(weight_decay), int(steps), k, float(eps), p, n,
+                      _stream_handle(stream))
+        super().__init__("bytecomp_muon_step", None, (weights, grads, momenta, ws))
+
+    def __call__(self, lr):
+        _check(self._fn, self._entry(*self._head, float(lr), *self._tail))
+
+
+def bytecomp_orthogonalize(updates, outs, ws, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, stream=None):
+    """Orthogonalised updates; see OrthogonalizeCall."""
+    OrthogonalizeCall(updates, outs, ws, steps, coefficients, eps, stream)()
+
+
+def bytecomp_muon_step(weights, grads, momenta, lr, ws, momentum=0.95, nesterov=True, weight_decay=0.0, scales=None,
+                       steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, stream=None):
+    """One optimizer step, in place; see MuonCall."""
+    MuonCall(weights, grads, momenta, ws, momentum, nesterov, weight_decay, scales, steps, coefficients, eps,
+             stream)(lr)

@@ -86,6 +86,150 @@ hipError_t operand(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_
     return launch_lay_out(dtype, a, s);
 }
 
+// -------------------------------------------------- orthogonalised updates
+constexpr int kMaxMatrices = 1 << 20;
+
+// The scales that keep X, A and B (kernels_ortho.hip) in fp16's range: the
+// largest singular value that the steps reach from [0, 1], and the largest
+// |b y + c y^2| for y up to its square, each rounded up to a power of two.
+// False: not finite, or past 64.
+bool ortho_scales(int steps, const double* k, float& top, float& gram_scale, float& poly_scale) {
+    const double a = k[0], b = k[1], c = k[2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double reach = 1.0, most = 1.0;
+    for (int i = 0; i + 1 < steps; ++i) {
+        auto f = [&](double x) { return std::fabs(x * (a + x * x * (b + c * x * x))); };
+        double next = f(reach);
+        // f' = a + 3 b y + 5 c y^2 with y = x^2
+        double y[2] = {-1.0, -1.0};
+        if (c != 0.0) {
+            const double d = 9.0 * b * b - 20.0 * a * c;
+            if (d >= 0.0) {
+                y[0] = (-3.0 * b + std::sqrt(d)) / (10.0 * c);
+                y[1] = (-3.0 * b - std::sqrt(d)) / (10.0 * c);
+            }
+        } else if (b != 0.0) {
+            y[0] = -a / (3.0 * b);
+        }
+        for (const double v : y)
+            if (v > 0.0 && v < reach * reach) next = std::fmax(next, f(std::sqrt(v)));
+        reach = next * 1.001;  // and what rounding adds
+        most = std::fmax(most, reach);
+        if (!(most <= 64.0)) return false;
+    }
+    auto p = [&](double y) { return std::fabs(y * (b + c * y)); };
+    double poly = p(most * most);
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < most * most) poly = std::fmax(poly, p(-b / (2.0 * c)));
+    auto above = [](double x) { return std::exp2(std::ceil(std::log2(x * 1.001))); };
+    const double hx = above(most), hp = poly > 0x1p-40 ? above(poly) : 0x1p-40;
+    if (!(hp <= 0x1p40)) return false;
+    top = (float)(0x1p15 / hx);
+    gram_scale = (float)(0x1p15 / (hx * hx));
+    poly_scale = (float)(0x1p15 / hp);
+    return true;
+}
+
+// Workspace offsets and workgroup counts of one matrix; `at` advances.
+void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoCall& c, Ortho& o) {
+    auto take = [&](uint64_t bytes) {
+        const uint64_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    o.rows = (uint32_t)rows;
+    o.cols = (uint32_t)cols;
+    o.turned = rows > cols;
+    o.m = o.turned ? o.cols : o.rows;
+    o.n = o.turned ? o.rows : o.cols;
+    o.part0 = c.parts;
+    o.tile0 = c.tiles;
+    for (int i = 0; i < 2; ++i) {
+        o.sym0[i] = c.sym[i];
+        o.full0[i] = c.full[i];
+    }
+    if (rows == 0 || cols == 0) return;
+    const uint64_t m = o.m, n = o.n, mp = plane_cols(m), np = plane_cols(n);
+    o.x = take(4 * m * np);
+    o.xt = take(8 * n * mp);
+    o.gram = take(4 * m * mp);
+    o.poly = take(4 * m * mp);
+    const uint64_t tiles = plane_cols(rows) / 64 * (plane_cols(cols) / 64);
+    o.parts = (uint32_t)(tiles < kOrthoParts ? tiles : kOrthoParts);
+    o.part = take(8 * o.parts);
+    c.parts += o.parts;
+    c.tiles += (uint32_t)tiles;
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t side = i ? 256 : 128, a = (m + side - 1) / side, b = (n + side - 1) / side;
+        c.sym[i] += (uint32_t)(a * (a + 1) / 2);
+        c.full[i] += (uint32_t)(a * b);
+    }
+}
+
+int check_ortho(int T, int steps, const double* k, double eps, float& top, OrthoCall& c) {
+    if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
+    if (!k) return BC_E_NULL;
+    if (steps < 1 || steps > 64 || !(eps >= 0.0) || std::isinf(eps)) return BC_E_VALUE;
+    if (!ortho_scales(steps, k, top, c.gram_scale, c.poly_scale)) return BC_E_VALUE;
+    c.a = (float)k[0];
+    c.b = (float)k[1];
+    c.c = (float)k[2];
+    c.eps = (float)eps;
+    c.steps = steps;
+    c.T = T;
+    return BC_OK;
+}
+
+// get(i, rows, cols, o): matrix i's shape, pointers and strides, or its
+// error.  The rest of the call: plan, table, launch.
+template <typename Get>
+int run_ortho(OrthoCall& c, float top, void* ws, size_t ws_bytes, hipStream_t s, Get get) {
+    std::vector<Ortho> table;
+    uint64_t at = 0, tiles = 0;
+    try {
+        table.resize((size_t)c.T);
+        std::memset((void*)table.data(), 0, table.size() * sizeof(Ortho));
+        for (int i = 0; i < c.T; ++i) {
+            uint64_t rows = 0, cols = 0;
+            Ortho& o = table[(size_t)i];
+            if (const int rc = get(i, rows, cols, o)) return rc;
+            if (rows >= kMaxDim || cols >= kMaxDim) return BC_E_SIZE;
+            tiles += plane_cols(rows) / 64 * (plane_cols(cols) / 64);
+            if (tiles >= (1ull << 31)) return BC_E_SIZE;  // workgroup counts stay within 32 bits
+            plan_matrix(rows, cols, at, c, o);
+            const double side = std::sqrt((double)rows * (double)cols);
+            o.x_scale = side > 1.0 ? std::fmin(top, (float)std::exp2(std::floor(std::log2(side)))) : std::fmin(top, 1.0f);
+        }
+    } catch (const std::bad_alloc&) {
+        return BC_E_SIZE;
+    }
+    if (c.tiles == 0) return BC_OK;
+    if (!ws || ws_bytes < at) return BC_E_WORKSPACE;
+    if ((uintptr_t)ws & 255) return BC_E_ALIGN;
+    c.ws = (char*)ws;
+    int dev = 0;
+    DevInfo di;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess) e = device_info(dev, &di);
+    if (e != hipSuccess) return BC_E_HIP;
+    c.cus = di.cus;
+    struct Ctx {
+        OrthoCall* c;
+        hipStream_t s;
+    } ctx{&c, s};
+    try {
+        e = with_table(table.data(), table.size() * sizeof(Ortho), s,
+                       [](void* p, const void* dev_table) {
+                           Ctx* x = (Ctx*)p;
+                           x->c->d = (const Ortho*)dev_table;
+                           return launch_orthogonalize(*x->c, x->s);
+                       },
+                       &ctx);
+    } catch (const std::bad_alloc&) {
+        return BC_E_SIZE;
+    }
+    return finish_call(status_of(e), s, nullptr);
+}
+
 }  // namespace
 
 extern "C" {
@@ -256,6 +400,85 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
         if (e == hipSuccess) e = launch_product(dtype, gdtype, false, p, s);
     }
     return finish_call(status_of(e), s, nullptr);
+}
+
+int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* cols, int T, size_t* bytes) {
+    if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
+    if (!bytes || (T > 0 && (!rows || !cols))) return BC_E_NULL;
+    OrthoCall c{};
+    uint64_t at = 0;
+    for (int i = 0; i < T; ++i) {
+        if (rows[i] >= kMaxDim || cols[i] >= kMaxDim) return BC_E_SIZE;
+        Ortho o{};
+        plan_matrix(rows[i], cols[i], at, c, o);
+    }
+    *bytes = (size_t)at;
+    return BC_OK;
+}
+
+int bytecomp_orthogonalize(int dtype, const bc_update* t, int T, int steps, const double* coefficients, double eps,
+                           void* ws, size_t ws_bytes, void* stream) {
+    const CallRange range("bytecomp_orthogonalize");
+    if (!dtype_ok(dtype)) return BC_E_DTYPE;
+    OrthoCall c{};
+    float top = 0.0f;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, top, c)) return rc;
+    if (T == 0) return BC_OK;
+    if (!t) return BC_E_NULL;
+    c.in_dtype = c.out_dtype = dtype;
+    return run_ortho(c, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+        const bc_update& u = t[i];
+        rows = u.rows;
+        cols = u.cols;
+        if (rows == 0 || cols == 0) return (int)BC_OK;
+        if (!u.update || !u.out) return (int)BC_E_NULL;
+        if (u.ld_update < cols || u.ld_out < cols) return (int)BC_E_SIZE;
+        if (misaligned(u.update, dtype) || misaligned(u.out, dtype)) return (int)BC_E_ALIGN;
+        o.in = u.update;
+        o.out = u.out;
+        o.ld_in = u.ld_update;
+        o.ld_out = u.ld_out;
+        return (int)BC_OK;
+    });
+}
+
+int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double lr, double momentum, int nesterov,
+                       double weight_decay, int steps, const double* coefficients, double eps, void* ws,
+                       size_t ws_bytes, void* stream) {
+    const CallRange range("bytecomp_muon_step");
+    if (!dtype_ok(wdtype) || !dtype_ok(gdtype)) return BC_E_DTYPE;
+    OrthoCall c{};
+    float top = 0.0f;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, top, c)) return rc;
+    if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay)) return BC_E_VALUE;
+    if (T == 0) return BC_OK;
+    if (!t) return BC_E_NULL;
+    c.in_dtype = gdtype;
+    c.out_dtype = wdtype;
+    c.muon = true;
+    c.nesterov = nesterov != 0;
+    c.momentum = (float)momentum;
+    c.keep = (float)(1.0 - lr * weight_decay);
+    c.lr = (float)lr;
+    return run_ortho(c, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+        const bc_param& u = t[i];
+        rows = u.rows;
+        cols = u.cols;
+        if (rows == 0 || cols == 0) return (int)BC_OK;
+        if (!u.weight || !u.grad || !u.momentum) return (int)BC_E_NULL;
+        if (u.ld_weight < cols || u.ld_grad < cols || u.ld_momentum < cols) return (int)BC_E_SIZE;
+        if (misaligned(u.weight, wdtype) || misaligned(u.grad, gdtype) || misaligned(u.momentum, BC_F32))
+            return (int)BC_E_ALIGN;
+        if (!std::isfinite(u.scale)) return (int)BC_E_VALUE;
+        o.in = u.grad;
+        o.out = u.weight;
+        o.momentum = u.momentum;
+        o.ld_in = u.ld_grad;
+        o.ld_out = u.ld_weight;
+        o.ld_momentum = u.ld_momentum;
+        o.step_scale = (float)u.scale;
+        return (int)BC_OK;
+    });
 }
 
 }  // extern "C"

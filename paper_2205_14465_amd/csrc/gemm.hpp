@@ -191,6 +191,44 @@ struct GemmTile {
         }
     }
 
+    // The same, and the block a second time by columns: epi.row(row, column, v)
+    // may change v, epi.column(row, column, v) then gets eight consecutive rows
+    // of a column as row() left them.
+    template <typename E>
+    __device__ __forceinline__ void finish_both_ways(char* lds, const E& epi) {
+        const int lane = threadIdx.x & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave / kWN, wn = wave % kWN;
+        float* strip = (float*)lds + wave * 32 * kEpiLd;
+        constexpr int kLanes = kEpiCols / 8, kPass = 64 / kLanes;
+#pragma unroll
+        for (int m = 0; m < kFM; ++m) {
+            to_strip(strip, m, lane);
+#pragma unroll
+            for (int r = 0; r < 32; r += kPass) {
+                const int row = r + lane / kLanes, col = lane % kLanes * 8;
+                float v[8];
+                float* s = strip + row * kEpiLd + col;
+                const float4 x = *(const float4*)s, y = *(const float4*)(s + 4);
+                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+                v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+                epi.row((wm * kFM + m) * 32 + row, wn * kEpiCols + col, v);
+                *(float4*)s = make_float4(v[0], v[1], v[2], v[3]);
+                *(float4*)(s + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int c = 0; c < kEpiCols; c += 16) {
+                const int col = c + lane / 4, row = lane % 4 * 8;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = strip[(row + i) * kEpiLd + col];
+                epi.column((wm * kFM + m) * 32 + row, wn * kEpiCols + col, v);
+            }
+            asm volatile("" ::: "memory");
+        }
+    }
+
     // Block row m of the wave's part of C into its LDS strip of 32 rows.
     __device__ __forceinline__ void to_strip(float* strip, int m, int lane) {
 #pragma unroll

@@ -85,3 +85,35 @@ def test_linear_refusals():
     with pytest.raises(B.BytecompError) as e:
         B.bytecomp_linear_workspace_size(7, 1, 1, 1)
     assert e.value.code == -3
+
+
+def test_orthogonalize_refusals():
+    L = B.lib()
+    abc = (ctypes.c_double * 3)(*B.MUON_COEFFICIENTS)
+
+    def orth(dtype=0, T=1, steps=5, k=abc, eps=1e-7, ws=WS, n=1 << 30, update=0x10000, out=0x20000, ldu=8, ldo=8, rows=4,
+             cols=8, null=False):
+        t = (B.bc_update * 1)(B.bc_update(update, out, ldu, ldo, rows, cols))
+        return L.bytecomp_orthogonalize(dtype, None if null else t, T, steps, k, eps, ws, n, None)
+
+    assert orth(dtype=5) == -3 and orth(T=-1) == -6 and orth(T=(1 << 20) + 1) == -6
+    assert orth(k=None) == -1 and orth(null=True) == -1 and orth(update=None) == -1 and orth(out=None) == -1
+    assert orth(steps=0) == -11 and orth(steps=65) == -11 and orth(eps=-1.0) == -11 and orth(eps=float("nan")) == -11
+    for bad in ((float("nan"), 0, 0), (1e300, 0, 0), (100.0, 0, 0), (3.0, 3.0, 3.0), (1.0, float("inf"), 0)):
+        assert orth(k=(ctypes.c_double * 3)(*bad)) == -11
+    assert orth(rows=1 << 22, cols=8) == -5 and orth(ldu=7) == -5 and orth(ldo=7) == -5
+    assert orth(update=0x10002) == -9 and orth(ws=P(0x40010)) == -9
+    assert orth(T=0) == 0 and orth(rows=0) == 0
+    need = B.bytecomp_orthogonalize_workspace_size([(4, 8)])
+    assert need > 0 and orth(n=need - 1) == -7 and orth(ws=None) == -7
+    assert B.bytecomp_orthogonalize_workspace_size([]) == 0
+    assert B.bytecomp_orthogonalize_workspace_size([(1600, 6400)]) <= 12 * 1600 * 6400 + 8 * 1600 * 1600 + (1 << 16)
+
+    def muon(wd=0, gd=0, lr=0.1, mu=0.9, decay=0.0, momentum=0x30000, scale=1.0, ldm=8, n=1 << 30):
+        t = (B.bc_param * 1)(B.bc_param(0x10000, 0x20000, momentum, 8, 8, ldm, 4, 8, scale))
+        return L.bytecomp_muon_step(wd, gd, t, 1, lr, mu, 1, decay, 5, abc, 1e-7, WS, n, None)
+
+    assert muon(wd=3) == -3 and muon(gd=-1) == -3
+    for v in (float("nan"), float("inf")):
+        assert muon(lr=v) == -11 and muon(mu=v) == -11 and muon(decay=v) == -11 and muon(scale=v) == -11
+    assert muon(momentum=None) == -1 and muon(ldm=7) == -5 and muon(momentum=0x30002) == -9 and muon(n=0) == -7
