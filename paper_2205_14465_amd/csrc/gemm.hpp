@@ -10,7 +10,7 @@
 //   P = 3: the same + a1 b1 + a0 b2 + a2 b0 (bfloat16: 24 bits)
 //
 // Per step of kBK along K the tile's rows of A and B go from memory to LDS
-// without passing registers (global_load_lds, 16 bytes a lane), kStages - 1
+// without passing registers (global_load_lds, 16 bytes a lane), up to kStages
 // steps ahead of their use.  A lane's 16 bytes land at 16 * lane, so the
 // swizzle that spreads a column of 16-byte chunks over the banks is applied to
 // the global address: chunk c of row r lies at place c ^ swizzle(r) of the row.
@@ -86,7 +86,7 @@ struct GemmTile {
 
     f32x16 acc[kFM][kFN];
 
-    static __device__ __forceinline__ int swizzle(int row) { return kBK == 64 ? row & 7 : (row >> 1) & 3; }
+    static __device__ __forceinline__ int swizzle(int row) { return kBK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
     // Products of `steps` steps of kBK into acc, which is cleared.
     __device__ __forceinline__ void multiply(const Operand<T>& a, const Operand<T>& b, int steps, char* lds) {
@@ -101,16 +101,17 @@ struct GemmTile {
             char* to = lds + stage * kStageBytes + wave * 1024;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const char* from = (const char*)(a.p + p * a.plane) + (uint64_t)step * kRow;
+                const __amdgpu_buffer_rsrc_t from = resource(a.p + p * a.plane);
 #pragma unroll
-                for (int i = 0; i < kLoadA; ++i) copy16(from, offa[i], to + (p * kBM * kRow + i * kWaves * 1024));
+                for (int i = 0; i < kLoadA; ++i)
+                    copy16(from, offa[i], step * kRow, to + (p * kBM * kRow + i * kWaves * 1024));
             }
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const char* from = (const char*)(b.p + p * b.plane) + (uint64_t)step * kRow;
+                const __amdgpu_buffer_rsrc_t from = resource(b.p + p * b.plane);
 #pragma unroll
                 for (int i = 0; i < kLoadB; ++i)
-                    copy16(from, offb[i], to + ((P * kBM + p * kBN) * kRow + i * kWaves * 1024));
+                    copy16(from, offb[i], step * kRow, to + ((P * kBM + p * kBN) * kRow + i * kWaves * 1024));
             }
         };
 #pragma unroll
@@ -120,47 +121,90 @@ struct GemmTile {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
         const int wm = wave / kWN, wn = wave % kWN;
-        const int hi = lane >> 5, l31 = lane & 31;
+        const int hi = lane >> 5, l31 = lane & 31, sw = swizzle(l31);
         const char* fa = lds + (wm * kFM * 32 + l31) * kRow;
         const char* fb = lds + (P * kBM + wn * kFN * 32 + l31) * kRow;
-        const int sw = swizzle(l31);
+        // fragments of 16 along k, read while the matrix cores work on the last ones
+        typename Frag<T>::type va[2][P][kFM], vb[2][P][kFN];
+        auto read = [&](int set, int stage, int kk) {
+            const int at = stage * kStageBytes + ((kk * 2 + hi) ^ sw) * 16;
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i)
-            if (i < steps) load(i, i);
-        int stage = 0, next = kStages - 1;
-        for (int step = 0; step < steps; ++step) {
-            // this step's data has landed: only later steps' loads may still be in flight
-            if (kStages > 2 && step + 1 < steps) wait_vmcnt<(kStages - 2) * kLoads>();
-            else wait_vmcnt<0>();
-            lds_barrier();
-            if (step + kStages - 1 < steps) load(next, step + kStages - 1);
-            const int at = stage * kStageBytes;
+            for (int p = 0; p < P; ++p) {
 #pragma unroll
-            for (int kk = 0; kk < kBK / 16; ++kk) {
-                typename Frag<T>::type va[P][kFM], vb[P][kFN];
-                const int c = ((kk * 2 + hi) ^ sw) * 16;
+                for (int n = 0; n < kFN; ++n)
+                    vb[set][p][n] = *(const typename Frag<T>::type*)(fb + at + (p * kBN + n * 32) * kRow);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
+                for (int m = 0; m < kFM; ++m)
+                    va[set][p][m] = *(const typename Frag<T>::type*)(fa + at + (p * kBM + m * 32) * kRow);
+            }
+        };
+        auto mma = [&](int set) {
 #pragma unroll
-                    for (int n = 0; n < kFN; ++n)
-                        vb[p][n] = *(const typename Frag<T>::type*)(fb + at + c + (p * kBN + n * 32) * kRow);
+            for (int pa = 0; pa < P; ++pa)
+#pragma unroll
+                for (int pb = 0; pb + pa < P; ++pb)
 #pragma unroll
                     for (int m = 0; m < kFM; ++m)
-                        va[p][m] = *(const typename Frag<T>::type*)(fa + at + c + (p * kBM + m * 32) * kRow);
-                }
 #pragma unroll
-                for (int pa = 0; pa < P; ++pa)
+                        for (int n = 0; n < kFN; ++n)
+                            acc[m][n] = Frag<T>::mma(vb[set][pb][n], va[set][pa][m], acc[m][n]);
+        };
+        constexpr int kKK = kBK / 16, kReads = P * (kFM + kFN), kMma = P * (P + 1) / 2 * kFM * kFN;
+        static_assert(kKK % 2 == 0, "fragment sets alternate");
+        if (steps > 0) {
 #pragma unroll
-                    for (int pb = 0; pb + pa < P; ++pb)
-#pragma unroll
-                        for (int m = 0; m < kFM; ++m)
-#pragma unroll
-                            for (int n = 0; n < kFN; ++n)
-                                acc[m][n] = Frag<T>::mma(vb[pb][n], va[pa][m], acc[m][n]);
-            }
-            stage = stage + 1 == kStages ? 0 : stage + 1;
-            next = next + 1 == kStages ? 0 : next + 1;
+            for (int i = 0; i < kStages; ++i)
+                if (i < steps) load(i, i);
+            // the first step's data has landed
+            if (steps >= kStages) wait_vmcnt<(kStages - 1) * kLoads>();
+            else wait_vmcnt<0>();
+            lds_barrier();
+            read(0, 0, 0);
         }
+        int stage = 0;
+        // One step: the matrix products of each 16 along k with the LDS reads of the
+        // next 16 between them, one after each product so that a read is never
+        // waited for at once.
+        auto work = [&](auto loading, int step) {
+            constexpr bool kLoad = decltype(loading)::value;
+            const int after = stage + 1 == kStages ? 0 : stage + 1;
+#pragma unroll
+            for (int kk = 0; kk + 1 < kKK; ++kk) {
+                read((kk + 1) & 1, stage, kk + 1);
+                mma(kk & 1);
+#pragma unroll
+                for (int i = 0; i < kMma; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                 // a matrix product
+                    if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // Every wave holds the last fragments of this step: its place in LDS is
+            // free for the step kStages on, and the next step's data has landed.
+            if (kLoad || step + 1 < steps) {
+                if (kLoad || step + kStages <= steps) wait_vmcnt<(kStages - 2) * kLoads>();
+                else wait_vmcnt<0>();
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // this wave's LDS reads are done
+                lds_barrier();
+                read(0, after, 0);
+                if (kLoad) load(stage, step + kStages);
+            }
+            mma((kKK - 1) & 1);
+            if (kLoad) {
+#pragma unroll
+                for (int i = 0; i < kMma; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    constexpr int kEach = (kLoads + kMma - 1) / kMma;
+                    if (i * kEach < kLoads) __builtin_amdgcn_sched_group_barrier(0x010, kEach, 0);  // loads to LDS
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            stage = after;
+        };
+        int step = 0;
+        for (; step + kStages < steps; ++step) work(Yes{}, step);
+        for (; step < steps; ++step) work(No{}, step);
         lds_barrier();  // every wave has read its last fragments: the epilogue may write LDS
     }
 
@@ -177,7 +221,9 @@ struct GemmTile {
 #pragma unroll
         for (int m = 0; m < kFM; ++m) {
             to_strip(strip, m, lane);
-#pragma unroll
+            // one copy of epi a block row: unrolled further, a large one keeps the
+            // compiler from unrolling over m, and acc goes to scratch memory
+#pragma unroll 1
             for (int r = 0; r < 32; r += kPass) {
                 const int row = r + lane / kLanes, col = lane % kLanes * 8;
                 float v[8];
@@ -204,7 +250,9 @@ struct GemmTile {
 #pragma unroll
         for (int m = 0; m < kFM; ++m) {
             to_strip(strip, m, lane);
-#pragma unroll
+            // one copy of epi a block row: unrolled further, a large one keeps the
+            // compiler from unrolling over m, and acc goes to scratch memory
+#pragma unroll 1
             for (int r = 0; r < 32; r += kPass) {
                 const int row = r + lane / kLanes, col = lane % kLanes * 8;
                 float v[8];
@@ -247,10 +295,17 @@ struct GemmTile {
         const uint32_t there = (uint32_t)row < rows ? (uint32_t)row : rows - 1;
         return there * ld * 2 + (uint32_t)((lane % kChunks) ^ swizzle(row)) * 16;
     }
-    static __device__ __forceinline__ void copy16(const char* base, uint32_t off, char* to) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + off),
-                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    // 16 bytes a lane from `from` + off (the lane's) + step (the wave's) to LDS
+    // at `to` + 16 * lane.
+    static __device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t from, uint32_t off, int step, char* to) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, (int)off, step,
+                                                 0, 0);
     }
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const T* p) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, -1, 0x00020000);
+    }
+    struct Yes { static constexpr bool value = true; };
+    struct No { static constexpr bool value = false; };
 };
 
 // Tile of workgroup b of a grid of tiles_m x tiles_n.  Workgroups are dealt to

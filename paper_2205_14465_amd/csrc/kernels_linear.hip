@@ -208,7 +208,7 @@ hipError_t launch_tiles(const Product& p, hipStream_t s) {
 template <typename T, typename TO, bool forward>
 hipError_t pick_tiles(const Product& p, hipStream_t s) {
     if constexpr (PlaneOf<T>::P == 3) {
-        return launch_tiles<GemmTile<bf16_t, 3, 128, 128, 32, 2, 2, 2>, TO, forward>(p, s);
+        return launch_tiles<GemmTile<bf16_t, 3, 256, 128, 32, 4, 2, 2>, TO, forward>(p, s);
     } else {
         const uint64_t big = (uint64_t)((p.rows + 255) / 256) * ((p.cols + 255) / 256);
         if (big >= 160) return launch_tiles<GemmTile<T, 1, 256, 256, 64, 2, 4, 2>, TO, forward>(p, s);
