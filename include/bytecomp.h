@@ -555,7 +555,7 @@ typedef struct bc_param {
 
 /* Bytes of workspace that the two calls below need for matrices of these
  * shapes (host arrays of T row and column counts; host only): 12 bytes an
- * element and 8 for each of min(rows, cols)^2, rounded up to whole 64s. */
+ * element and 12 for each of min(rows, cols)^2, rounded up to whole 64s. */
 int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* cols, int T, size_t* bytes);
 
 /* Orthogonalise T updates.

@@ -3,6 +3,7 @@
 // the launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -89,11 +90,11 @@ hipError_t operand(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_
 // -------------------------------------------------- orthogonalised updates
 constexpr int kMaxMatrices = 1 << 20;
 
-// The scales that keep X, A and B (kernels_ortho.hip) in fp16's range: the
-// largest singular value that the steps reach from [0, 1], and the largest
-// |b y + c y^2| for y up to its square, each rounded up to a power of two.
-// False: not finite, or past 64.
-bool ortho_scales(int steps, const double* k, float& top, float& gram_scale, float& poly_scale) {
+// The scales that keep X and the symmetric matrices (kernels_ortho.hip) in
+// fp16's range: bounds on their largest singular values, rounded up to powers of
+// two.  `reach` bounds X's within the steps, from [0, 1] at the start.  False:
+// the coefficients are not finite, or reach passes 64.
+bool ortho_scales(int steps, const double* k, float& top, float* scale) {
     const double a = k[0], b = k[1], c = k[2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
     double reach = 1.0, most = 1.0;
@@ -117,20 +118,25 @@ bool ortho_scales(int steps, const double* k, float& top, float& gram_scale, flo
         most = std::fmax(most, reach);
         if (!(most <= 64.0)) return false;
     }
+    // |b y + c y^2| for y up to the Gram matrix's largest eigenvalue
     auto p = [&](double y) { return std::fabs(y * (b + c * y)); };
     double poly = p(most * most);
     if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < most * most) poly = std::fmax(poly, p(-b / (2.0 * c)));
-    auto above = [](double x) { return std::exp2(std::ceil(std::log2(x * 1.001))); };
-    const double hx = above(most), hp = poly > 0x1p-40 ? above(poly) : 0x1p-40;
-    if (!(hp <= 0x1p40)) return false;
-    top = (float)(0x1p15 / hx);
-    gram_scale = (float)(0x1p15 / (hx * hx));
-    poly_scale = (float)(0x1p15 / hp);
+    const double whole = std::fabs(a) + poly;  // of a I + the polynomial
+    auto below = [](double x) {
+        return (float)(0x1p15 / std::exp2(std::ceil(std::log2(std::fmax(x, 0x1p-40) * 1.001))));
+    };
+    const double bounds[4] = {most * most, poly, most * most * whole, whole * whole + a * a};
+    for (int i = 0; i < 4; ++i) {
+        if (!(bounds[i] <= 0x1p40)) return false;
+        scale[i] = below(bounds[i]);
+    }
+    top = below(most);
     return true;
 }
 
 // Workspace offsets and workgroup counts of one matrix; `at` advances.
-void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoCall& c, Ortho& o) {
+void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho& o) {
     auto take = [&](uint64_t bytes) {
         const uint64_t p = at;
         at += align256(bytes);
@@ -141,87 +147,106 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoCall& c, Ortho
     o.turned = rows > cols;
     o.m = o.turned ? o.cols : o.rows;
     o.n = o.turned ? o.rows : o.cols;
-    o.part0 = c.parts;
-    o.tile0 = c.tiles;
-    for (int i = 0; i < 2; ++i) {
-        o.sym0[i] = c.sym[i];
-        o.full0[i] = c.full[i];
+    o.part0 = p.c.parts;
+    o.tile0 = p.c.tiles;
+    for (int i = 0; i < kOrthoSides; ++i) {
+        o.sym0[i] = p.sym[i].workgroups;
+        o.full0[i] = p.full[i].workgroups;
     }
     if (rows == 0 || cols == 0) return;
     const uint64_t m = o.m, n = o.n, mp = plane_cols(m), np = plane_cols(n);
     o.x = take(4 * m * np);
     o.xt = take(8 * n * mp);
-    o.gram = take(4 * m * mp);
-    o.poly = take(4 * m * mp);
+    o.sym = take(12 * m * mp);
     const uint64_t tiles = plane_cols(rows) / 64 * (plane_cols(cols) / 64);
     o.parts = (uint32_t)(tiles < kOrthoParts ? tiles : kOrthoParts);
     o.part = take(8 * o.parts);
-    c.parts += o.parts;
-    c.tiles += (uint32_t)tiles;
-    for (int i = 0; i < 2; ++i) {
-        const uint64_t side = i ? 256 : 128, a = (m + side - 1) / side, b = (n + side - 1) / side;
-        c.sym[i] += (uint32_t)(a * (a + 1) / 2);
-        c.full[i] += (uint32_t)(a * b);
+    p.c.parts += o.parts;
+    p.c.tiles += (uint32_t)tiles;
+    auto add = [](OrthoLoad& l, uint64_t tiles, uint64_t k) {
+        l.workgroups += matrix_workgroups((uint32_t)tiles);
+        l.steps += (double)tiles * (double)(k / 32);
+        l.longest = std::fmax(l.longest, (double)(k / 32));
+    };
+    for (int i = 0; i < kOrthoSides; ++i) {
+        const uint64_t side = 64u << i, a = (m + side - 1) / side, b = (n + side - 1) / side;
+        add(p.gram[i], a * (a + 1) / 2, np);
+        add(p.sym[i], a * (a + 1) / 2, mp);
+        add(p.full[i], a * b, mp);
     }
 }
 
-int check_ortho(int T, int steps, const double* k, double eps, float& top, OrthoCall& c) {
+int check_ortho(int T, int steps, const double* k, double eps, float& top, OrthoPlan& p) {
+    OrthoCall& c = p.c;
     if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
     if (!k) return BC_E_NULL;
     if (steps < 1 || steps > 64 || !(eps >= 0.0) || std::isinf(eps)) return BC_E_VALUE;
-    if (!ortho_scales(steps, k, top, c.gram_scale, c.poly_scale)) return BC_E_VALUE;
+    if (!ortho_scales(steps, k, top, c.scale)) return BC_E_VALUE;
     c.a = (float)k[0];
     c.b = (float)k[1];
     c.c = (float)k[2];
     c.eps = (float)eps;
-    c.steps = steps;
+    p.steps = steps;
     c.T = T;
     return BC_OK;
 }
 
 // get(i, rows, cols, o): matrix i's shape, pointers and strides, or its
-// error.  The rest of the call: plan, table, launch.
+// error.  The rest of the call: plan, table, launch.  Long products come first
+// in the table, so that a launch ends on short ones.
 template <typename Get>
-int run_ortho(OrthoCall& c, float top, void* ws, size_t ws_bytes, hipStream_t s, Get get) {
+int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s, Get get) {
     std::vector<Ortho> table;
     uint64_t at = 0, tiles = 0;
     try {
-        table.resize((size_t)c.T);
-        std::memset((void*)table.data(), 0, table.size() * sizeof(Ortho));
-        for (int i = 0; i < c.T; ++i) {
+        std::vector<Ortho> given((size_t)p.c.T);
+        std::memset((void*)given.data(), 0, given.size() * sizeof(Ortho));
+        std::vector<std::pair<uint64_t, int>> order;
+        for (int i = 0; i < p.c.T; ++i) {
             uint64_t rows = 0, cols = 0;
-            Ortho& o = table[(size_t)i];
+            Ortho& o = given[(size_t)i];
             if (const int rc = get(i, rows, cols, o)) return rc;
             if (rows >= kMaxDim || cols >= kMaxDim) return BC_E_SIZE;
             tiles += plane_cols(rows) / 64 * (plane_cols(cols) / 64);
-            if (tiles >= (1ull << 31)) return BC_E_SIZE;  // workgroup counts stay within 32 bits
-            plan_matrix(rows, cols, at, c, o);
-            const double side = std::sqrt((double)rows * (double)cols);
-            o.x_scale = side > 1.0 ? std::fmin(top, (float)std::exp2(std::floor(std::log2(side)))) : std::fmin(top, 1.0f);
+            if (tiles >= (1ull << 28)) return BC_E_SIZE;  // workgroup counts stay within 32 bits
+            o.rows = (uint32_t)rows;
+            o.cols = (uint32_t)cols;
+            if (rows && cols) order.push_back({rows > cols ? rows : cols, i});
+        }
+        std::sort(order.begin(), order.end(), [](const auto& x, const auto& y) {
+            return x.first != y.first ? x.first > y.first : x.second < y.second;
+        });
+        for (const auto& [longer, i] : order) {
+            table.push_back(given[(size_t)i]);
+            Ortho& o = table.back();
+            plan_matrix(o.rows, o.cols, at, p, o);
+            const double side = std::sqrt((double)o.rows * (double)o.cols);
+            o.x_scale = std::fmin(top, (float)std::exp2(std::floor(std::log2(side))));
         }
     } catch (const std::bad_alloc&) {
         return BC_E_SIZE;
     }
-    if (c.tiles == 0) return BC_OK;
+    if (table.empty()) return BC_OK;
     if (!ws || ws_bytes < at) return BC_E_WORKSPACE;
     if ((uintptr_t)ws & 255) return BC_E_ALIGN;
-    c.ws = (char*)ws;
+    p.c.ws = (char*)ws;
+    p.c.T = (int)table.size();
     int dev = 0;
     DevInfo di;
     hipError_t e = hipGetDevice(&dev);
     if (e == hipSuccess) e = device_info(dev, &di);
     if (e != hipSuccess) return BC_E_HIP;
-    c.cus = di.cus;
+    p.cus = di.cus;
     struct Ctx {
-        OrthoCall* c;
+        OrthoPlan* p;
         hipStream_t s;
-    } ctx{&c, s};
+    } ctx{&p, s};
     try {
         e = with_table(table.data(), table.size() * sizeof(Ortho), s,
-                       [](void* p, const void* dev_table) {
-                           Ctx* x = (Ctx*)p;
-                           x->c->d = (const Ortho*)dev_table;
-                           return launch_orthogonalize(*x->c, x->s);
+                       [](void* ctx, const void* dev_table) {
+                           Ctx* x = (Ctx*)ctx;
+                           x->p->c.d = (const Ortho*)dev_table;
+                           return launch_orthogonalize(*x->p, x->s);
                        },
                        &ctx);
     } catch (const std::bad_alloc&) {
@@ -405,12 +430,12 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
 int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* cols, int T, size_t* bytes) {
     if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
     if (!bytes || (T > 0 && (!rows || !cols))) return BC_E_NULL;
-    OrthoCall c{};
+    OrthoPlan p{};
     uint64_t at = 0;
     for (int i = 0; i < T; ++i) {
         if (rows[i] >= kMaxDim || cols[i] >= kMaxDim) return BC_E_SIZE;
         Ortho o{};
-        plan_matrix(rows[i], cols[i], at, c, o);
+        plan_matrix(rows[i], cols[i], at, p, o);
     }
     *bytes = (size_t)at;
     return BC_OK;
@@ -420,13 +445,14 @@ int bytecomp_orthogonalize(int dtype, const bc_update* t, int T, int steps, cons
                            void* ws, size_t ws_bytes, void* stream) {
     const CallRange range("bytecomp_orthogonalize");
     if (!dtype_ok(dtype)) return BC_E_DTYPE;
-    OrthoCall c{};
+    OrthoPlan p{};
+    OrthoCall& c = p.c;
     float top = 0.0f;
-    if (const int rc = check_ortho(T, steps, coefficients, eps, top, c)) return rc;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, top, p)) return rc;
     if (T == 0) return BC_OK;
     if (!t) return BC_E_NULL;
     c.in_dtype = c.out_dtype = dtype;
-    return run_ortho(c, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+    return run_ortho(p, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
         const bc_update& u = t[i];
         rows = u.rows;
         cols = u.cols;
@@ -447,9 +473,10 @@ int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double 
                        size_t ws_bytes, void* stream) {
     const CallRange range("bytecomp_muon_step");
     if (!dtype_ok(wdtype) || !dtype_ok(gdtype)) return BC_E_DTYPE;
-    OrthoCall c{};
+    OrthoPlan p{};
+    OrthoCall& c = p.c;
     float top = 0.0f;
-    if (const int rc = check_ortho(T, steps, coefficients, eps, top, c)) return rc;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, top, p)) return rc;
     if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay)) return BC_E_VALUE;
     if (T == 0) return BC_OK;
     if (!t) return BC_E_NULL;
@@ -460,7 +487,7 @@ int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double 
     c.momentum = (float)momentum;
     c.keep = (float)(1.0 - lr * weight_decay);
     c.lr = (float)lr;
-    return run_ortho(c, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+    return run_ortho(p, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
         const bc_param& u = t[i];
         rows = u.rows;
         cols = u.cols;

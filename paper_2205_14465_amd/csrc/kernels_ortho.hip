@@ -1,14 +1,24 @@
 // kernels_ortho.hip -- updates orthogonalised by Newton-Schulz products, for
 // lists of matrices: X_0 = U / (|U| + eps) with the Frobenius norm, then
-//   A = X X^T,  B = b A + c A^2,  X <- a X + B X
-// `steps` times, X with its shorter side as rows; and the optimizer step around
-// it (momentum before, weights after).
+//   A = X X^T,  B = b A + c A^2,  X <- (a I + B) X
+// `steps` times, X with its shorter side m as rows and its longer side n as
+// columns; and the optimizer step around it (momentum before, weights after).
 //
-// The work is three dependent products a step.  All matrices of the call share
-// each launch (a tile finds its matrix by a search in the call's table), so a
-// model's list costs 3 launches a step, and small matrices fill the chip
-// together.  A and B are symmetric: only tiles on and above the diagonal are
-// computed, and written twice.
+// Two steps can share their long products, for everything else is a polynomial
+// of A, m x m and symmetric: with P = a I + B the second step's Gram matrix is
+// A' = P A P, and with B' from it
+//   X <- (a I + B') (a I + B) X = (a^2 I + a (B + B') + B' B) X.
+// That is 3/2 m^2 n + 5/2 m^3 multiply-adds for two steps (symmetric results
+// half) instead of 3 m^2 n + m^3, and one pass over X instead of two.  More than
+// two steps from one Gram matrix would lose digits: A's small eigenvalues are the
+// squares of X's and grow by a^2 a step, their rounding with them.  (Gradients
+// with dominant directions, error of fp32 products as 1: two steps 1.0 to 1.1,
+// five steps 13.)
+//
+// All matrices of the call share each launch (a tile finds its matrix by a
+// search in the call's table), so a model's list costs 3 launches a step or 7 for
+// two, and small matrices fill the chip together.  Of a symmetric result only
+// tiles on and above the diagonal are computed, and written twice.
 //
 // Precision: singular values under one grow by up to a per step, and with them
 // every rounding made before, so 16-bit factors are not enough (in one fp16 part
@@ -20,6 +30,8 @@
 #include "gemm.hpp"
 #include "launch.hpp"
 #include "layers.hpp"
+
+#include <algorithm>
 
 namespace bc {
 
@@ -146,40 +158,53 @@ __global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
 }
 
 // ----------------------------------------------------------------- products
-enum Stage { kGram, kPoly, kNext, kLast };
+enum Stage { kGram, kSym, kNext, kLast };
 
-// Writes a symmetric m x m result (kGram, kPoly): the tile, and across the
-// diagonal its mirror image.
-template <int stage>
+// What a launch computes: kSym: matrix `out` = alpha U V + beta U + gamma V of
+// the symmetric matrices u and v; kGram: matrix `out`, kNext and kLast:
+// X <- alpha X + U X / scale, read from copy `from` of X^T.  The factors
+// contain the scales of what they multiply.
+struct StageArgs {
+    int u, v, out, from, side;
+    float alpha, beta, gamma;
+};
+
+// Writes a symmetric m x m result: the tile, and across the diagonal its
+// mirror image.
 struct SymmetricEpilogue {
     f16_t* out;
-    const f16_t* gram;          // kPoly
+    const f16_t *u, *v;         // NULL where their factor is 0
     uint64_t ld, plane;
     uint32_t m, m0, n0;
-    float scale, gram_factor;
-    __device__ __forceinline__ void row(int row, int col, float (&v)[8]) const {
+    float alpha, beta, gamma;
+    __device__ __forceinline__ void row(int row, int col, float (&x)[8]) const {
         const uint32_t r = m0 + row, c = n0 + col;
         const bool there = r < m && c < ld;
-        float g[8];
-        if constexpr (stage == kPoly) {
-            if (there) load_two(gram + r * ld + c, plane, g);
-            else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) x[i] *= alpha;
+        if (there) {
+            float g[8];
+            if (u) {
+                load_two(u + r * ld + c, plane, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] += beta * g[i];
+            }
+            if (v) {
+                load_two(v + r * ld + c, plane, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] += gamma * g[i];
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] *= scale;
-            if constexpr (stage == kPoly) v[i] += gram_factor * g[i];
-            if (c + i >= m) v[i] = 0.0f;
-        }
-        if (there) store_two(out + r * ld + c, plane, v);
+        for (int i = 0; i < 8; ++i)
+            if (c + i >= m) x[i] = 0.0f;
+        if (there) store_two(out + r * ld + c, plane, x);
     }
-    __device__ __forceinline__ void column(int row, int col, float (&v)[8]) const {
+    __device__ __forceinline__ void column(int row, int col, float (&x)[8]) const {
         if (m0 == n0) return;
         // rows of this tile are whole: it lies above the diagonal
         const uint32_t r = m0 + row, c = n0 + col;
-        if (c < m) store_two(out + c * ld + r, plane, v);
+        if (c < m) store_two(out + c * ld + r, plane, x);
     }
 };
 
@@ -204,22 +229,29 @@ struct NextEpilogue {
     }
 };
 
+// Tile of a matrix that its workgroup b takes, of `tiles` (or past them).
+// Workgroups are dealt to the eight compute dies in turn, each die with an L2
+// of its own: each gets a run of consecutive tiles of every larger matrix.
+__device__ __forceinline__ uint32_t tile_of_matrix(uint32_t b, uint32_t tiles) {
+    return tiles >= 16 ? b % 8 * ((tiles + 7) / 8) + b / 8 : b;
+}
+
 template <typename G, int stage>
-__global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, int which, int from) {
+__global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageArgs s) {
     extern __shared__ char lds[];
-    constexpr bool symmetric = stage == kGram || stage == kPoly;
-    // workgroups are dealt to the eight compute dies in turn: a die gets a run
-    // of consecutive tiles
-    const uint32_t total = gridDim.x, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
-    const uint32_t b = die * q + (die < rest ? die : rest) + blockIdx.x / 8;
-    const Ortho& o = a.d[owner(a.d, a.T, b, [which](const Ortho& x) { return symmetric ? x.sym0[which] : x.full0[which]; })];
+    constexpr bool symmetric = stage == kGram || stage == kSym;
+    const Ortho& o =
+        a.d[owner(a.d, a.T, blockIdx.x, [&](const Ortho& x) { return symmetric ? x.sym0[s.side] : x.full0[s.side]; })];
     const uint64_t mp = plane_cols(o.m), np = plane_cols(o.n);
     const f16_t* x = (const f16_t*)(a.ws + o.x);
     f16_t* xt[2] = {(f16_t*)(a.ws + o.xt), (f16_t*)(a.ws + o.xt) + 2 * o.n * mp};
-    f16_t* gram = (f16_t*)(a.ws + o.gram);
-    f16_t* poly = (f16_t*)(a.ws + o.poly);
-    uint32_t t = b - (symmetric ? o.sym0[which] : o.full0[which]), tm, tn;
+    auto sym = [&](int i) { return (f16_t*)(a.ws + o.sym) + i * (2 * o.m * mp); };
+    const uint32_t b = blockIdx.x - (symmetric ? o.sym0[s.side] : o.full0[s.side]);
+    uint32_t tm, tn;
     if constexpr (symmetric) {
+        const uint32_t across = (o.m + G::kBM - 1) / G::kBM, tiles = across * (across + 1) / 2;
+        const uint32_t t = tile_of_matrix(b, tiles);
+        if (t >= tiles) return;
         tn = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
         while (tn * (tn + 1) / 2 > t) --tn;
         while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
@@ -228,6 +260,8 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, int wh
         const bool tall = stage == kLast && o.turned;
         const uint32_t tiles_m = ((tall ? o.n : o.m) + G::kBM - 1) / G::kBM;
         const uint32_t tiles_n = ((tall ? o.m : o.n) + G::kBN - 1) / G::kBN;
+        const uint32_t t = tile_of_matrix(b, tiles_m * tiles_n);
+        if (t >= tiles_m * tiles_n) return;
         const uint32_t band = t / (8 * tiles_n), first = band * 8;
         const uint32_t high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - first * tiles_n;
         tm = first + in % high;
@@ -240,26 +274,26 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, int wh
     };
     if constexpr (stage == kGram) {
         g.multiply(rows_of(x, np, o.m, m0), rows_of(x, np, o.m, n0), (int)(np / G::kBK), lds);
-        const SymmetricEpilogue<stage> e{gram, nullptr, mp, o.m * mp, o.m, m0, n0,
-                                         a.gram_scale / (o.x_scale * o.x_scale), 0.0f};
+        const SymmetricEpilogue e{sym(s.out), nullptr, nullptr, mp, o.m * mp, o.m, m0, n0,
+                                  s.alpha / (o.x_scale * o.x_scale), 0.0f, 0.0f};
         g.finish_both_ways(lds, e);
-    } else if constexpr (stage == kPoly) {
-        g.multiply(rows_of(gram, mp, o.m, m0), rows_of(gram, mp, o.m, n0), (int)(mp / G::kBK), lds);
-        const SymmetricEpilogue<stage> e{poly, gram, mp, o.m * mp, o.m, m0, n0,
-                                         a.c * a.poly_scale / (a.gram_scale * a.gram_scale),
-                                         a.b * a.poly_scale / a.gram_scale};
+    } else if constexpr (stage == kSym) {
+        g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(sym(s.v), mp, o.m, n0), (int)(mp / G::kBK), lds);
+        const SymmetricEpilogue e{sym(s.out), s.beta != 0.0f ? sym(s.u) : nullptr,
+                                  s.gamma != 0.0f ? sym(s.v) : nullptr, mp, o.m * mp, o.m, m0, n0,
+                                  s.alpha, s.beta, s.gamma};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kNext) {
-        g.multiply(rows_of(poly, mp, o.m, m0), rows_of(xt[from], mp, o.n, n0), (int)(mp / G::kBK), lds);
-        const NextEpilogue e{(f16_t*)x, xt[1 - from], np, mp, o.m, o.n, m0, n0, a.a, 1.0f / a.poly_scale};
+        g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(xt[s.from], mp, o.n, n0), (int)(mp / G::kBK), lds);
+        const NextEpilogue e{(f16_t*)x, xt[1 - s.from], np, mp, o.m, o.n, m0, n0, s.alpha, s.beta};
         g.finish_both_ways(lds, e);
     } else {
-        // the caller's orientation: X, or X^T <- a X^T + X^T B
-        const f16_t* old = o.turned ? xt[from] : x;
+        // the caller's orientation: X, or its transpose, whose product is X^T U
+        const f16_t* old = o.turned ? xt[s.from] : x;
         const uint64_t old_ld = o.turned ? mp : np, old_plane = o.turned ? o.n * mp : o.m * np;
-        if (o.turned) g.multiply(rows_of(xt[from], mp, o.n, m0), rows_of(poly, mp, o.m, n0), (int)(mp / G::kBK), lds);
-        else g.multiply(rows_of(poly, mp, o.m, m0), rows_of(xt[from], mp, o.n, n0), (int)(mp / G::kBK), lds);
-        const float inv = 1.0f / o.x_scale, scale = 1.0f / a.poly_scale;
+        if (o.turned) g.multiply(rows_of(old, mp, o.n, m0), rows_of(sym(s.u), mp, o.m, n0), (int)(mp / G::kBK), lds);
+        else g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(xt[s.from], mp, o.n, n0), (int)(mp / G::kBK), lds);
+        const float inv = 1.0f / o.x_scale;
         g.finish(lds, [&](int row, int col, float (&v)[8]) {
             const uint64_t r = m0 + row;
             const uint32_t c = n0 + col;
@@ -268,7 +302,7 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, int wh
             float t[8];
             load_two(old + r * old_ld + c, old_plane, t);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (a.a * t[i] + v[i] * scale) * inv;
+            for (int i = 0; i < 8; ++i) v[i] = (s.alpha * t[i] + v[i] * s.beta) * inv;
             if (a.muon) {
                 load_any(a.out_dtype, o.out, r * o.ld_out + c, left, t);
 #pragma unroll
@@ -279,40 +313,79 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, int wh
     }
 }
 
-typedef GemmTile<f16_t, 2, 128, 128, 32, 2, 2, 2> Small;
-typedef GemmTile<f16_t, 2, 256, 256, 32, 2, 4, 2> Large;
+// Tile shapes and the model that picks among them: a tile's time for 32 along k
+// with its compute unit to itself, and a compute unit's time for one when the
+// chip is full (us, from products of 128 x 768 x 6400 to 4096 x 1600 x 1600).
+typedef GemmTile<f16_t, 2, 64, 64, 64, 2, 2, 2> Tile64;
+typedef GemmTile<f16_t, 2, 128, 128, 32, 2, 4, 3> Tile128;
+typedef GemmTile<f16_t, 2, 256, 256, 32, 2, 4, 2> Tile256;
+constexpr double kAlone[kOrthoSides] = {0.32, 0.58, 1.55}, kFull[kOrthoSides] = {0.22, 0.65, 1.7};
+constexpr double kLaunch = 3.0;  // a launch's time besides
+
+double time_of(const OrthoLoad& l, int side, int cus) {
+    return kLaunch + std::max(l.longest * kAlone[side], l.steps * kFull[side] / cus);
+}
+int best_side(const OrthoLoad* l, int cus) {
+    int best = 0;
+    for (int i = 1; i < kOrthoSides; ++i)
+        if (time_of(l[i], i, cus) < time_of(l[best], best, cus)) best = i;
+    return best;
+}
 
 template <typename G, int stage>
-hipError_t launch_stage(const OrthoCall& c, int which, int from, hipStream_t s) {
+hipError_t launch_tiles(const OrthoCall& c, const StageArgs& a, uint32_t workgroups, hipStream_t s) {
+    // more LDS than a kernel may use by default; the attribute is per device
+    // and setting it again costs next to nothing
     const hipError_t e = hipFuncSetAttribute((const void*)ortho_product<G, stage>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (e != hipSuccess) return e;
-    const uint32_t grid = stage == kGram || stage == kPoly ? c.sym[which] : c.full[which];
-    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(grid), dim3(G::kThreads), G::kLdsBytes, s, c, which, from);
+    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(workgroups), dim3(G::kThreads), G::kLdsBytes, s, c, a);
     return hipGetLastError();
 }
 
 template <int stage>
-hipError_t launch_tiles(const OrthoCall& c, int from, hipStream_t s) {
-    // large tiles move less data per product, small ones waste less at the
-    // edges and in the last round: the smaller number of rounds times a round's time
-    const uint32_t* count = stage == kGram || stage == kPoly ? c.sym : c.full;
-    const uint32_t slots = (uint32_t)c.cus;
-    const double small = (count[0] + 2 * slots - 1) / (2 * slots) * 2 * 1.2, large = (count[1] + slots - 1) / slots * 4;
-    if (large <= small) return launch_stage<Large, stage>(c, 1, from, s);
-    return launch_stage<Small, stage>(c, 0, from, s);
+hipError_t launch_stage(const OrthoPlan& p, StageArgs a, hipStream_t s) {
+    const OrthoLoad* l = stage == kGram ? p.gram : stage == kSym ? p.sym : p.full;
+    a.side = best_side(l, p.cus);
+    // the Gram products use the symmetric ones' workgroups
+    const uint32_t n = (stage == kGram || stage == kSym ? p.sym : p.full)[a.side].workgroups;
+    if (a.side == 0) return launch_tiles<Tile64, stage>(p.c, a, n, s);
+    if (a.side == 1) return launch_tiles<Tile128, stage>(p.c, a, n, s);
+    return launch_tiles<Tile256, stage>(p.c, a, n, s);
 }
 
 }  // namespace
 
-hipError_t launch_orthogonalize(const OrthoCall& c, hipStream_t s) {
+hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
+    const OrthoCall& c = p.c;
     hipLaunchKernelGGL(ortho_norm, dim3(c.parts), dim3(256), 0, s, c);
     hipLaunchKernelGGL(ortho_start, dim3(c.tiles), dim3(256), 0, s, c);
     hipError_t e = hipGetLastError();
-    for (int i = 0; i < c.steps && e == hipSuccess; ++i) {
-        e = launch_tiles<kGram>(c, 0, s);
-        if (e == hipSuccess) e = launch_tiles<kPoly>(c, 0, s);
-        if (e == hipSuccess) e = i + 1 < c.steps ? launch_tiles<kNext>(c, i & 1, s) : launch_tiles<kLast>(c, i & 1, s);
+    auto best = [&](const OrthoLoad* l) { const int i = best_side(l, p.cus); return time_of(l[i], i, p.cus); };
+    const bool pairs = best(p.gram) + 5 * best(p.sym) + best(p.full) < 2 * (best(p.gram) + best(p.sym) + best(p.full));
+    // out = alpha U V + beta U + gamma V, each matrix with the scale of its kind
+    auto sym = [&](int u, SymScale ku, int v, SymScale kv, int out, SymScale ko, float alpha, float beta, float gamma) {
+        const float *k = c.scale, to = k[ko];
+        if (e == hipSuccess)
+            e = launch_stage<kSym>(p, StageArgs{u, v, out, 0, 0, alpha * to / (k[ku] * k[kv]), beta * to / k[ku],
+                                                gamma * to / k[kv]}, s);
+    };
+    int from = 0;
+    for (int left = p.steps; left > 0 && e == hipSuccess;) {
+        const bool two = pairs && left >= 2;
+        e = launch_stage<kGram>(p, StageArgs{0, 0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
+        sym(0, kScaleGram, 0, kScaleGram, 1, kScalePoly, c.c, c.b, 0.0f);             // 1: B
+        StageArgs next{1, 0, 0, from, 0, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
+        if (two) {
+            sym(1, kScalePoly, 0, kScaleGram, 2, kScaleTurn, 1.0f, 0.0f, c.a);        // 2: P A
+            sym(2, kScaleTurn, 1, kScalePoly, 0, kScaleGram, 1.0f, c.a, 0.0f);        // 0: A' = P A P
+            sym(0, kScaleGram, 0, kScaleGram, 2, kScalePoly, c.c, c.b, 0.0f);         // 2: B'
+            sym(2, kScalePoly, 1, kScalePoly, 0, kScalePair, 1.0f, c.a, c.a);         // 0: B' B + a (B + B')
+            next = StageArgs{0, 0, 0, from, 0, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
+        }
+        left -= two ? 2 : 1;
+        if (e == hipSuccess) e = left > 0 ? launch_stage<kNext>(p, next, s) : launch_stage<kLast>(p, next, s);
+        from = 1 - from;
     }
     return e;
 }

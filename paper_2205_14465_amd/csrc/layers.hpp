@@ -90,38 +90,55 @@ hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s);
 // One matrix of a call (device table).  X is the matrix with its shorter side
 // m as rows (turned: the caller's has it as columns), n the longer side.  The
 // workspace holds, as two fp16 planes each, X [m][plane_cols(n)], X^T twice
-// [n][plane_cols(m)] (a product reads one and writes the other), the Gram
-// matrix and the polynomial of it [m][plane_cols(m)].
+// [n][plane_cols(m)] (a product reads one and writes the other), and three
+// symmetric matrices [m][plane_cols(m)].
+constexpr int kOrthoSides = 3;          // tiles 64, 128 and 256 wide
 struct Ortho {
     const void* in;          // update, or gradient
     void* out;               // result, or weight
     float* momentum;         // NULL: the update is `in`
     uint64_t ld_in, ld_out, ld_momentum;
-    uint64_t x, xt, gram, poly, part;    // byte offsets in the workspace
+    uint64_t x, xt, sym, part;           // byte offsets in the workspace
     uint32_t rows, cols, m, n;
     uint32_t turned, parts;  // parts: partial sums of squares
     uint32_t part0;          // workgroups before this matrix's: of the norm,
     uint32_t tile0;          // of the 64 x 64 tiles of the start,
-    uint32_t sym0[2];        // of the products with a symmetric result, 128 and 256 wide tiles,
-    uint32_t full0[2];       // of the others
+    uint32_t sym0[kOrthoSides];   // of the products with a symmetric result,
+    uint32_t full0[kOrthoSides];  // of the others
     float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
 };
-static_assert(sizeof(Ortho) == 8 * 11 + 4 * 14, "Ortho layout");
+static_assert(sizeof(Ortho) == 8 * 10 + 4 * 16, "Ortho layout");
 
+// Workgroups for `tiles` tiles of one matrix (see tile_of_matrix).
+__host__ __device__ inline uint32_t matrix_workgroups(uint32_t tiles) {
+    return tiles >= 16 ? (tiles + 7) / 8 * 8 : tiles;
+}
+
+// The work of a launch with one tile side: workgroups, and steps of 32 along
+// k, in all and of the longest tile.
+struct OrthoLoad {
+    uint32_t workgroups;
+    double steps, longest;
+};
 struct OrthoCall {
     const Ortho* d;
     char* ws;
     int T;
     int in_dtype, out_dtype;
-    uint32_t parts, tiles, sym[2], full[2];  // workgroups of the launches
-    float a, b, c, eps, gram_scale, poly_scale;
-    int steps;
+    uint32_t parts, tiles;   // workgroups of the norm and of the start
+    float a, b, c, eps;
+    float scale[4];          // of the symmetric matrices by what they hold (SymScale)
     bool muon, nesterov;
     float momentum, keep, lr;   // keep: 1 - lr * weight decay
-    int cus;
+};
+enum SymScale { kScaleGram, kScalePoly, kScaleTurn, kScalePair };
+struct OrthoPlan {
+    OrthoCall c;
+    int steps, cus;
+    OrthoLoad gram[kOrthoSides], sym[kOrthoSides], full[kOrthoSides];
 };
 constexpr uint32_t kOrthoParts = 256;
-hipError_t launch_orthogonalize(const OrthoCall& c, hipStream_t s);
+hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s);
 
 }  // namespace bc

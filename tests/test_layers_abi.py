@@ -107,7 +107,7 @@ def test_orthogonalize_refusals():
     need = B.bytecomp_orthogonalize_workspace_size([(4, 8)])
     assert need > 0 and orth(n=need - 1) == -7 and orth(ws=None) == -7
     assert B.bytecomp_orthogonalize_workspace_size([]) == 0
-    assert B.bytecomp_orthogonalize_workspace_size([(1600, 6400)]) <= 12 * 1600 * 6400 + 8 * 1600 * 1600 + (1 << 16)
+    assert B.bytecomp_orthogonalize_workspace_size([(1600, 6400)]) <= 12 * 1600 * 6400 + 12 * 1600 * 1600 + (1 << 16)
 
     def muon(wd=0, gd=0, lr=0.1, mu=0.9, decay=0.0, momentum=0x30000, scale=1.0, ldm=8, n=1 << 30):
         t = (B.bc_param * 1)(B.bc_param(0x10000, 0x20000, momentum, 8, 8, ldm, 4, 8, scale))
