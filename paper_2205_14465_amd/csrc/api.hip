@@ -346,10 +346,11 @@ int finish_call(int rc, hipStream_t s, void* ws) {
     return BC_OK;
 }
 
-hipError_t with_table(const void* bytes, size_t len, hipStream_t s, TableLaunch launch, void* ctx) {
+hipError_t with_table(const void* bytes, size_t len, size_t extra, TableFill fill, hipStream_t s, TableLaunch launch,
+                      void* ctx) {
     std::lock_guard<std::mutex> lk(g_mu);
     Entry* en = nullptr;
-    hipError_t e = cache_get(bytes, len, 0, [](void*) {}, s, &en);
+    hipError_t e = cache_get(bytes, len, extra, [&](void* dst) { fill(ctx, dst); }, s, &en);
     if (e != hipSuccess) return e;
     e = launch(ctx, en->dev);
     cache_mark_used(en, s);

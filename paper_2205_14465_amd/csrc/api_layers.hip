@@ -135,6 +135,15 @@ bool ortho_scales(int steps, const double* k, float& top, float* scale) {
     return true;
 }
 
+// Tiles of a product, and steps of 32 along its k.
+uint64_t ortho_tiles(const Ortho& o, int kind, int side) {
+    const uint64_t w = 64u << side, a = (o.m + w - 1) / w, b = (o.n + w - 1) / w;
+    return kind == kOrthoFull ? a * b : a * (a + 1) / 2;
+}
+double ortho_steps(const Ortho& o, int kind) {
+    return (double)plane_cols(kind == kOrthoGram ? o.n : o.m) / 32.0;
+}
+
 // Workspace offsets and workgroup counts of one matrix; `at` advances.
 void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho& o) {
     auto take = [&](uint64_t bytes) {
@@ -149,10 +158,6 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.n = o.turned ? o.rows : o.cols;
     o.part0 = p.c.parts;
     o.tile0 = p.c.tiles;
-    for (int i = 0; i < kOrthoSides; ++i) {
-        o.sym0[i] = p.sym[i].workgroups;
-        o.full0[i] = p.full[i].workgroups;
-    }
     if (rows == 0 || cols == 0) return;
     const uint64_t m = o.m, n = o.n, mp = plane_cols(m), np = plane_cols(n);
     o.x = take(4 * m * np);
@@ -163,17 +168,54 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.part = take(8 * o.parts);
     p.c.parts += o.parts;
     p.c.tiles += (uint32_t)tiles;
-    auto add = [](OrthoLoad& l, uint64_t tiles, uint64_t k) {
-        l.workgroups += matrix_workgroups((uint32_t)tiles);
-        l.steps += (double)tiles * (double)(k / 32);
-        l.longest = std::fmax(l.longest, (double)(k / 32));
-    };
-    for (int i = 0; i < kOrthoSides; ++i) {
-        const uint64_t side = 64u << i, a = (m + side - 1) / side, b = (n + side - 1) / side;
-        add(p.gram[i], a * (a + 1) / 2, np);
-        add(p.sym[i], a * (a + 1) / 2, mp);
-        add(p.full[i], a * b, mp);
+    for (int i = 0; i < kOrthoSides; ++i)
+        for (int kind = 0; kind < kOrthoKinds; ++kind) {
+            OrthoLoad& l = p.load[kind][i];
+            const double steps = ortho_steps(o, kind);
+            l.tiles += (double)ortho_tiles(o, kind, i);
+            l.steps += (double)ortho_tiles(o, kind, i) * steps;
+            l.longest = std::fmax(l.longest, steps);
+        }
+}
+
+// The workgroups of a launch, dealt to the eight compute dies in turn, each
+// with an L2 of its own.  Where all tiles take about as long, the matrices' tiles
+// one after the other are cut into eight runs of equal work, so that a die works
+// on few matrices; otherwise each matrix of 16 tiles or more is cut into eight and
+// smaller ones go whole to the least loaded die, the long tiles first.  `list`
+// receives 8 x the longest die's count entries, the others' ends idle; returns
+// that count.
+uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kind, std::vector<OrthoWork>& list) {
+    constexpr int kDies = 8;
+    std::vector<OrthoWork> die[kDies];
+    const int side = p.side[kind];
+    const OrthoLoad& all = p.load[kind][side];
+    if (all.longest * all.tiles <= 1.25 * all.steps) {
+        double done = 0.0;
+        for (size_t i = 0; i < table.size(); ++i) {
+            const uint64_t tiles = ortho_tiles(table[i], kind, side);
+            for (uint64_t t = 0; t < tiles; ++t) {
+                die[std::min(kDies - 1, (int)(done * kDies / all.steps))].push_back(OrthoWork{(uint32_t)i, (uint32_t)t});
+                done += ortho_steps(table[i], kind);
+            }
+        }
+    } else {
+        double load[kDies] = {};
+        for (size_t i = 0; i < table.size(); ++i) {
+            const uint64_t tiles = ortho_tiles(table[i], kind, side), pieces = tiles >= 16 ? kDies : 1;
+            for (uint64_t q = 0; q < pieces; ++q) {
+                const int to = (int)(std::min_element(load, load + kDies) - load);
+                const uint64_t lo = tiles * q / pieces, hi = tiles * (q + 1) / pieces;
+                for (uint64_t t = lo; t < hi; ++t) die[to].push_back(OrthoWork{(uint32_t)i, (uint32_t)t});
+                load[to] += (double)(hi - lo) * ortho_steps(table[i], kind);
+            }
+        }
     }
+    size_t longest = 0;
+    for (const auto& d : die) longest = std::max(longest, d.size());
+    for (size_t q = 0; q < longest; ++q)
+        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0});
+    return (uint32_t)(kDies * longest);
 }
 
 int check_ortho(int T, int steps, const double* k, double eps, float& top, OrthoPlan& p) {
@@ -237,15 +279,30 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
     if (e == hipSuccess) e = device_info(dev, &di);
     if (e != hipSuccess) return BC_E_HIP;
     p.cus = di.cus;
+    ortho_choose(p);
+    // the table, then the work lists, which follow from it
     struct Ctx {
         OrthoPlan* p;
         hipStream_t s;
-    } ctx{&p, s};
+        std::vector<OrthoWork> list;
+        size_t at;
+    } ctx{&p, s, {}, table.size() * sizeof(Ortho)};
     try {
-        e = with_table(table.data(), table.size() * sizeof(Ortho), s,
-                       [](void* ctx, const void* dev_table) {
-                           Ctx* x = (Ctx*)ctx;
+        for (int kind = 0; kind < kOrthoKinds; ++kind) p.workgroups[kind] = ortho_list(p, table, kind, ctx.list);
+        e = with_table(table.data(), ctx.at, ctx.list.size() * sizeof(OrthoWork),
+                       [](void* c, void* extra) {
+                           const Ctx* x = (const Ctx*)c;
+                           std::memcpy(extra, x->list.data(), x->list.size() * sizeof(OrthoWork));
+                       },
+                       s,
+                       [](void* c, const void* dev_table) {
+                           Ctx* x = (Ctx*)c;
                            x->p->c.d = (const Ortho*)dev_table;
+                           const OrthoWork* l = (const OrthoWork*)((const char*)dev_table + x->at);
+                           for (int kind = 0; kind < kOrthoKinds; ++kind) {
+                               x->p->list[kind] = l;
+                               l += x->p->workgroups[kind];
+                           }
                            return launch_orthogonalize(*x->p, x->s);
                        },
                        &ctx);

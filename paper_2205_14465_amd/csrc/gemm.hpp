@@ -250,9 +250,7 @@ struct GemmTile {
 #pragma unroll
         for (int m = 0; m < kFM; ++m) {
             to_strip(strip, m, lane);
-            // one copy of epi a block row: unrolled further, a large one keeps the
-            // compiler from unrolling over m, and acc goes to scratch memory
-#pragma unroll 1
+#pragma unroll
             for (int r = 0; r < 32; r += kPass) {
                 const int row = r + lane / kLanes, col = lane % kLanes * 8;
                 float v[8];

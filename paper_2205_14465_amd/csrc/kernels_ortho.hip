@@ -15,9 +15,9 @@
 // with dominant directions, error of fp32 products as 1: two steps 1.0 to 1.1,
 // five steps 13.)
 //
-// All matrices of the call share each launch (a tile finds its matrix by a
-// search in the call's table), so a model's list costs 3 launches a step or 7 for
-// two, and small matrices fill the chip together.  Of a symmetric result only
+// All matrices of the call share each launch (a workgroup finds its matrix and
+// tile in a list made with the call's table), so a model's list costs 3 launches
+// a step or 7 for two, and small matrices fill the chip together.  Of a symmetric result only
 // tiles on and above the diagonal are computed, and written twice.
 //
 // Precision: singular values under one grow by up to a per step, and with them
@@ -165,7 +165,7 @@ enum Stage { kGram, kSym, kNext, kLast };
 // X <- alpha X + U X / scale, read from copy `from` of X^T.  The factors
 // contain the scales of what they multiply.
 struct StageArgs {
-    int u, v, out, from, side;
+    int u, v, out, from;
     float alpha, beta, gamma;
 };
 
@@ -229,29 +229,21 @@ struct NextEpilogue {
     }
 };
 
-// Tile of a matrix that its workgroup b takes, of `tiles` (or past them).
-// Workgroups are dealt to the eight compute dies in turn, each die with an L2
-// of its own: each gets a run of consecutive tiles of every larger matrix.
-__device__ __forceinline__ uint32_t tile_of_matrix(uint32_t b, uint32_t tiles) {
-    return tiles >= 16 ? b % 8 * ((tiles + 7) / 8) + b / 8 : b;
-}
-
 template <typename G, int stage>
-__global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageArgs s) {
+__global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageArgs s,
+                                                             const OrthoWork* __restrict__ list) {
     extern __shared__ char lds[];
     constexpr bool symmetric = stage == kGram || stage == kSym;
-    const Ortho& o =
-        a.d[owner(a.d, a.T, blockIdx.x, [&](const Ortho& x) { return symmetric ? x.sym0[s.side] : x.full0[s.side]; })];
+    const OrthoWork work = list[blockIdx.x];
+    if (work.matrix == kOrthoIdle) return;
+    const Ortho& o = a.d[work.matrix];
     const uint64_t mp = plane_cols(o.m), np = plane_cols(o.n);
     const f16_t* x = (const f16_t*)(a.ws + o.x);
     f16_t* xt[2] = {(f16_t*)(a.ws + o.xt), (f16_t*)(a.ws + o.xt) + 2 * o.n * mp};
     auto sym = [&](int i) { return (f16_t*)(a.ws + o.sym) + i * (2 * o.m * mp); };
-    const uint32_t b = blockIdx.x - (symmetric ? o.sym0[s.side] : o.full0[s.side]);
+    const uint32_t t = work.tile;
     uint32_t tm, tn;
     if constexpr (symmetric) {
-        const uint32_t across = (o.m + G::kBM - 1) / G::kBM, tiles = across * (across + 1) / 2;
-        const uint32_t t = tile_of_matrix(b, tiles);
-        if (t >= tiles) return;
         tn = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
         while (tn * (tn + 1) / 2 > t) --tn;
         while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
@@ -260,8 +252,6 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         const bool tall = stage == kLast && o.turned;
         const uint32_t tiles_m = ((tall ? o.n : o.m) + G::kBM - 1) / G::kBM;
         const uint32_t tiles_n = ((tall ? o.m : o.n) + G::kBN - 1) / G::kBN;
-        const uint32_t t = tile_of_matrix(b, tiles_m * tiles_n);
-        if (t >= tiles_m * tiles_n) return;
         const uint32_t band = t / (8 * tiles_n), first = band * 8;
         const uint32_t high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - first * tiles_n;
         tm = first + in % high;
@@ -313,75 +303,82 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
     }
 }
 
-// Tile shapes and the model that picks among them: a tile's time for 32 along k
-// with its compute unit to itself, and a compute unit's time for one when the
-// chip is full (us, from products of 128 x 768 x 6400 to 4096 x 1600 x 1600).
+// Tile shapes and the model that picks among them (us): a tile's time for 32
+// along k with its compute unit to itself, and a compute unit's share of it when
+// the chip is full; a tile's start and epilogue.  From products of 768 x 768 x 768
+// to 4096 x 4096 x 6400; a launch ends, on average, half a tile after its mean.
 typedef GemmTile<f16_t, 2, 64, 64, 64, 2, 2, 2> Tile64;
-typedef GemmTile<f16_t, 2, 128, 128, 32, 2, 4, 3> Tile128;
+typedef GemmTile<f16_t, 2, 128, 128, 64, 2, 4, 2> Tile128;
 typedef GemmTile<f16_t, 2, 256, 256, 32, 2, 4, 2> Tile256;
-constexpr double kAlone[kOrthoSides] = {0.32, 0.58, 1.55}, kFull[kOrthoSides] = {0.22, 0.65, 1.7};
-constexpr double kLaunch = 3.0;  // a launch's time besides
+constexpr double kAlone[kOrthoSides] = {0.32, 0.50, 1.55}, kFull[kOrthoSides] = {0.21, 0.63, 2.2};
+constexpr double kEnds[kOrthoSides] = {1.5, 6.0, 40.0};
+constexpr double kLaunch = 3.0;
 
 double time_of(const OrthoLoad& l, int side, int cus) {
-    return kLaunch + std::max(l.longest * kAlone[side], l.steps * kFull[side] / cus);
-}
-int best_side(const OrthoLoad* l, int cus) {
-    int best = 0;
-    for (int i = 1; i < kOrthoSides; ++i)
-        if (time_of(l[i], i, cus) < time_of(l[best], best, cus)) best = i;
-    return best;
+    const double alone = l.longest * kAlone[side] + kEnds[side];
+    const double full = (l.steps * kFull[side] + l.tiles * kEnds[side]) / cus;
+    return kLaunch + std::max(alone, full + 0.5 * (l.longest * kFull[side] + kEnds[side]));
 }
 
 template <typename G, int stage>
-hipError_t launch_tiles(const OrthoCall& c, const StageArgs& a, uint32_t workgroups, hipStream_t s) {
+hipError_t launch_tiles(const OrthoPlan& p, int kind, const StageArgs& a, hipStream_t s) {
     // more LDS than a kernel may use by default; the attribute is per device
     // and setting it again costs next to nothing
     const hipError_t e = hipFuncSetAttribute((const void*)ortho_product<G, stage>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(workgroups), dim3(G::kThreads), G::kLdsBytes, s, c, a);
+    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(p.workgroups[kind]), dim3(G::kThreads), G::kLdsBytes, s, p.c, a,
+                       p.list[kind]);
     return hipGetLastError();
 }
 
 template <int stage>
-hipError_t launch_stage(const OrthoPlan& p, StageArgs a, hipStream_t s) {
-    const OrthoLoad* l = stage == kGram ? p.gram : stage == kSym ? p.sym : p.full;
-    a.side = best_side(l, p.cus);
-    // the Gram products use the symmetric ones' workgroups
-    const uint32_t n = (stage == kGram || stage == kSym ? p.sym : p.full)[a.side].workgroups;
-    if (a.side == 0) return launch_tiles<Tile64, stage>(p.c, a, n, s);
-    if (a.side == 1) return launch_tiles<Tile128, stage>(p.c, a, n, s);
-    return launch_tiles<Tile256, stage>(p.c, a, n, s);
+hipError_t launch_stage(const OrthoPlan& p, const StageArgs& a, hipStream_t s) {
+    constexpr int kind = stage == kGram ? kOrthoGram : stage == kSym ? kOrthoSym : kOrthoFull;
+    if (p.side[kind] == 0) return launch_tiles<Tile64, stage>(p, kind, a, s);
+    if (p.side[kind] == 1) return launch_tiles<Tile128, stage>(p, kind, a, s);
+    return launch_tiles<Tile256, stage>(p, kind, a, s);
 }
 
 }  // namespace
+
+void ortho_choose(OrthoPlan& p) {
+    double time[kOrthoKinds];
+    for (int kind = 0; kind < kOrthoKinds; ++kind) {
+        p.side[kind] = 0;
+        for (int i = 1; i < kOrthoSides; ++i)
+            if (time_of(p.load[kind][i], i, p.cus) < time_of(p.load[kind][p.side[kind]], p.side[kind], p.cus))
+                p.side[kind] = i;
+        time[kind] = time_of(p.load[kind][p.side[kind]], p.side[kind], p.cus);
+    }
+    p.pairs = 4 * time[kOrthoSym] + time[kOrthoFull] + time[kOrthoGram] + time[kOrthoSym] <
+              2 * (time[kOrthoGram] + time[kOrthoSym] + time[kOrthoFull]);
+}
 
 hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
     const OrthoCall& c = p.c;
     hipLaunchKernelGGL(ortho_norm, dim3(c.parts), dim3(256), 0, s, c);
     hipLaunchKernelGGL(ortho_start, dim3(c.tiles), dim3(256), 0, s, c);
     hipError_t e = hipGetLastError();
-    auto best = [&](const OrthoLoad* l) { const int i = best_side(l, p.cus); return time_of(l[i], i, p.cus); };
-    const bool pairs = best(p.gram) + 5 * best(p.sym) + best(p.full) < 2 * (best(p.gram) + best(p.sym) + best(p.full));
     // out = alpha U V + beta U + gamma V, each matrix with the scale of its kind
     auto sym = [&](int u, SymScale ku, int v, SymScale kv, int out, SymScale ko, float alpha, float beta, float gamma) {
         const float *k = c.scale, to = k[ko];
         if (e == hipSuccess)
-            e = launch_stage<kSym>(p, StageArgs{u, v, out, 0, 0, alpha * to / (k[ku] * k[kv]), beta * to / k[ku],
+            e = launch_stage<kSym>(p, StageArgs{u, v, out, 0, alpha * to / (k[ku] * k[kv]), beta * to / k[ku],
                                                 gamma * to / k[kv]}, s);
     };
     int from = 0;
     for (int left = p.steps; left > 0 && e == hipSuccess;) {
-        const bool two = pairs && left >= 2;
-        e = launch_stage<kGram>(p, StageArgs{0, 0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
+        const bool two = p.pairs && left >= 2;
+        e = launch_stage<kGram>(p, StageArgs{0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
         sym(0, kScaleGram, 0, kScaleGram, 1, kScalePoly, c.c, c.b, 0.0f);             // 1: B
-        StageArgs next{1, 0, 0, from, 0, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
+        StageArgs next{1, 0, 0, from, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
         if (two) {
             sym(1, kScalePoly, 0, kScaleGram, 2, kScaleTurn, 1.0f, 0.0f, c.a);        // 2: P A
             sym(2, kScaleTurn, 1, kScalePoly, 0, kScaleGram, 1.0f, c.a, 0.0f);        // 0: A' = P A P
             sym(0, kScaleGram, 0, kScaleGram, 2, kScalePoly, c.c, c.b, 0.0f);         // 2: B'
             sym(2, kScalePoly, 1, kScalePoly, 0, kScalePair, 1.0f, c.a, c.a);         // 0: B' B + a (B + B')
-            next = StageArgs{0, 0, 0, from, 0, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
+            next = StageArgs{0, 0, 0, from, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
         }
         left -= two ? 2 : 1;
         if (e == hipSuccess) e = left > 0 ? launch_stage<kNext>(p, next, s) : launch_stage<kLast>(p, next, s);

@@ -105,10 +105,12 @@ hipError_t compress_launch(int kind, double ratio, uint64_t seed, const Compress
 // rc, after a synchronisation and a look at the workspace's failure flags
 // (ws NULL: none) where BYTECOMP_DEBUG=1 asks for them.
 int finish_call(int rc, hipStream_t s, void* ws);
-// Runs launch(device copy of bytes) with the descriptor cache's copy, marked
-// as in use by stream s.
+// Runs launch(device copy of bytes and the `extra` bytes that fill derives
+// from them) with the descriptor cache's copy, marked as in use by stream s.
 typedef hipError_t (*TableLaunch)(void* ctx, const void* table);
-hipError_t with_table(const void* bytes, size_t len, hipStream_t s, TableLaunch launch, void* ctx);
+typedef void (*TableFill)(void* ctx, void* extra);
+hipError_t with_table(const void* bytes, size_t len, size_t extra, TableFill fill, hipStream_t s, TableLaunch launch,
+                      void* ctx);
 
 struct DevInfo {
     int cus;

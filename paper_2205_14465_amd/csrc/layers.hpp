@@ -102,24 +102,23 @@ struct Ortho {
     uint32_t rows, cols, m, n;
     uint32_t turned, parts;  // parts: partial sums of squares
     uint32_t part0;          // workgroups before this matrix's: of the norm,
-    uint32_t tile0;          // of the 64 x 64 tiles of the start,
-    uint32_t sym0[kOrthoSides];   // of the products with a symmetric result,
-    uint32_t full0[kOrthoSides];  // of the others
+    uint32_t tile0;          // of the 64 x 64 tiles of the start
     float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
 };
-static_assert(sizeof(Ortho) == 8 * 10 + 4 * 16, "Ortho layout");
+static_assert(sizeof(Ortho) == 8 * 10 + 4 * 10, "Ortho layout");
 
-// Workgroups for `tiles` tiles of one matrix (see tile_of_matrix).
-__host__ __device__ inline uint32_t matrix_workgroups(uint32_t tiles) {
-    return tiles >= 16 ? (tiles + 7) / 8 * 8 : tiles;
-}
+// What a workgroup of a product launch computes: a tile of a matrix, or
+// nothing (matrix kOrthoIdle).
+struct OrthoWork {
+    uint32_t matrix, tile;
+};
+constexpr uint32_t kOrthoIdle = 0xFFFFFFFFu;
 
-// The work of a launch with one tile side: workgroups, and steps of 32 along
-// k, in all and of the longest tile.
+// The work of a launch with one tile side: tiles, and steps of 32 along k, in
+// all and of the longest tile.
 struct OrthoLoad {
-    uint32_t workgroups;
-    double steps, longest;
+    double tiles, steps, longest;
 };
 struct OrthoCall {
     const Ortho* d;
@@ -133,11 +132,20 @@ struct OrthoCall {
     float momentum, keep, lr;   // keep: 1 - lr * weight decay
 };
 enum SymScale { kScaleGram, kScalePoly, kScaleTurn, kScalePair };
+// Products of a call by what bounds their work lists: X X^T, the symmetric
+// m x m ones, and those with X's shape.
+enum OrthoKind { kOrthoGram, kOrthoSym, kOrthoFull, kOrthoKinds };
 struct OrthoPlan {
     OrthoCall c;
     int steps, cus;
-    OrthoLoad gram[kOrthoSides], sym[kOrthoSides], full[kOrthoSides];
+    OrthoLoad load[kOrthoKinds][kOrthoSides];
+    int side[kOrthoKinds];             // the tile side chosen (ortho_choose)
+    uint32_t workgroups[kOrthoKinds];  // and its launch's size
+    const OrthoWork* list[kOrthoKinds];
+    bool pairs;                        // two steps from one Gram matrix
 };
+// Picks tile sides and the schedule from the loads.
+void ortho_choose(OrthoPlan& p);
 constexpr uint32_t kOrthoParts = 256;
 hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s);
 
