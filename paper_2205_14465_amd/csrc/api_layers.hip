@@ -51,10 +51,19 @@ size_t planes_bytes(int dtype, uint64_t rows, uint64_t k) {
     return align256((size_t)(rows * plane_cols(k) * 2 * (uint64_t)planes_of(dtype)));
 }
 
+// Bytes for the sums of a product [rows, cols] whose k is split.
+size_t sums_bytes(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
+    return align256((size_t)split_bytes(product_cut(dtype, rows, cols, k), rows, cols));
+}
+
 size_t linear_ws(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, bool backward) {
-    if (!backward) return rows <= kFewRows ? 0 : planes_bytes(dtype, rows, inner) + planes_bytes(dtype, cols, inner);
+    if (!backward)
+        return rows <= kFewRows ? 0
+                                : planes_bytes(dtype, rows, inner) + planes_bytes(dtype, cols, inner) +
+                                      sums_bytes(dtype, rows, cols, inner);
     return planes_bytes(dtype, rows, cols) + planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows) +
-           planes_bytes(dtype, inner, cols) + align256((size_t)((rows + 63) / 64 * cols * sizeof(float)));
+           planes_bytes(dtype, inner, cols) + align256((size_t)((rows + 63) / 64 * cols * sizeof(float))) +
+           std::max(sums_bytes(dtype, rows, inner, cols), sums_bytes(dtype, cols, inner, rows));
 }
 
 // Hands out the workspace piece by piece.
@@ -74,17 +83,19 @@ bool readable(int dtype, const void* p, uint64_t ld, uint64_t k) {
 }
 
 // An operand of `rows` rows and k columns for the product kernels: where it
-// lies, or laid out at `c`.
-hipError_t operand(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t k, Carver& c, Planes& out,
-                   hipStream_t s) {
-    if (readable(dtype, p, ld, k)) {
-        out = Planes{p, ld, 0};
-        return hipSuccess;
-    }
+// lies, or laid out at `c` by the call's lay_out launch.
+Planes operand(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t k, Carver& c, LayOuts& l) {
+    if (readable(dtype, p, ld, k)) return Planes{p, ld, 0};
     void* to = c.take(planes_bytes(dtype, rows, k));
-    out = Planes{to, plane_cols(k), rows * plane_cols(k)};
-    const LayOut a{p, nullptr, ld, 0, (uint32_t)rows, (uint32_t)k, to, nullptr, nullptr, BC_ACT_NONE};
-    return launch_lay_out(dtype, a, s);
+    l.of[l.count++] = LayOut{p, nullptr, ld, 0, (uint32_t)rows, (uint32_t)k, to, nullptr, nullptr, BC_ACT_NONE};
+    return Planes{to, plane_cols(k), rows * plane_cols(k)};
+}
+
+// The transpose of a rows x cols matrix as an operand of cols rows.
+Planes turned(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t cols, Carver& c, LayOuts& l) {
+    void* to = c.take(planes_bytes(dtype, cols, rows));
+    l.of[l.count++] = LayOut{p, nullptr, ld, 0, (uint32_t)rows, (uint32_t)cols, nullptr, to, nullptr, BC_ACT_NONE};
+    return Planes{to, plane_cols(rows), cols * plane_cols(rows)};
 }
 
 // -------------------------------------------------- orthogonalised updates
@@ -329,7 +340,7 @@ int bytecomp_layernorm_forward(int dtype, int wdtype, uint64_t rows, uint64_t co
         misaligned(mean, BC_F32) || misaligned(rstd, BC_F32))
         return BC_E_ALIGN;
     const LnForward a{x, weight, bias, y, mean, rstd, rows, ldx, ldy, (uint32_t)cols, (float)(1.0 / (double)cols),
-                      (float)eps};
+                      (float)eps, streams(rows * cols * dtype_bytes(dtype))};
     hipStream_t s = (hipStream_t)stream;
     return finish_call(status_of(launch_ln_forward(dtype, wdtype, a, s)), s, nullptr);
 }
@@ -357,7 +368,8 @@ int bytecomp_layernorm_backward(int dtype, int wdtype, uint64_t rows, uint64_t c
     const bool sums = dweight || dbias;
     if (sums && rows > 0 && (!ws || ws_bytes < layernorm_ws(rows, cols))) return BC_E_WORKSPACE;
     const LnBackward a{dy, x, weight, mean, rstd, dx, sums ? (float*)ws : nullptr, rows, lddy, ldx, lddx,
-                       (uint32_t)cols, ln_parts(rows, (uint32_t)cols, dtype), (float)(1.0 / (double)cols)};
+                       (uint32_t)cols, ln_parts(rows, (uint32_t)cols, dtype), (float)(1.0 / (double)cols),
+                       streams(rows * cols * dtype_bytes(dtype))};
     hipStream_t s = (hipStream_t)stream;
     return finish_call(status_of(launch_ln_backward(dtype, wdtype, a, dweight, dbias, s)), s, nullptr);
 }
@@ -393,11 +405,16 @@ int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t c
     size_t need = 0;
     if (!readable(dtype, x, ldx, inner)) need += planes_bytes(dtype, rows, inner);
     if (!readable(dtype, w, ldw, inner)) need += planes_bytes(dtype, cols, inner);
+    const Cut cut = product_cut(dtype, rows, cols, inner);
+    const size_t sums = align256((size_t)split_bytes(cut, rows, cols));
+    need += sums;
     if (need > 0 && (!ws || ws_bytes < need)) return BC_E_WORKSPACE;
     Carver c{(char*)ws};
     Product p{};
-    hipError_t e = operand(dtype, x, ldx, rows, inner, c, p.a, s);
-    if (e == hipSuccess) e = operand(dtype, w, ldw, cols, inner, c, p.b, s);
+    LayOuts l{};
+    p.a = operand(dtype, x, ldx, rows, inner, c, l);
+    p.b = operand(dtype, w, ldw, cols, inner, c, l);
+    hipError_t e = launch_lay_outs(dtype, l, s);
     if (e == hipSuccess) {
         p.rows = (uint32_t)rows;
         p.cols = (uint32_t)cols;
@@ -410,7 +427,9 @@ int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t c
         p.ld_residual = ld_residual;
         p.ld_z = ldz;
         p.act = act;
-        e = launch_product(dtype, dtype, true, p, s);
+        p.nt = streams(rows * cols * dtype_bytes(dtype));
+        p.part = (float*)c.take(sums);
+        e = launch_product(dtype, dtype, true, cut, p, s);
     }
     return finish_call(status_of(e), s, nullptr);
 }
@@ -424,9 +443,9 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
     if (gdtype != dtype && gdtype != BC_F32) return BC_E_DTYPE;
     if (act < BC_ACT_NONE || act > BC_ACT_SILU) return BC_E_KIND;
     if (!dx && !dw && !dbias) return BC_OK;
-    const bool product = rows > 0 && cols > 0 && inner > 0;
+    const bool any = rows > 0 && cols > 0 && inner > 0;
     if (rows > 0 && cols > 0 && (!dy || (act != BC_ACT_NONE && !z))) return BC_E_NULL;
-    if (product && ((dw && !x) || (dx && !w))) return BC_E_NULL;
+    if (any && ((dw && !x) || (dx && !w))) return BC_E_NULL;
     if (lddy < cols || (act != BC_ACT_NONE && ldz < cols) || (dw && (ldx < inner || lddw < inner)) ||
         (dx && (ldw < inner || lddx < inner)))
         return BC_E_SIZE;
@@ -441,46 +460,50 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
     if (dw) need += planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows);
     const size_t part_bytes = align256((size_t)((rows + 63) / 64 * cols * sizeof(float)));
     if (dbias) need += part_bytes;
+    // the products' split sums share their place: one product follows the other
+    const Cut cut_x = product_cut(dtype, rows, inner, cols), cut_w = product_cut(dtype, cols, inner, rows);
+    const size_t sums = std::max(dx ? align256((size_t)split_bytes(cut_x, rows, inner)) : 0,
+                                 dw ? align256((size_t)split_bytes(cut_w, cols, inner)) : 0);
+    need += sums;
     if (need > 0 && (!ws || ws_bytes < need)) return BC_E_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     Carver c{(char*)ws};
-    hipError_t e = hipSuccess;
-    LayOut l{dy, act != BC_ACT_NONE ? z : nullptr, lddy, ldz, (uint32_t)rows, (uint32_t)cols, nullptr, nullptr,
-             nullptr, act};
-    if (flat) l.flat = c.take(planes_bytes(dtype, rows, cols));
-    if (dw) l.turned = c.take(planes_bytes(dtype, cols, rows));
-    if (dbias) l.part = (float*)c.take(part_bytes);
-    if (flat || dw || dbias) e = launch_lay_out(dtype, l, s);
+    float* part = (float*)c.take(sums);
+    LayOuts l{};
+    Planes dz{}, dz_turned{}, w_turned{}, x_turned{};
+    float* columns = nullptr;
+    if (flat || dw || dbias) {
+        LayOut& o = l.of[l.count++];
+        o = LayOut{dy, act != BC_ACT_NONE ? z : nullptr, lddy, ldz, (uint32_t)rows, (uint32_t)cols, nullptr, nullptr,
+                   nullptr, act};
+        if (flat) o.flat = c.take(planes_bytes(dtype, rows, cols));
+        if (dw) o.turned = c.take(planes_bytes(dtype, cols, rows));
+        if (dbias) o.part = columns = (float*)c.take(part_bytes);
+        dz = Planes{o.flat, plane_cols(cols), rows * plane_cols(cols)};
+        dz_turned = Planes{o.turned, plane_cols(rows), cols * plane_cols(rows)};
+    }
+    if (!flat) dz = Planes{dy, lddy, 0};
+    if (dx) w_turned = turned(dtype, w, ldw, cols, inner, c, l);
+    if (dw) x_turned = turned(dtype, x, ldx, rows, inner, c, l);
+    hipError_t e = launch_lay_outs(dtype, l, s);
     if (e == hipSuccess && dbias)
-        e = launch_sum_parts(gdtype, l.part, (uint32_t)((rows + 63) / 64), cols, (uint32_t)cols, dbias, nullptr, s);
-    if (e == hipSuccess && dx) {
+        e = launch_sum_parts(gdtype, columns, (uint32_t)((rows + 63) / 64), cols, (uint32_t)cols, dbias, nullptr, s);
+    auto product = [&](const Planes& a, const Planes& b, uint64_t m, uint64_t k, const Cut& cut, void* out, uint64_t ld,
+                       int out_dtype) {
         Product p{};
-        p.a = flat ? Planes{l.flat, plane_cols(cols), rows * plane_cols(cols)} : Planes{dy, lddy, 0};
-        void* turned = c.take(planes_bytes(dtype, inner, cols));
-        p.b = Planes{turned, plane_cols(cols), inner * plane_cols(cols)};
-        const LayOut t{w, nullptr, ldw, 0, (uint32_t)cols, (uint32_t)inner, nullptr, turned, nullptr, BC_ACT_NONE};
-        e = launch_lay_out(dtype, t, s);
-        p.rows = (uint32_t)rows;
+        p.a = a;
+        p.b = b;
+        p.rows = (uint32_t)m;
         p.cols = (uint32_t)inner;
-        p.steps = (uint32_t)(plane_cols(cols) / kPlaneCols);
-        p.out = dx;
-        p.ld_out = lddx;
-        if (e == hipSuccess) e = launch_product(dtype, dtype, false, p, s);
-    }
-    if (e == hipSuccess && dw) {
-        Product p{};
-        p.a = Planes{l.turned, plane_cols(rows), cols * plane_cols(rows)};
-        void* turned = c.take(planes_bytes(dtype, inner, rows));
-        p.b = Planes{turned, plane_cols(rows), inner * plane_cols(rows)};
-        const LayOut t{x, nullptr, ldx, 0, (uint32_t)rows, (uint32_t)inner, nullptr, turned, nullptr, BC_ACT_NONE};
-        e = launch_lay_out(dtype, t, s);
-        p.rows = (uint32_t)cols;
-        p.cols = (uint32_t)inner;
-        p.steps = (uint32_t)(plane_cols(rows) / kPlaneCols);
-        p.out = dw;
-        p.ld_out = lddw;
-        if (e == hipSuccess) e = launch_product(dtype, gdtype, false, p, s);
-    }
+        p.steps = (uint32_t)(plane_cols(k) / kPlaneCols);
+        p.out = out;
+        p.ld_out = ld;
+        p.nt = streams(m * inner * dtype_bytes(out_dtype));
+        p.part = part;
+        return launch_product(dtype, out_dtype, false, cut, p, s);
+    };
+    if (e == hipSuccess && dx) e = product(dz, w_turned, rows, cols, cut_x, dx, lddx, dtype);
+    if (e == hipSuccess && dw) e = product(dz_turned, x_turned, cols, rows, cut_w, dw, lddw, gdtype);
     return finish_call(status_of(e), s, nullptr);
 }
 

@@ -17,6 +17,9 @@
 #include "launch.hpp"
 #include "layers.hpp"
 
+#include <algorithm>
+#include <cmath>
+
 namespace bc {
 
 namespace {
@@ -102,13 +105,16 @@ __device__ __forceinline__ void store_planes(typename PlaneOf<T>::type* p, uint6
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void lay_out(LayOut a) {
+__global__ __launch_bounds__(256) void lay_out(LayOuts all) {
     typedef typename PlaneOf<T>::type E;
+    const int which = blockIdx.x >= all.first[2] ? 2 : blockIdx.x >= all.first[1] ? 1 : 0;
+    const LayOut& a = all.of[which];
+    const uint32_t block = blockIdx.x - all.first[which];
     __shared__ float tile[64][65];
     __shared__ float sums[4][64];
     const uint64_t flat_ld = plane_cols(a.cols), turned_ld = plane_cols(a.rows);
-    const uint32_t across = (uint32_t)(flat_ld / 64), by = blockIdx.x / across;
-    const uint32_t r0 = by * 64, c0 = blockIdx.x % across * 64;
+    const uint32_t across = (uint32_t)(flat_ld / 64), by = block / across;
+    const uint32_t r0 = by * 64, c0 = block % across * 64;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t lr = threadIdx.x / 8 + 32 * i, lc = threadIdx.x % 8 * 8;
@@ -155,64 +161,113 @@ __global__ __launch_bounds__(256) void lay_out(LayOut a) {
 }
 
 // ----------------------------------------------------------------- products
+// Eight columns of a row of the result from the fp32 sums v, in place.
+template <typename TO, bool forward>
+__device__ __forceinline__ void finish_row(const Product& p, uint64_t m, uint32_t n, float (&v)[8]) {
+    constexpr bool exact = sizeof(TO) == 4;
+    const int left = (int)(p.cols - n);
+    if constexpr (forward) {
+        float t[8];
+        if (p.bias) {
+            load_vec((const TO*)p.bias + n, left, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        if (p.z) store_vec((TO*)p.z + m * p.ld_z + n, left, v, p.nt);
+        if (p.act != BC_ACT_NONE)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate<exact>(p.act, v[i]);
+        if (p.residual) {
+            load_vec((const TO*)p.residual + m * p.ld_residual + n, left, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+    }
+    store_vec((TO*)p.out + m * p.ld_out + n, left, v, p.nt);
+}
+
 template <typename G, typename TO, bool forward>
 __global__ __launch_bounds__(G::kThreads) void product(Product p) {
     typedef typename G::T T;
     extern __shared__ char lds[];
+    const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     uint32_t tm, tn;
-    tile_of<8>(blockIdx.x, (p.rows + G::kBM - 1) / G::kBM, (p.cols + G::kBN - 1) / G::kBN, tm, tn);
+    tile_of<8>(blockIdx.x, tiles_m, tiles_n, tm, tn);
     const uint32_t m0 = tm * G::kBM, n0 = tn * G::kBN;
-    const Operand<T> a{(const T*)p.a.p + m0 * p.a.ld, (uint32_t)p.a.ld, p.a.plane, p.rows - m0};
-    const Operand<T> b{(const T*)p.b.p + n0 * p.b.ld, (uint32_t)p.b.ld, p.b.plane, p.cols - n0};
+    // this workgroup's steps along k
+    const uint32_t from = (uint32_t)((uint64_t)p.steps * blockIdx.y / p.split);
+    const uint32_t to = (uint32_t)((uint64_t)p.steps * (blockIdx.y + 1) / p.split);
+    const uint64_t k0 = (uint64_t)from * kPlaneCols;
+    const Operand<T> a{(const T*)p.a.p + m0 * p.a.ld + k0, (uint32_t)p.a.ld, p.a.plane, p.rows - m0};
+    const Operand<T> b{(const T*)p.b.p + n0 * p.b.ld + k0, (uint32_t)p.b.ld, p.b.plane, p.cols - n0};
     G g;
-    g.multiply(a, b, p.steps * (kPlaneCols / G::kBK), lds);
-    constexpr bool exact = sizeof(TO) == 4;
+    g.multiply(a, b, (to - from) * (kPlaneCols / G::kBK), lds);
+    float* part = p.split > 1 ? p.part + (uint64_t)blockIdx.y * p.rows * p.cols : nullptr;
     g.finish(lds, [&](int row, int col, float (&v)[8]) {
         const uint64_t m = m0 + row;
         const uint32_t n = n0 + col;
         if (m >= p.rows || n >= p.cols) return;
-        const int left = (int)(p.cols - n);
-        if constexpr (forward) {
-            float t[8];
-            if (p.bias) {
-                load_vec((const TO*)p.bias + n, left, t);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += t[i];
-            }
-            if (p.z) store_vec((TO*)p.z + m * p.ld_z + n, left, v);
-            if (p.act != BC_ACT_NONE)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate<exact>(p.act, v[i]);
-            if (p.residual) {
-                load_vec((const TO*)p.residual + m * p.ld_residual + n, left, t);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += t[i];
-            }
-        }
-        store_vec((TO*)p.out + m * p.ld_out + n, left, v);
+        if (part) store_vec(part + m * p.cols + n, (int)(p.cols - n), v);
+        else finish_row<TO, forward>(p, m, n, v);
     });
+}
+
+// The result from the sums of the parts of k, added in order.
+template <typename TO, bool forward>
+__global__ __launch_bounds__(256) void join_parts(Product p) {
+    const uint32_t across = (p.cols + 7) / 8;
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, m = i / across;
+    const uint32_t n = (uint32_t)(i % across) * 8;
+    if (m >= p.rows) return;
+    const int left = (int)(p.cols - n);
+    float v[8];
+    load_vec(p.part + m * p.cols + n, left, v);
+    for (uint32_t s = 1; s < p.split; ++s) {
+        float t[8];
+        load_vec(p.part + ((uint64_t)s * p.rows + m) * p.cols + n, left, t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += t[j];
+    }
+    finish_row<TO, forward>(p, m, n, v);
 }
 
 template <typename G, typename TO, bool forward>
 hipError_t launch_tiles(const Product& p, hipStream_t s) {
     // more LDS than a kernel may use by default; the attribute is per device
     // and setting it again costs next to nothing
-    const hipError_t e = hipFuncSetAttribute((const void*)product<G, TO, forward>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+    hipError_t e = hipFuncSetAttribute((const void*)product<G, TO, forward>,
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (e != hipSuccess) return e;
     const uint32_t tiles = ((p.rows + G::kBM - 1) / G::kBM) * ((p.cols + G::kBN - 1) / G::kBN);
-    hipLaunchKernelGGL((product<G, TO, forward>), dim3(tiles), dim3(G::kThreads), G::kLdsBytes, s, p);
+    hipLaunchKernelGGL((product<G, TO, forward>), dim3(tiles, p.split), dim3(G::kThreads), G::kLdsBytes, s, p);
+    e = hipGetLastError();
+    if (e != hipSuccess || p.split == 1) return e;
+    const uint64_t pieces = (uint64_t)p.rows * ((p.cols + 7) / 8);
+    hipLaunchKernelGGL((join_parts<TO, forward>), dim3((uint32_t)((pieces + 255) / 256)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 
+// Tile shapes, small to large, and what product_cut knows of them (us): a tile's
+// time for 64 along k with its compute unit nearly to itself, a compute unit's
+// share of it when the chip is full, and a tile's start and epilogue.  From
+// products of 768 x 768 x 1600 to 4096 x 4096 x 6400.
+struct TileCost {
+    uint32_t rows, cols;
+    double alone, full, ends;
+};
+constexpr TileCost kCost16[3] = {{64, 64, 0.30, 0.193, 0.5}, {128, 128, 0.60, 0.53, 2.0}, {256, 256, 1.05, 1.50, 11.0}};
+constexpr TileCost kCost32[3] = {{64, 64, 0.82, 0.95, 0.5}, {128, 128, 1.86, 2.56, 1.5}, {256, 128, 3.4, 4.68, 8.7}};
+
 template <typename T, typename TO, bool forward>
-hipError_t pick_tiles(const Product& p, hipStream_t s) {
+hipError_t launch_cut(int tile, const Product& p, hipStream_t s) {
     if constexpr (PlaneOf<T>::P == 3) {
+        if (tile == 0) return launch_tiles<GemmTile<bf16_t, 3, 64, 64, 32, 2, 2, 3>, TO, forward>(p, s);
+        if (tile == 1) return launch_tiles<GemmTile<bf16_t, 3, 128, 128, 32, 2, 4, 3>, TO, forward>(p, s);
         return launch_tiles<GemmTile<bf16_t, 3, 256, 128, 32, 4, 2, 2>, TO, forward>(p, s);
     } else {
-        const uint64_t big = (uint64_t)((p.rows + 255) / 256) * ((p.cols + 255) / 256);
-        if (big >= 160) return launch_tiles<GemmTile<T, 1, 256, 256, 64, 2, 4, 2>, TO, forward>(p, s);
-        return launch_tiles<GemmTile<T, 1, 128, 128, 64, 2, 2, 2>, TO, forward>(p, s);
+        if (tile == 0) return launch_tiles<GemmTile<T, 1, 64, 64, 64, 2, 2, 2>, TO, forward>(p, s);
+        if (tile == 1) return launch_tiles<GemmTile<T, 1, 128, 128, 64, 2, 4, 2>, TO, forward>(p, s);
+        return launch_tiles<GemmTile<T, 1, 256, 256, 64, 2, 4, 2>, TO, forward>(p, s);
     }
 }
 
@@ -339,29 +394,67 @@ void few_rows_launch(const FewRows& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_lay_out(int dtype, const LayOut& a, hipStream_t s) {
-    const dim3 grid((uint32_t)(plane_cols(a.cols) / 64 * (plane_cols(a.rows) / 64))), block(256);
-    if (grid.x == 0) return hipSuccess;
+hipError_t launch_lay_outs(int dtype, LayOuts& a, hipStream_t s) {
+    uint64_t n = 0;
+    for (int i = 0; i < 3; ++i) {
+        a.first[i] = (uint32_t)n;
+        if (i < a.count) n += plane_cols(a.of[i].cols) / 64 * (plane_cols(a.of[i].rows) / 64);
+        else a.first[i] = 0xFFFFFFFFu;
+    }
+    if (n == 0) return hipSuccess;
+    if (n >= (1ull << 31)) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)n), block(256);
     if (dtype == BC_F32) hipLaunchKernelGGL(lay_out<float>, grid, block, 0, s, a);
     else if (dtype == BC_F16) hipLaunchKernelGGL(lay_out<f16_t>, grid, block, 0, s, a);
     else hipLaunchKernelGGL(lay_out<bf16_t>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 
-hipError_t launch_product(int dtype, int out_dtype, bool forward, const Product& p, hipStream_t s) {
-    if (p.rows == 0 || p.cols == 0) return hipSuccess;
+// The cheapest cut by the costs above.  Splitting k pays where tiles are fewer
+// than compute units: its sums are written and read again (about 4 TB/s from
+// the caches) and joined in a launch of their own.
+Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
+    constexpr double kUnits = 256.0;
+    const TileCost* cost = dtype == BC_F32 ? kCost32 : kCost16;
+    const uint64_t steps = plane_cols(k) / kPlaneCols;
+    Cut best{0, 1};
+    double least = 1e30;
+    for (int i = 0; i < 3; ++i) {
+        const double tiles = (double)((rows + cost[i].rows - 1) / cost[i].rows) *
+                             (double)((cols + cost[i].cols - 1) / cost[i].cols);
+        for (uint32_t split = 1; split <= 32 && (split == 1 || (split * 4 <= steps && tiles * split <= 512)); split *= 2) {
+            const double each = (double)((steps + split - 1) / split);
+            const double full = each * cost[i].full + cost[i].ends, n = tiles * split / kUnits;
+            // the largest tiles come one to a unit, in whole rounds
+            const double busy = i == 2 ? std::ceil(n) * full : n <= 1.0 ? 0.0 : (n + 0.5) * full;
+            double t = std::max(each * cost[i].alone + cost[i].ends, busy);
+            if (split > 1) t += 4.0 + 2.0 * 4.0 * (double)split * (double)rows * (double)cols / 4e6;
+            if (t < least) {
+                least = t;
+                best = Cut{i, split};
+            }
+        }
+    }
+    return best;
+}
+
+hipError_t launch_product(int dtype, int out_dtype, bool forward, const Cut& cut, const Product& given, hipStream_t s) {
+    if (given.rows == 0 || given.cols == 0) return hipSuccess;
+    Product p = given;
+    p.split = cut.split;
+    const int t = cut.tile;
     if (forward) {
-        if (dtype == BC_F32) return pick_tiles<float, float, true>(p, s);
-        if (dtype == BC_F16) return pick_tiles<f16_t, f16_t, true>(p, s);
-        return pick_tiles<bf16_t, bf16_t, true>(p, s);
+        if (dtype == BC_F32) return launch_cut<float, float, true>(t, p, s);
+        if (dtype == BC_F16) return launch_cut<f16_t, f16_t, true>(t, p, s);
+        return launch_cut<bf16_t, bf16_t, true>(t, p, s);
     }
-    if (dtype == BC_F32) return pick_tiles<float, float, false>(p, s);
+    if (dtype == BC_F32) return launch_cut<float, float, false>(t, p, s);
     if (dtype == BC_F16) {
-        if (out_dtype == BC_F32) return pick_tiles<f16_t, float, false>(p, s);
-        return pick_tiles<f16_t, f16_t, false>(p, s);
+        if (out_dtype == BC_F32) return launch_cut<f16_t, float, false>(t, p, s);
+        return launch_cut<f16_t, f16_t, false>(t, p, s);
     }
-    if (out_dtype == BC_F32) return pick_tiles<bf16_t, float, false>(p, s);
-    return pick_tiles<bf16_t, bf16_t, false>(p, s);
+    if (out_dtype == BC_F32) return launch_cut<bf16_t, float, false>(t, p, s);
+    return launch_cut<bf16_t, bf16_t, false>(t, p, s);
 }
 
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s) {

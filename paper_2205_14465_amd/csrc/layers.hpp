@@ -16,6 +16,7 @@ struct LnForward {
     uint64_t rows, ldx, ldy;
     uint32_t cols;
     float inv_cols, eps;
+    bool nt;                // y is written with the non-temporal hint
 };
 struct LnBackward {
     const void *dy, *x, *weight;
@@ -25,6 +26,7 @@ struct LnBackward {
     uint64_t rows, lddy, ldx, lddx;
     uint32_t cols, parts;
     float inv_cols;
+    bool nt;                // dx likewise
 };
 // Workgroups that leave column sums for a call of this shape.
 uint32_t ln_parts(uint64_t rows, uint32_t cols, int dtype);
@@ -59,7 +61,13 @@ struct LayOut {
     float* part;             // [ceil(rows / 64)][cols] column sums of v, or NULL
     int act;
 };
-hipError_t launch_lay_out(int dtype, const LayOut& a, hipStream_t s);
+// Up to three matrices in one launch.
+struct LayOuts {
+    LayOut of[3];
+    uint32_t first[3];       // workgroups before each (those past `count`: all)
+    int count;
+};
+hipError_t launch_lay_outs(int dtype, LayOuts& a, hipStream_t s);
 
 // out [rows, cols] = epilogue(A B^T), A [rows, k], B [cols, k] as planes.
 struct Product {
@@ -72,8 +80,22 @@ struct Product {
     void* z;
     uint64_t ld_residual, ld_z;
     int act;
+    bool nt;                      // out and z are written with the non-temporal hint
+    float* part;                  // [split][rows][cols] sums of the parts of k, with split > 1
+    uint32_t split;
 };
-hipError_t launch_product(int dtype, int out_dtype, bool forward, const Product& p, hipStream_t s);
+// How a product of this shape is cut: the tiles' index and the parts of k (more
+// than one where tiles are few and long; their sums then need
+// split_bytes of workspace).
+struct Cut {
+    int tile;
+    uint32_t split;
+};
+Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k);
+inline uint64_t split_bytes(const Cut& c, uint64_t rows, uint64_t cols) {
+    return c.split > 1 ? c.split * rows * cols * sizeof(float) : 0;
+}
+hipError_t launch_product(int dtype, int out_dtype, bool forward, const Cut& cut, const Product& p, hipStream_t s);
 
 // The forward pass for few rows: x and w as the caller has them.
 struct FewRows {
