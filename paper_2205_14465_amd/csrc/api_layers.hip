@@ -178,7 +178,7 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.parts = (uint32_t)(tiles < kOrthoParts ? tiles : kOrthoParts);
     o.part = take(8 * o.parts);
     p.c.parts += o.parts;
-    p.c.tiles += (uint32_t)tiles;
+    p.c.tiles += (uint32_t)((tiles + p.run - 1) / p.run * p.run);
     for (int i = 0; i < kOrthoSides; ++i)
         for (int kind = 0; kind < kOrthoKinds; ++kind) {
             OrthoLoad& l = p.load[kind][i];
@@ -199,6 +199,11 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
 uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kind, std::vector<OrthoWork>& list) {
     constexpr int kDies = 8;
     std::vector<OrthoWork> die[kDies];
+    auto work = [&](size_t i, uint64_t tile) {
+        const Ortho& o = table[i];
+        return OrthoWork{(uint32_t)i, (uint32_t)tile, o.m, o.n, (uint32_t)(o.x >> 8), (uint32_t)(o.xt >> 8),
+                         (uint32_t)(o.sym >> 8), o.x_scale};
+    };
     const int side = p.side[kind];
     const OrthoLoad& all = p.load[kind][side];
     if (all.longest * all.tiles <= 1.25 * all.steps) {
@@ -206,7 +211,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kin
         for (size_t i = 0; i < table.size(); ++i) {
             const uint64_t tiles = ortho_tiles(table[i], kind, side);
             for (uint64_t t = 0; t < tiles; ++t) {
-                die[std::min(kDies - 1, (int)(done * kDies / all.steps))].push_back(OrthoWork{(uint32_t)i, (uint32_t)t});
+                die[std::min(kDies - 1, (int)(done * kDies / all.steps))].push_back(work(i, t));
                 done += ortho_steps(table[i], kind);
             }
         }
@@ -217,7 +222,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kin
             for (uint64_t q = 0; q < pieces; ++q) {
                 const int to = (int)(std::min_element(load, load + kDies) - load);
                 const uint64_t lo = tiles * q / pieces, hi = tiles * (q + 1) / pieces;
-                for (uint64_t t = lo; t < hi; ++t) die[to].push_back(OrthoWork{(uint32_t)i, (uint32_t)t});
+                for (uint64_t t = lo; t < hi; ++t) die[to].push_back(work(i, t));
                 load[to] += (double)(hi - lo) * ortho_steps(table[i], kind);
             }
         }
@@ -225,7 +230,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kin
     size_t longest = 0;
     for (const auto& d : die) longest = std::max(longest, d.size());
     for (size_t q = 0; q < longest; ++q)
-        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0});
+        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0, 0, 0, 0, 0, 0, 0.0f});
     return (uint32_t)(kDies * longest);
 }
 
@@ -266,6 +271,8 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
             o.cols = (uint32_t)cols;
             if (rows && cols) order.push_back({rows > cols ? rows : cols, i});
         }
+        // a workgroup's own start (the norm) costs about as much as a tile
+        p.run = tiles >= 4096 ? 4 : 1;
         std::sort(order.begin(), order.end(), [](const auto& x, const auto& y) {
             return x.first != y.first ? x.first > y.first : x.second < y.second;
         });
@@ -280,6 +287,7 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
         return BC_E_SIZE;
     }
     if (table.empty()) return BC_OK;
+    if (at >= (1ull << 40)) return BC_E_SIZE;  // offsets in 256 bytes stay within 32 bits
     if (!ws || ws_bytes < at) return BC_E_WORKSPACE;
     if ((uintptr_t)ws & 255) return BC_E_ALIGN;
     p.c.ws = (char*)ws;
@@ -511,6 +519,7 @@ int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* 
     if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
     if (!bytes || (T > 0 && (!rows || !cols))) return BC_E_NULL;
     OrthoPlan p{};
+    p.run = 1;
     uint64_t at = 0;
     for (int i = 0; i < T; ++i) {
         if (rows[i] >= kMaxDim || cols[i] >= kMaxDim) return BC_E_SIZE;

@@ -77,82 +77,113 @@ __device__ __forceinline__ void load_two(const f16_t* p, uint64_t plane, float (
     for (int i = 0; i < 8; ++i) v[i] = (float)hi[i] + (float)lo[i];
 }
 
-// Eight elements of the update U at (r, c); first: the momentum's new value is
-// made and kept (later passes find it there).
-template <bool first>
-__device__ __forceinline__ void load_update(const OrthoCall& a, const Ortho& o, uint64_t r, uint32_t c, int left,
-                                            float (&u)[8]) {
-    load_any(a.in_dtype, o.in, left ? r * o.ld_in + c : 0, left, u);
-    if (!a.muon) return;
-    float m[8];
-    float* at = o.momentum + (left ? r * o.ld_momentum + c : 0);
-    load_vec(at, left, m);
-    if constexpr (first) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m[i] = a.momentum * m[i] + u[i];
-        store_vec(at, left, m);
+// N elements of the update U at (r, c), fetched and then made: in the first
+// pass the momentum's new value is made and kept, later passes find it there.
+// (Fetches of several pieces go before the first store: the compiler cannot know
+// that they do not overlap.)
+template <typename T, int N>
+struct Update {
+    float g[N], m[N];
+    float* at;
+    int left;
+    __device__ __forceinline__ void fetch(const OrthoCall& a, const Ortho& o, uint64_t r, uint32_t c, int n) {
+        left = n;
+        load_vec((const T*)o.in + (left ? r * o.ld_in + c : 0), left, g);
+        if (!a.muon) return;
+        at = o.momentum + (left ? r * o.ld_momentum + c : 0);
+        load_vec(at, left, m);
     }
+    template <bool first>
+    __device__ __forceinline__ void make(const OrthoCall& a) {
+        if (!a.muon) return;
+        if constexpr (first) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = a.nesterov ? a.momentum * m[i] + u[i] : m[i];
-}
+            for (int i = 0; i < N; ++i) m[i] = a.momentum * m[i] + g[i];
+            store_vec(at, left, m);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = a.nesterov ? a.momentum * m[i] + g[i] : m[i];
+    }
+};
 
-// Sums of squares in fp64 (no overflow or underflow from any fp32 value): a
-// workgroup adds 64 x 64 tiles a fixed step apart, threads meet in a fixed tree.
+// Sums of squares in fp64 (no overflow or underflow from any fp32 value): the
+// workgroups of a matrix take its pieces of four elements in turn, row after
+// row, threads meet in a fixed tree.
+template <typename T>
 __global__ __launch_bounds__(256) void ortho_norm(OrthoCall a) {
     __shared__ double sh[4];
-    const Ortho& o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.part0; })];
-    const uint32_t part = blockIdx.x - o.part0;
-    const uint32_t across = (o.cols + 63) / 64, tiles = across * ((o.rows + 63) / 64);
+    const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.part0; })];
+    const uint32_t part = blockIdx.x - o.part0, across = (o.cols + 3) / 4;
+    const uint64_t pieces = (uint64_t)o.rows * across, step = (uint64_t)o.parts * 256;
     double sum = 0.0;
-    for (uint32_t t = part; t < tiles; t += o.parts) {
+    constexpr int kFetch = 2;
+    for (uint64_t q = (uint64_t)part * 256 + threadIdx.x; q < pieces; q += kFetch * step) {
+        Update<T, 4> u[kFetch];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t r = t / across * 64 + threadIdx.x / 8 + 32 * i, c = t % across * 64 + threadIdx.x % 8 * 8;
-            const int left = r < o.rows && c < o.cols ? (int)(o.cols - c) : 0;
-            float u[8];
-            load_update<true>(a, o, r, c, left, u);
+        for (int f = 0; f < kFetch; ++f) {
+            const uint64_t at = q + f * step;
+            const uint32_t r = pieces < (1ull << 32) ? (uint32_t)at / across : (uint32_t)(at / across);
+            const uint32_t c = (uint32_t)(at - (uint64_t)r * across) * 4;
+            u[f].fetch(a, o, r, c, at < pieces ? (int)(o.cols - c) : 0);
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += j < left ? (double)u[j] * (double)u[j] : 0.0;
+        for (int f = 0; f < kFetch; ++f) {
+            u[f].template make<true>(a);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += j < u[f].left ? (double)u[f].g[j] * (double)u[f].g[j] : 0.0;
         }
     }
     const double total = block_sum_f64(sum, sh);
     if (threadIdx.x == 0) ((double*)(a.ws + o.part))[part] = total;
 }
 
-// X_0 and its transpose as planes, a workgroup a 64 x 64 tile of U (columns
-// and rows past the end as zeros, as far as the planes go).
-__global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
+// X_0 and its transpose as planes, a workgroup up to `run` 64 x 64 tiles of U one
+// beside the other (columns and rows past the end as zeros, as far as the planes
+// go).
+template <typename T>
+__global__ __launch_bounds__(256) void ortho_start(OrthoCall a, uint32_t run) {
     __shared__ double sh[4];
     __shared__ float tile[64][65];
-    const Ortho& o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.tile0; })];
+    const Ortho o = a.d[owner(a.d, a.T, blockIdx.x * run, [](const Ortho& x) { return x.tile0; })];
     const double mine = threadIdx.x < o.parts ? ((const double*)(a.ws + o.part))[threadIdx.x] : 0.0;
     const float scale = (float)((double)o.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
-    const uint32_t t = blockIdx.x - o.tile0, across = (o.cols + 63) / 64;
-    const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+    const uint32_t across = (o.cols + 63) / 64;
     f16_t* flat = (f16_t*)(a.ws + (o.turned ? o.xt : o.x));
     f16_t* turned = (f16_t*)(a.ws + (o.turned ? o.x : o.xt));
     const uint64_t flat_ld = plane_cols(o.cols), turned_ld = plane_cols(o.rows);
+    for (uint32_t q = 0; q < run; ++q) {
+        const uint32_t t = blockIdx.x * run + q - o.tile0;
+        if (t >= across * ((o.rows + 63) / 64)) return;  // the same for the whole workgroup
+        const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+        Update<T, 8> u[2];
+        const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t lr = threadIdx.x / 8 + 32 * i, lc = threadIdx.x % 8 * 8, r = r0 + lr, c = c0 + lc;
-        const int left = r < o.rows && c < o.cols ? (int)(o.cols - c) : 0;
-        float u[8];
-        load_update<false>(a, o, r, c, left, u);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = r0 + threadIdx.x / 8 + 32 * i;
+            u[i].fetch(a, o, r, c, r < o.rows && c < o.cols ? (int)(o.cols - c) : 0);
+        }
+        if (q) __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = j < left ? u[j] * scale : 0.0f;  // 0 even where scale is infinite
-        if (r < o.rows) store_two(flat + r * flat_ld + c, o.rows * flat_ld, u);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t lr = threadIdx.x / 8 + 32 * i, r = r0 + lr;
+            u[i].template make<false>(a);
+            float (&v)[8] = u[i].g;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) tile[lr][lc + j] = u[j];
-    }
-    __syncthreads();
+            for (int j = 0; j < 8; ++j) v[j] = j < u[i].left ? v[j] * scale : 0.0f;  // 0 even where scale is infinite
+            if (r < o.rows) store_two(flat + r * flat_ld + c, o.rows * flat_ld, v);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t lc = threadIdx.x / 8 + 32 * i, lr = threadIdx.x % 8 * 8, c = c0 + lc, r = r0 + lr;
-        if (c < o.cols) {
-            float v[8];
+            for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];
+        }
+        __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = tile[lr + j][lc];
-            store_two(turned + c * turned_ld + r, o.cols * turned_ld, v);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t tc = threadIdx.x / 8 + 32 * i, tr = threadIdx.x % 8 * 8;
+            if (c0 + tc < o.cols) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = tile[tr + j][tc];
+                store_two(turned + (c0 + tc) * turned_ld + r0 + tr, o.cols * turned_ld, v);
+            }
         }
     }
 }
@@ -236,11 +267,14 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
     constexpr bool symmetric = stage == kGram || stage == kSym;
     const OrthoWork work = list[blockIdx.x];
     if (work.matrix == kOrthoIdle) return;
-    const Ortho& o = a.d[work.matrix];
-    const uint64_t mp = plane_cols(o.m), np = plane_cols(o.n);
-    const f16_t* x = (const f16_t*)(a.ws + o.x);
-    f16_t* xt[2] = {(f16_t*)(a.ws + o.xt), (f16_t*)(a.ws + o.xt) + 2 * o.n * mp};
-    auto sym = [&](int i) { return (f16_t*)(a.ws + o.sym) + i * (2 * o.m * mp); };
+    const uint32_t m = work.m, n = work.n;
+    const uint64_t mp = plane_cols(m), np = plane_cols(n);
+    f16_t* x = (f16_t*)(a.ws + ((uint64_t)work.x << 8));
+    f16_t* xt[2];
+    xt[0] = (f16_t*)(a.ws + ((uint64_t)work.xt << 8));
+    xt[1] = xt[0] + 2 * n * mp;
+    auto sym = [&](int i) { return (f16_t*)(a.ws + ((uint64_t)work.sym << 8)) + i * (2 * m * mp); };
+    const bool tall = stage == kLast && a.d[work.matrix].turned;
     const uint32_t t = work.tile;
     uint32_t tm, tn;
     if constexpr (symmetric) {
@@ -249,9 +283,8 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
         tm = t - tn * (tn + 1) / 2;
     } else {
-        const bool tall = stage == kLast && o.turned;
-        const uint32_t tiles_m = ((tall ? o.n : o.m) + G::kBM - 1) / G::kBM;
-        const uint32_t tiles_n = ((tall ? o.m : o.n) + G::kBN - 1) / G::kBN;
+        const uint32_t tiles_m = ((tall ? n : m) + G::kBM - 1) / G::kBM;
+        const uint32_t tiles_n = ((tall ? m : n) + G::kBN - 1) / G::kBN;
         const uint32_t band = t / (8 * tiles_n), first = band * 8;
         const uint32_t high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - first * tiles_n;
         tm = first + in % high;
@@ -263,27 +296,28 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         return Operand<f16_t>{p + at * ld, (uint32_t)ld, rows * ld, rows - at};
     };
     if constexpr (stage == kGram) {
-        g.multiply(rows_of(x, np, o.m, m0), rows_of(x, np, o.m, n0), (int)(np / G::kBK), lds);
-        const SymmetricEpilogue e{sym(s.out), nullptr, nullptr, mp, o.m * mp, o.m, m0, n0,
-                                  s.alpha / (o.x_scale * o.x_scale), 0.0f, 0.0f};
+        g.multiply(rows_of(x, np, m, m0), rows_of(x, np, m, n0), (int)(np / G::kBK), lds);
+        const SymmetricEpilogue e{sym(s.out), nullptr, nullptr, mp, m * mp, m, m0, n0,
+                                  s.alpha / (work.x_scale * work.x_scale), 0.0f, 0.0f};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kSym) {
-        g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(sym(s.v), mp, o.m, n0), (int)(mp / G::kBK), lds);
+        g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(sym(s.v), mp, m, n0), (int)(mp / G::kBK), lds);
         const SymmetricEpilogue e{sym(s.out), s.beta != 0.0f ? sym(s.u) : nullptr,
-                                  s.gamma != 0.0f ? sym(s.v) : nullptr, mp, o.m * mp, o.m, m0, n0,
+                                  s.gamma != 0.0f ? sym(s.v) : nullptr, mp, m * mp, m, m0, n0,
                                   s.alpha, s.beta, s.gamma};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kNext) {
-        g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(xt[s.from], mp, o.n, n0), (int)(mp / G::kBK), lds);
-        const NextEpilogue e{(f16_t*)x, xt[1 - s.from], np, mp, o.m, o.n, m0, n0, s.alpha, s.beta};
+        g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(xt[s.from], mp, n, n0), (int)(mp / G::kBK), lds);
+        const NextEpilogue e{x, xt[1 - s.from], np, mp, m, n, m0, n0, s.alpha, s.beta};
         g.finish_both_ways(lds, e);
     } else {
         // the caller's orientation: X, or its transpose, whose product is X^T U
-        const f16_t* old = o.turned ? xt[s.from] : x;
-        const uint64_t old_ld = o.turned ? mp : np, old_plane = o.turned ? o.n * mp : o.m * np;
-        if (o.turned) g.multiply(rows_of(old, mp, o.n, m0), rows_of(sym(s.u), mp, o.m, n0), (int)(mp / G::kBK), lds);
-        else g.multiply(rows_of(sym(s.u), mp, o.m, m0), rows_of(xt[s.from], mp, o.n, n0), (int)(mp / G::kBK), lds);
-        const float inv = 1.0f / o.x_scale;
+        const Ortho o = a.d[work.matrix];
+        const f16_t* old = tall ? xt[s.from] : x;
+        const uint64_t old_ld = tall ? mp : np, old_plane = tall ? n * mp : m * np;
+        if (tall) g.multiply(rows_of(old, mp, n, m0), rows_of(sym(s.u), mp, m, n0), (int)(mp / G::kBK), lds);
+        else g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(xt[s.from], mp, n, n0), (int)(mp / G::kBK), lds);
+        const float inv = 1.0f / work.x_scale;
         g.finish(lds, [&](int row, int col, float (&v)[8]) {
             const uint64_t r = m0 + row;
             const uint32_t c = n0 + col;
@@ -308,6 +342,7 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
 // the chip is full; a tile's start and epilogue.  From products of 768 x 768 x 768
 // to 4096 x 4096 x 6400; a launch ends, on average, half a tile after its mean.
 typedef GemmTile<f16_t, 2, 64, 64, 64, 2, 2, 2> Tile64;
+typedef GemmTile<f16_t, 2, 64, 64, 64, 2, 2, 3> Tile64Deep;
 typedef GemmTile<f16_t, 2, 128, 128, 64, 2, 4, 2> Tile128;
 typedef GemmTile<f16_t, 2, 256, 256, 32, 2, 4, 2> Tile256;
 constexpr double kAlone[kOrthoSides] = {0.32, 0.50, 1.55}, kFull[kOrthoSides] = {0.21, 0.63, 2.2};
@@ -335,9 +370,20 @@ hipError_t launch_tiles(const OrthoPlan& p, int kind, const StageArgs& a, hipStr
 template <int stage>
 hipError_t launch_stage(const OrthoPlan& p, const StageArgs& a, hipStream_t s) {
     constexpr int kind = stage == kGram ? kOrthoGram : stage == kSym ? kOrthoSym : kOrthoFull;
+    // A compute unit holds two workgroups of the one or one of the other, whose
+    // loads run further ahead: one 768 x 768 matrix (144 tiles) 155 us against 184,
+    // ResNet-50's list 1056 against 1045.
+    if (p.side[kind] == 0 && p.workgroups[kind] <= (uint32_t)p.cus) return launch_tiles<Tile64Deep, stage>(p, kind, a, s);
     if (p.side[kind] == 0) return launch_tiles<Tile64, stage>(p, kind, a, s);
     if (p.side[kind] == 1) return launch_tiles<Tile128, stage>(p, kind, a, s);
     return launch_tiles<Tile256, stage>(p, kind, a, s);
+}
+
+template <typename T>
+hipError_t launch_start(const OrthoPlan& p, hipStream_t s) {
+    hipLaunchKernelGGL(ortho_norm<T>, dim3(p.c.parts), dim3(256), 0, s, p.c);
+    hipLaunchKernelGGL(ortho_start<T>, dim3(p.c.tiles / p.run), dim3(256), 0, s, p.c, p.run);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -357,9 +403,9 @@ void ortho_choose(OrthoPlan& p) {
 
 hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
     const OrthoCall& c = p.c;
-    hipLaunchKernelGGL(ortho_norm, dim3(c.parts), dim3(256), 0, s, c);
-    hipLaunchKernelGGL(ortho_start, dim3(c.tiles), dim3(256), 0, s, c);
-    hipError_t e = hipGetLastError();
+    hipError_t e = c.in_dtype == BC_F32   ? launch_start<float>(p, s)
+                   : c.in_dtype == BC_F16 ? launch_start<f16_t>(p, s)
+                                          : launch_start<bf16_t>(p, s);
     // out = alpha U V + beta U + gamma V, each matrix with the scale of its kind
     auto sym = [&](int u, SymScale ku, int v, SymScale kv, int out, SymScale ko, float alpha, float beta, float gamma) {
         const float *k = c.scale, to = k[ko];

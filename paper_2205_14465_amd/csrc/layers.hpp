@@ -124,17 +124,21 @@ struct Ortho {
     uint32_t rows, cols, m, n;
     uint32_t turned, parts;  // parts: partial sums of squares
     uint32_t part0;          // workgroups before this matrix's: of the norm,
-    uint32_t tile0;          // of the 64 x 64 tiles of the start
+    uint32_t tile0;          // of the 64 x 64 tiles of the start (a multiple of OrthoPlan::run)
     float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
 };
 static_assert(sizeof(Ortho) == 8 * 10 + 4 * 10, "Ortho layout");
 
 // What a workgroup of a product launch computes: a tile of a matrix, or
-// nothing (matrix kOrthoIdle).
+// nothing (matrix kOrthoIdle).  It carries what all but the last product need of
+// the matrix, so that a workgroup's operands are one load from its start.
 struct OrthoWork {
-    uint32_t matrix, tile;
+    uint32_t matrix, tile, m, n;
+    uint32_t x, xt, sym;     // offsets in the workspace, in 256 bytes
+    float x_scale;
 };
+static_assert(sizeof(OrthoWork) == 32, "OrthoWork layout");
 constexpr uint32_t kOrthoIdle = 0xFFFFFFFFu;
 
 // The work of a launch with one tile side: tiles, and steps of 32 along k, in
@@ -163,6 +167,7 @@ struct OrthoPlan {
     OrthoLoad load[kOrthoKinds][kOrthoSides];
     int side[kOrthoKinds];             // the tile side chosen (ortho_choose)
     uint32_t workgroups[kOrthoKinds];  // and its launch's size
+    uint32_t run;                      // tiles of the start that a workgroup makes
     const OrthoWork* list[kOrthoKinds];
     bool pairs;                        // two steps from one Gram matrix
 };
