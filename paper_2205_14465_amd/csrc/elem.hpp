@@ -22,10 +22,18 @@ template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);
 
 // V consecutive elements widened to fp32; the first `left` of them when
-// fewer are left (the others 0, not read).
-template <typename T, int V>
+// fewer are left (the others 0, not read).  kWhole: left is at least V or at
+// most 0, which the caller knows of all its lanes; without the branch for a part
+// the compiler lets loads follow each other unwaited for.
+template <bool kWhole = false, typename T, int V>
 __device__ __forceinline__ void load_vec(const T* p, int left, float (&f)[V]) {
-    if (left >= V) {
+    if constexpr (kWhole) {
+        typedef T vec __attribute__((ext_vector_type(V)));
+        vec v = (T)0.0f;
+        if (left > 0) __builtin_memcpy(&v, p, sizeof(v));
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = (float)v[i];
+    } else if (left >= V) {
         typedef T vec __attribute__((ext_vector_type(V)));
         vec v;
         __builtin_memcpy(&v, p, sizeof(v));
@@ -42,8 +50,12 @@ template <typename T, int V>
 struct Raw {
     typedef T vec __attribute__((ext_vector_type(V)));
     vec v;
+    template <bool kWhole = false>
     __device__ __forceinline__ void load(const T* p, int left) {
-        if (left >= V) {
+        if constexpr (kWhole) {
+            v = (T)0.0f;
+            if (left > 0) __builtin_memcpy(&v, p, sizeof(v));
+        } else if (left >= V) {
             __builtin_memcpy(&v, p, sizeof(v));
         } else {
 #pragma unroll

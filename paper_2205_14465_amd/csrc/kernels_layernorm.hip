@@ -40,10 +40,10 @@ __device__ __forceinline__ float group_sum(float x, float* sh) {
 }
 
 // Weights of N columns from c, `none` where the call has no weights.
-template <typename WT, int N>
+template <bool kWhole, typename WT, int N>
 __device__ __forceinline__ void load_weight(const void* w, uint32_t c, int left, float none, float (&f)[N]) {
     if (w) {
-        load_vec((const WT*)w + c, left, f);
+        load_vec<kWhole>((const WT*)w + c, left, f);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = none;
@@ -52,10 +52,10 @@ __device__ __forceinline__ void load_weight(const void* w, uint32_t c, int left,
 
 // ---------------------------------------------------------------- forward
 // kGroup threads a row (64: four rows a workgroup, kLnBlock: one), kPer
-// vectors a thread.  (Rows following each other with their weights in registers,
+// vectors a thread; kWhole: rows are whole vectors.  (Rows following each other with their weights in registers,
 // as in the backward pass, measured 14.3 us against 13.5 at 8192 x 1600: the
 // registers cost more waves than the weights cost loads.)
-template <typename T, typename WT, int kGroup, int kPer>
+template <typename T, typename WT, int kGroup, int kPer, bool kWhole>
 __global__ __launch_bounds__(kLnBlock) void ln_forward(LnForward a) {
     constexpr int V = kVec<T>;
     __shared__ float sh[kLnWaves];
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kLnBlock) void ln_forward(LnForward a) {
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
         const int c = (p * kGroup + j) * V;
-        load_vec(x + c, (int)a.cols - c, v[p]);
+        load_vec<kWhole>(x + c, (int)a.cols - c, v[p]);
     }
 #pragma unroll
     for (int p = 0; p < kPer; ++p)
@@ -96,8 +96,8 @@ __global__ __launch_bounds__(kLnBlock) void ln_forward(LnForward a) {
         const int c = (p * kGroup + j) * V, left = (int)a.cols - c;
         if (left > 0) {
             float w[V], b[V], o[V];
-            load_weight<WT>(a.weight, c, left, 1.0f, w);
-            load_weight<WT>(a.bias, c, left, 0.0f, b);
+            load_weight<kWhole, WT>(a.weight, c, left, 1.0f, w);
+            load_weight<kWhole, WT>(a.bias, c, left, 0.0f, b);
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = (v[p][i] - mean) * rstd * w[i] + b[i];
             store_vec(y + c, left, o, a.nt);
@@ -148,8 +148,8 @@ __global__ __launch_bounds__(kWideBlock) void ln_forward_wide(LnForward a) {
         const int left = (int)(a.cols - c);
         float v[V], w[V], b[V];
         load_vec(x + c, left, v);
-        load_weight<WT>(a.weight, c, left, 1.0f, w);
-        load_weight<WT>(a.bias, c, left, 0.0f, b);
+        load_weight<false, WT>(a.weight, c, left, 1.0f, w);
+        load_weight<false, WT>(a.bias, c, left, 0.0f, b);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = (v[i] - mean) * rstd * w[i] + b[i];
         store_vec(y + c, left, v, a.nt);
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kWideBlock) void ln_forward_wide(LnForward a) {
 // j, j + kGroup, ...  The next row's loads are in flight under the arithmetic of
 // the last; weights stay in registers.  The waves of a workgroup then meet in
 // LDS, and the workgroup's sums go to part[block] (cols of dw, then cols of db).
-template <typename T, typename WT, int kGroup, int kPer>
+template <typename T, typename WT, int kGroup, int kPer, bool kWhole>
 __global__ __launch_bounds__(kLnBlock) void ln_backward(LnBackward a) {
     constexpr int V = kVec<T>;
     __shared__ float sh[kLnWaves];
@@ -177,15 +177,15 @@ __global__ __launch_bounds__(kLnBlock) void ln_backward(LnBackward a) {
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             const int c = (p * kGroup + j) * V;
-            nx[p].load(x + c, (int)a.cols - c);
-            ny[p].load(dy + c, (int)a.cols - c);
+            nx[p].template load<kWhole>(x + c, (int)a.cols - c);
+            ny[p].template load<kWhole>(dy + c, (int)a.cols - c);
         }
     };
     if (unit < a.rows) fetch(unit);
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
         const int c = (p * kGroup + j) * V;
-        load_weight<WT>(a.weight, c, (int)a.cols - c, 1.0f, w[p]);
+        load_weight<kWhole, WT>(a.weight, c, (int)a.cols - c, 1.0f, w[p]);
 #pragma unroll
         for (int i = 0; i < V; ++i) aw[p][i] = ab[p][i] = 0.0f;
     }
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kWideBlock) void ln_backward_wide(LnBackward a) {
         float v[V], d[V], w[V];
         load_vec(x + c, left, v);
         load_vec(dy + c, left, d);
-        load_weight<WT>(a.weight, c, left, 1.0f, w);
+        load_weight<false, WT>(a.weight, c, left, 1.0f, w);
         float p1 = 0.0f, p2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kWideBlock) void ln_backward_wide(LnBackward a) {
         float v[V], d[V], w[V];
         load_vec(x + c, left, v);
         load_vec(dy + c, left, d);
-        load_weight<WT>(a.weight, c, left, 1.0f, w);
+        load_weight<false, WT>(a.weight, c, left, 1.0f, w);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = rstd * (d[i] * w[i] - s1 - (v[i] - mean) * rstd * s2);
         store_vec(dx + c, left, v, a.nt);
@@ -389,28 +389,28 @@ hipError_t launch_sum_parts(int dtype, const float* part, uint32_t parts, uint64
 
 // Rows of up to 64 * kPer vectors go to a wave, of up to kLnBlock * kPer to a
 // workgroup, longer ones to the wide kernels.
-template <typename T, typename WT>
+template <typename T, typename WT, bool kWhole>
 static void ln_forward_launch(const LnForward& a, hipStream_t s) {
     const uint32_t vecs = (a.cols + kVec<T> - 1) / kVec<T>;
     const dim3 block(kLnBlock), waves((uint32_t)((a.rows + kLnWaves - 1) / kLnWaves)), rows((uint32_t)a.rows);
-    if (vecs <= 64) hipLaunchKernelGGL((ln_forward<T, WT, 64, 1>), waves, block, 0, s, a);
-    else if (vecs <= 128) hipLaunchKernelGGL((ln_forward<T, WT, 64, 2>), waves, block, 0, s, a);
-    else if (vecs <= 256) hipLaunchKernelGGL((ln_forward<T, WT, 64, 4>), waves, block, 0, s, a);
-    else if (vecs <= 512) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 2>), rows, block, 0, s, a);
-    else if (vecs <= 1024) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 4>), rows, block, 0, s, a);
-    else if (vecs <= 2048) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 8>), rows, block, 0, s, a);
+    if (vecs <= 64) hipLaunchKernelGGL((ln_forward<T, WT, 64, 1, kWhole>), waves, block, 0, s, a);
+    else if (vecs <= 128) hipLaunchKernelGGL((ln_forward<T, WT, 64, 2, kWhole>), waves, block, 0, s, a);
+    else if (vecs <= 256) hipLaunchKernelGGL((ln_forward<T, WT, 64, 4, kWhole>), waves, block, 0, s, a);
+    else if (vecs <= 512) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 2, kWhole>), rows, block, 0, s, a);
+    else if (vecs <= 1024) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 4, kWhole>), rows, block, 0, s, a);
+    else if (vecs <= 2048) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 8, kWhole>), rows, block, 0, s, a);
     else hipLaunchKernelGGL((ln_forward_wide<T, WT>), rows, dim3(kWideBlock), 0, s, a);
 }
 
-template <typename T, typename WT>
+template <typename T, typename WT, bool kWhole>
 static void ln_backward_launch(const LnBackward& a, hipStream_t s) {
     const uint32_t vecs = (a.cols + kVec<T> - 1) / kVec<T>;
     const dim3 block(kLnBlock), grid(a.parts);
-    if (vecs <= 64) hipLaunchKernelGGL((ln_backward<T, WT, 64, 1>), grid, block, 0, s, a);
-    else if (vecs <= 128) hipLaunchKernelGGL((ln_backward<T, WT, 64, 2>), grid, block, 0, s, a);
-    else if (vecs <= 256) hipLaunchKernelGGL((ln_backward<T, WT, 64, 4>), grid, block, 0, s, a);
-    else if (vecs <= 512) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 2>), grid, block, 0, s, a);
-    else if (vecs <= 1024) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 4>), grid, block, 0, s, a);
+    if (vecs <= 64) hipLaunchKernelGGL((ln_backward<T, WT, 64, 1, kWhole>), grid, block, 0, s, a);
+    else if (vecs <= 128) hipLaunchKernelGGL((ln_backward<T, WT, 64, 2, kWhole>), grid, block, 0, s, a);
+    else if (vecs <= 256) hipLaunchKernelGGL((ln_backward<T, WT, 64, 4, kWhole>), grid, block, 0, s, a);
+    else if (vecs <= 512) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 2, kWhole>), grid, block, 0, s, a);
+    else if (vecs <= 1024) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 4, kWhole>), grid, block, 0, s, a);
     else {
         if (a.dx) hipLaunchKernelGGL((ln_backward_wide<T, WT>), dim3((uint32_t)a.rows), dim3(kWideBlock), 0, s, a);
         if (a.part)
@@ -425,22 +425,33 @@ uint32_t ln_parts(uint64_t rows, uint32_t cols, int dtype) {
     return (uint32_t)(units < most ? units : most);
 }
 
+template <typename T, typename WT>
+static void ln_forward_any(const LnForward& a, hipStream_t s) {
+    if (a.cols % kVec<T> == 0) ln_forward_launch<T, WT, true>(a, s);
+    else ln_forward_launch<T, WT, false>(a, s);
+}
+template <typename T, typename WT>
+static void ln_backward_any(const LnBackward& a, hipStream_t s) {
+    if (a.cols % kVec<T> == 0) ln_backward_launch<T, WT, true>(a, s);
+    else ln_backward_launch<T, WT, false>(a, s);
+}
+
 hipError_t launch_ln_forward(int dtype, int wdtype, const LnForward& a, hipStream_t s) {
-    if (dtype == BC_F32) ln_forward_launch<float, float>(a, s);
-    else if (dtype == BC_F16 && wdtype == BC_F16) ln_forward_launch<f16_t, f16_t>(a, s);
-    else if (dtype == BC_F16) ln_forward_launch<f16_t, float>(a, s);
-    else if (wdtype == BC_BF16) ln_forward_launch<bf16_t, bf16_t>(a, s);
-    else ln_forward_launch<bf16_t, float>(a, s);
+    if (dtype == BC_F32) ln_forward_any<float, float>(a, s);
+    else if (dtype == BC_F16 && wdtype == BC_F16) ln_forward_any<f16_t, f16_t>(a, s);
+    else if (dtype == BC_F16) ln_forward_any<f16_t, float>(a, s);
+    else if (wdtype == BC_BF16) ln_forward_any<bf16_t, bf16_t>(a, s);
+    else ln_forward_any<bf16_t, float>(a, s);
     return hipGetLastError();
 }
 
 hipError_t launch_ln_backward(int dtype, int wdtype, const LnBackward& a, void* dweight, void* dbias, hipStream_t s) {
     if (a.rows) {
-        if (dtype == BC_F32) ln_backward_launch<float, float>(a, s);
-        else if (dtype == BC_F16 && wdtype == BC_F16) ln_backward_launch<f16_t, f16_t>(a, s);
-        else if (dtype == BC_F16) ln_backward_launch<f16_t, float>(a, s);
-        else if (wdtype == BC_BF16) ln_backward_launch<bf16_t, bf16_t>(a, s);
-        else ln_backward_launch<bf16_t, float>(a, s);
+        if (dtype == BC_F32) ln_backward_any<float, float>(a, s);
+        else if (dtype == BC_F16 && wdtype == BC_F16) ln_backward_any<f16_t, f16_t>(a, s);
+        else if (dtype == BC_F16) ln_backward_any<f16_t, float>(a, s);
+        else if (wdtype == BC_BF16) ln_backward_any<bf16_t, bf16_t>(a, s);
+        else ln_backward_any<bf16_t, float>(a, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace bc {
 
@@ -115,48 +116,54 @@ __global__ __launch_bounds__(256) void lay_out(LayOuts all) {
     const uint64_t flat_ld = plane_cols(a.cols), turned_ld = plane_cols(a.rows);
     const uint32_t across = (uint32_t)(flat_ld / 64), by = block / across;
     const uint32_t r0 = by * 64, c0 = block % across * 64;
+    const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
+    float v[2][8], z[2][8];
+    auto fetch = [&](auto whole) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = r0 + threadIdx.x / 8 + 32 * i;
+            const int left = r < a.rows && c < a.cols ? (int)(a.cols - c) : 0;
+            load_vec<decltype(whole)::value>((const T*)a.in + (left > 0 ? r * a.ld_in + c : 0), left, v[i]);
+            if (a.z) load_vec<decltype(whole)::value>((const T*)a.z + (left > 0 ? r * a.ld_z + c : 0), left, z[i]);
+        }
+    };
+    if (a.cols % 8 == 0 || c0 + 64 <= a.cols) fetch(std::true_type{});
+    else fetch(std::false_type{});
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint32_t lr = threadIdx.x / 8 + 32 * i, lc = threadIdx.x % 8 * 8;
-        const uint32_t r = r0 + lr, c = c0 + lc;
-        const int left = r < a.rows && c < a.cols ? (int)(a.cols - c) : 0;
-        float v[8];
-        load_vec((const T*)a.in + (left ? r * a.ld_in + c : 0), left, v);
-        if (a.z) {
-            float z[8];
-            load_vec((const T*)a.z + (left ? r * a.ld_z + c : 0), left, z);
+        const uint32_t lr = threadIdx.x / 8 + 32 * i, r = r0 + lr;
+        if (a.z)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] * act_slope<sizeof(T) == 4>(a.act, z[j]) : 0.0f;
-        }
+            for (int j = 0; j < 8; ++j)
+                v[i][j] = r < a.rows && c + j < a.cols ? v[i][j] * act_slope<sizeof(T) == 4>(a.act, z[i][j]) : 0.0f;
         if (a.flat && r < a.rows && c < flat_ld)
-            store_planes<T>((E*)a.flat + r * flat_ld + c, (uint64_t)a.rows * flat_ld, v);
+            store_planes<T>((E*)a.flat + r * flat_ld + c, (uint64_t)a.rows * flat_ld, v[i]);
         if (a.turned || a.part)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];
+            for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[i][j];
     }
     if (!a.turned && !a.part) return;
     __syncthreads();
     if (a.turned)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t lc = threadIdx.x / 8 + 32 * i, lr = threadIdx.x % 8 * 8;
-            const uint32_t c = c0 + lc, r = r0 + lr;
-            if (c < a.cols && r < turned_ld) {
-                float v[8];
+            const uint32_t tc = threadIdx.x / 8 + 32 * i, tr = threadIdx.x % 8 * 8;
+            if (c0 + tc < a.cols && r0 + tr < turned_ld) {
+                float w[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = tile[lr + j][lc];
-                store_planes<T>((E*)a.turned + c * turned_ld + r, (uint64_t)a.cols * turned_ld, v);
+                for (int j = 0; j < 8; ++j) w[j] = tile[tr + j][tc];
+                store_planes<T>((E*)a.turned + (c0 + tc) * turned_ld + r0 + tr, (uint64_t)a.cols * turned_ld, w);
             }
         }
     if (a.part) {
-        const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
+        const int tc = threadIdx.x & 63, g = threadIdx.x >> 6;
         float s = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s += tile[g * 16 + r][c];
-        sums[g][c] = s;
+        for (int r = 0; r < 16; ++r) s += tile[g * 16 + r][tc];
+        sums[g][tc] = s;
         __syncthreads();
-        if (g == 0 && c0 + c < a.cols)
-            a.part[(uint64_t)by * a.cols + c0 + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+        if (g == 0 && c0 + tc < a.cols)
+            a.part[(uint64_t)by * a.cols + c0 + tc] = (sums[0][tc] + sums[1][tc]) + (sums[2][tc] + sums[3][tc]);
     }
 }
 

@@ -86,12 +86,13 @@ struct Update {
     float g[N], m[N];
     float* at;
     int left;
+    template <bool kWhole>
     __device__ __forceinline__ void fetch(const OrthoCall& a, const Ortho& o, uint64_t r, uint32_t c, int n) {
         left = n;
-        load_vec((const T*)o.in + (left ? r * o.ld_in + c : 0), left, g);
+        load_vec<kWhole>((const T*)o.in + (left ? r * o.ld_in + c : 0), left, g);
         if (!a.muon) return;
         at = o.momentum + (left ? r * o.ld_momentum + c : 0);
-        load_vec(at, left, m);
+        load_vec<kWhole>(at, left, m);
     }
     template <bool first>
     __device__ __forceinline__ void make(const OrthoCall& a) {
@@ -115,6 +116,7 @@ __global__ __launch_bounds__(256) void ortho_norm(OrthoCall a) {
     const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.part0; })];
     const uint32_t part = blockIdx.x - o.part0, across = (o.cols + 3) / 4;
     const uint64_t pieces = (uint64_t)o.rows * across, step = (uint64_t)o.parts * 256;
+    const bool whole = o.cols % 4 == 0;
     double sum = 0.0;
     constexpr int kFetch = 2;
     for (uint64_t q = (uint64_t)part * 256 + threadIdx.x; q < pieces; q += kFetch * step) {
@@ -124,7 +126,9 @@ __global__ __launch_bounds__(256) void ortho_norm(OrthoCall a) {
             const uint64_t at = q + f * step;
             const uint32_t r = pieces < (1ull << 32) ? (uint32_t)at / across : (uint32_t)(at / across);
             const uint32_t c = (uint32_t)(at - (uint64_t)r * across) * 4;
-            u[f].fetch(a, o, r, c, at < pieces ? (int)(o.cols - c) : 0);
+            const int n = at < pieces ? (int)(o.cols - c) : 0;
+            if (whole) u[f].template fetch<true>(a, o, r, c, n);
+            else u[f].template fetch<false>(a, o, r, c, n);
         }
 #pragma unroll
         for (int f = 0; f < kFetch; ++f) {
@@ -155,12 +159,15 @@ __global__ __launch_bounds__(256) void ortho_start(OrthoCall a, uint32_t run) {
         const uint32_t t = blockIdx.x * run + q - o.tile0;
         if (t >= across * ((o.rows + 63) / 64)) return;  // the same for the whole workgroup
         const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+        const bool whole = o.cols % 8 == 0 || c0 + 64 <= o.cols;
         Update<T, 8> u[2];
         const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t r = r0 + threadIdx.x / 8 + 32 * i;
-            u[i].fetch(a, o, r, c, r < o.rows && c < o.cols ? (int)(o.cols - c) : 0);
+            const int n = r < o.rows && c < o.cols ? (int)(o.cols - c) : 0;
+            if (whole) u[i].template fetch<true>(a, o, r, c, n);
+            else u[i].template fetch<false>(a, o, r, c, n);
         }
         if (q) __syncthreads();
 #pragma unroll
