@@ -85,6 +85,9 @@ struct GemmTile {
     static_assert(kLoadA * kRows * kWaves == kBM && kLoadB * kRows * kWaves == kBN, "loads cover the tile");
 
     f32x16 acc[kFM][kFN];
+    // Small tiles have the registers to add the products of lesser planes apart:
+    // two thirds (P = 2) of the roundings at the size of the sum fall away.
+    static constexpr bool kApart = P > 1 && kFM * kFN <= 2;
 
     static __device__ __forceinline__ int swizzle(int row) { return kBK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
@@ -138,6 +141,15 @@ struct GemmTile {
                     va[set][p][m] = *(const typename Frag<T>::type*)(fa + at + (p * kBM + m * 32) * kRow);
             }
         };
+        f32x16 lesser[kApart ? kFM : 1][kApart ? kFN : 1];
+        if constexpr (kApart) {
+#pragma unroll
+            for (int m = 0; m < kFM; ++m)
+#pragma unroll
+                for (int n = 0; n < kFN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) lesser[m][n][r] = 0.0f;
+        }
         auto mma = [&](int set) {
 #pragma unroll
             for (int pa = 0; pa < P; ++pa)
@@ -146,8 +158,10 @@ struct GemmTile {
 #pragma unroll
                     for (int m = 0; m < kFM; ++m)
 #pragma unroll
-                        for (int n = 0; n < kFN; ++n)
-                            acc[m][n] = Frag<T>::mma(vb[set][pb][n], va[set][pa][m], acc[m][n]);
+                        for (int n = 0; n < kFN; ++n) {
+                            f32x16& to = kApart && pa + pb > 0 ? lesser[kApart ? m : 0][kApart ? n : 0] : acc[m][n];
+                            to = Frag<T>::mma(vb[set][pb][n], va[set][pa][m], to);
+                        }
         };
         constexpr int kKK = kBK / 16, kReads = P * (kFM + kFN), kMma = P * (P + 1) / 2 * kFM * kFN;
         static_assert(kKK % 2 == 0, "fragment sets alternate");
@@ -205,6 +219,12 @@ struct GemmTile {
         int step = 0;
         for (; step + kStages < steps; ++step) work(Yes{}, step);
         for (; step < steps; ++step) work(No{}, step);
+        if constexpr (kApart) {
+#pragma unroll
+            for (int m = 0; m < kFM; ++m)
+#pragma unroll
+                for (int n = 0; n < kFN; ++n) acc[m][n] += lesser[m][n];
+        }
         lds_barrier();  // every wave has read its last fragments: the epilogue may write LDS
     }
 
