@@ -178,10 +178,10 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.parts = (uint32_t)(tiles < kOrthoParts ? tiles : kOrthoParts);
     o.part = take(8 * o.parts);
     p.c.parts += o.parts;
-    p.c.tiles += (uint32_t)((tiles + p.run - 1) / p.run * p.run);
+    p.c.tiles += (uint32_t)tiles;
     for (int i = 0; i < kOrthoSides; ++i)
         for (int kind = 0; kind < kOrthoKinds; ++kind) {
-            OrthoLoad& l = p.load[kind][i];
+            OrthoLoad& l = p.group[ortho_group(p.c, o.m)].load[kind][i];
             const double steps = ortho_steps(o, kind);
             l.tiles += (double)ortho_tiles(o, kind, i);
             l.steps += (double)ortho_tiles(o, kind, i) * steps;
@@ -196,7 +196,8 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
 // smaller ones go whole to the least loaded die, the long tiles first.  `list`
 // receives 8 x the longest die's count entries, the others' ends idle; returns
 // that count.
-uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kind, std::vector<OrthoWork>& list) {
+uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int group, int kind,
+                    std::vector<OrthoWork>& list) {
     constexpr int kDies = 8;
     std::vector<OrthoWork> die[kDies];
     auto work = [&](size_t i, uint64_t tile) {
@@ -204,11 +205,13 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kin
         return OrthoWork{(uint32_t)i, (uint32_t)tile, o.m, o.n, (uint32_t)(o.x >> 8), (uint32_t)(o.xt >> 8),
                          (uint32_t)(o.sym >> 8), o.x_scale};
     };
-    const int side = p.side[kind];
-    const OrthoLoad& all = p.load[kind][side];
+    const OrthoGroup& g = p.group[group];
+    const int side = g.side[kind];
+    const OrthoLoad& all = g.load[kind][side];
     if (all.longest * all.tiles <= 1.25 * all.steps) {
         double done = 0.0;
         for (size_t i = 0; i < table.size(); ++i) {
+            if (ortho_group(p.c, table[i].m) != group) continue;
             const uint64_t tiles = ortho_tiles(table[i], kind, side);
             for (uint64_t t = 0; t < tiles; ++t) {
                 die[std::min(kDies - 1, (int)(done * kDies / all.steps))].push_back(work(i, t));
@@ -218,6 +221,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int kin
     } else {
         double load[kDies] = {};
         for (size_t i = 0; i < table.size(); ++i) {
+            if (ortho_group(p.c, table[i].m) != group) continue;
             const uint64_t tiles = ortho_tiles(table[i], kind, side), pieces = tiles >= 16 ? kDies : 1;
             for (uint64_t q = 0; q < pieces; ++q) {
                 const int to = (int)(std::min_element(load, load + kDies) - load);
@@ -271,8 +275,6 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
             o.cols = (uint32_t)cols;
             if (rows && cols) order.push_back({rows > cols ? rows : cols, i});
         }
-        // a workgroup's own start (the norm) costs about as much as a tile
-        p.run = tiles >= 4096 ? 4 : 1;
         std::sort(order.begin(), order.end(), [](const auto& x, const auto& y) {
             return x.first != y.first ? x.first > y.first : x.second < y.second;
         });
@@ -298,7 +300,7 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
     if (e == hipSuccess) e = device_info(dev, &di);
     if (e != hipSuccess) return BC_E_HIP;
     p.cus = di.cus;
-    ortho_choose(p);
+    for (int g = 0; g < 2; ++g) ortho_choose(p.group[g], g == 1, p.cus);
     // the table, then the work lists, which follow from it
     struct Ctx {
         OrthoPlan* p;
@@ -307,7 +309,9 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
         size_t at;
     } ctx{&p, s, {}, table.size() * sizeof(Ortho)};
     try {
-        for (int kind = 0; kind < kOrthoKinds; ++kind) p.workgroups[kind] = ortho_list(p, table, kind, ctx.list);
+        for (int g = 0; g < 2; ++g)
+            for (int kind = 0; kind < kOrthoKinds; ++kind)
+                p.group[g].workgroups[kind] = ortho_list(p, table, g, kind, ctx.list);
         e = with_table(table.data(), ctx.at, ctx.list.size() * sizeof(OrthoWork),
                        [](void* c, void* extra) {
                            const Ctx* x = (const Ctx*)c;
@@ -318,10 +322,11 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
                            Ctx* x = (Ctx*)c;
                            x->p->c.d = (const Ortho*)dev_table;
                            const OrthoWork* l = (const OrthoWork*)((const char*)dev_table + x->at);
-                           for (int kind = 0; kind < kOrthoKinds; ++kind) {
-                               x->p->list[kind] = l;
-                               l += x->p->workgroups[kind];
-                           }
+                           for (OrthoGroup& g : x->p->group)
+                               for (int kind = 0; kind < kOrthoKinds; ++kind) {
+                                   g.list[kind] = l;
+                                   l += g.workgroups[kind];
+                               }
                            return launch_orthogonalize(*x->p, x->s);
                        },
                        &ctx);
@@ -496,8 +501,7 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
     hipError_t e = launch_lay_outs(dtype, l, s);
     if (e == hipSuccess && dbias)
         e = launch_sum_parts(gdtype, columns, (uint32_t)((rows + 63) / 64), cols, (uint32_t)cols, dbias, nullptr, s);
-    auto product = [&](const Planes& a, const Planes& b, uint64_t m, uint64_t k, const Cut& cut, void* out, uint64_t ld,
-                       int out_dtype) {
+    auto product = [&](const Planes& a, const Planes& b, uint64_t m, uint64_t k, void* out, uint64_t ld, int out_dtype) {
         Product p{};
         p.a = a;
         p.b = b;
@@ -508,10 +512,18 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
         p.ld_out = ld;
         p.nt = streams(m * inner * dtype_bytes(out_dtype));
         p.part = part;
-        return launch_product(dtype, out_dtype, false, cut, p, s);
+        return p;
     };
-    if (e == hipSuccess && dx) e = product(dz, w_turned, rows, cols, cut_x, dx, lddx, dtype);
-    if (e == hipSuccess && dw) e = product(dz_turned, x_turned, cols, rows, cut_w, dw, lddw, gdtype);
+    const Product px = product(dz, w_turned, rows, cols, dx, lddx, dtype);
+    const Product pw = product(dz_turned, x_turned, cols, rows, dw, lddw, gdtype);
+    // (the choice depends on the shape alone: each gradient is the same, whatever else is wanted)
+    const int both = pair_tile(dtype, Shape{rows, inner, cols}, Shape{cols, inner, rows});
+    if (e == hipSuccess && dx && dw && both >= 0 && gdtype == dtype) {
+        e = launch_pair(dtype, both, px, pw, s);
+    } else {
+        if (e == hipSuccess && dx) e = launch_product(dtype, dtype, false, both >= 0 ? Cut{both, 1} : cut_x, px, s);
+        if (e == hipSuccess && dw) e = launch_product(dtype, gdtype, false, both >= 0 ? Cut{both, 1} : cut_w, pw, s);
+    }
     return finish_call(status_of(e), s, nullptr);
 }
 
@@ -519,7 +531,6 @@ int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* 
     if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
     if (!bytes || (T > 0 && (!rows || !cols))) return BC_E_NULL;
     OrthoPlan p{};
-    p.run = 1;
     uint64_t at = 0;
     for (int i = 0; i < T; ++i) {
         if (rows[i] >= kMaxDim || cols[i] >= kMaxDim) return BC_E_SIZE;

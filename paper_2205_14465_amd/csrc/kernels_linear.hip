@@ -194,12 +194,11 @@ __device__ __forceinline__ void finish_row(const Product& p, uint64_t m, uint32_
 }
 
 template <typename G, typename TO, bool forward>
-__global__ __launch_bounds__(G::kThreads) void product(Product p) {
+__device__ __forceinline__ void product_tile(const Product& p, uint32_t index, char* lds) {
     typedef typename G::T T;
-    extern __shared__ char lds[];
     const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     uint32_t tm, tn;
-    tile_of<8>(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    tile_of<8>(index, tiles_m, tiles_n, tm, tn);
     const uint32_t m0 = tm * G::kBM, n0 = tn * G::kBN;
     // this workgroup's steps along k
     const uint32_t from = (uint32_t)((uint64_t)p.steps * blockIdx.y / p.split);
@@ -217,6 +216,22 @@ __global__ __launch_bounds__(G::kThreads) void product(Product p) {
         if (part) store_vec(part + m * p.cols + n, (int)(p.cols - n), v);
         else finish_row<TO, forward>(p, m, n, v);
     });
+}
+
+// One product.  The two of a pair have a kernel of their own: choosing between
+// them at run time costs the single one its arguments in scalar registers
+// (8192x1600x6400 forward, bf16: 211 us, against 227).
+template <typename G, typename TO, bool forward>
+__global__ __launch_bounds__(G::kThreads) void product(Product p) {
+    extern __shared__ char lds[];
+    product_tile<G, TO, forward>(p, blockIdx.x, lds);
+}
+
+template <typename G, typename TO>
+__global__ __launch_bounds__(G::kThreads) void product_pair(Products all) {
+    extern __shared__ char lds[];
+    const bool second = blockIdx.x >= all.first;
+    product_tile<G, TO, false>(all.of[second], blockIdx.x - (second ? all.first : 0), lds);
 }
 
 // The result from the sums of the parts of k, added in order.
@@ -238,19 +253,36 @@ __global__ __launch_bounds__(256) void join_parts(Product p) {
     finish_row<TO, forward>(p, m, n, v);
 }
 
+template <typename G>
+uint32_t tiles_of(const Product& p) {
+    return ((p.rows + G::kBM - 1) / G::kBM) * ((p.cols + G::kBN - 1) / G::kBN);
+}
+
+// More LDS than a kernel may use by default; the attribute is per device and
+// setting it again costs next to nothing.
+template <typename G>
+hipError_t allow_lds(const void* kernel) {
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+}
+
 template <typename G, typename TO, bool forward>
 hipError_t launch_tiles(const Product& p, hipStream_t s) {
-    // more LDS than a kernel may use by default; the attribute is per device
-    // and setting it again costs next to nothing
-    hipError_t e = hipFuncSetAttribute((const void*)product<G, TO, forward>,
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+    hipError_t e = allow_lds<G>((const void*)product<G, TO, forward>);
     if (e != hipSuccess) return e;
-    const uint32_t tiles = ((p.rows + G::kBM - 1) / G::kBM) * ((p.cols + G::kBN - 1) / G::kBN);
-    hipLaunchKernelGGL((product<G, TO, forward>), dim3(tiles, p.split), dim3(G::kThreads), G::kLdsBytes, s, p);
+    hipLaunchKernelGGL((product<G, TO, forward>), dim3(tiles_of<G>(p), p.split), dim3(G::kThreads), G::kLdsBytes, s, p);
     e = hipGetLastError();
     if (e != hipSuccess || p.split == 1) return e;
     const uint64_t pieces = (uint64_t)p.rows * ((p.cols + 7) / 8);
     hipLaunchKernelGGL((join_parts<TO, forward>), dim3((uint32_t)((pieces + 255) / 256)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+template <typename G, typename TO>
+hipError_t launch_both(const Product& p, const Product& q, hipStream_t s) {
+    hipError_t e = allow_lds<G>((const void*)product_pair<G, TO>);
+    if (e != hipSuccess) return e;
+    const Products all{{p, q}, tiles_of<G>(p)};
+    hipLaunchKernelGGL((product_pair<G, TO>), dim3(all.first + tiles_of<G>(q)), dim3(G::kThreads), G::kLdsBytes, s, all);
     return hipGetLastError();
 }
 
@@ -265,17 +297,29 @@ struct TileCost {
 constexpr TileCost kCost16[3] = {{64, 64, 0.30, 0.193, 0.5}, {128, 128, 0.60, 0.53, 2.0}, {256, 256, 1.05, 1.50, 11.0}};
 constexpr TileCost kCost32[3] = {{64, 64, 0.82, 0.95, 0.5}, {128, 128, 1.86, 2.56, 1.5}, {256, 128, 3.4, 4.68, 8.7}};
 
+// The tiles of those costs.
+template <typename T> struct Tiles {
+    typedef GemmTile<T, 1, 64, 64, 64, 2, 2, 2> Small;
+    typedef GemmTile<T, 1, 128, 128, 64, 2, 4, 2> Middle;
+    typedef GemmTile<T, 1, 256, 256, 64, 2, 4, 2> Large;
+};
+template <> struct Tiles<float> {
+    typedef GemmTile<bf16_t, 3, 64, 64, 32, 2, 2, 3> Small;
+    typedef GemmTile<bf16_t, 3, 128, 128, 32, 2, 4, 3> Middle;
+    typedef GemmTile<bf16_t, 3, 256, 128, 32, 4, 2, 2> Large;
+};
+
 template <typename T, typename TO, bool forward>
 hipError_t launch_cut(int tile, const Product& p, hipStream_t s) {
-    if constexpr (PlaneOf<T>::P == 3) {
-        if (tile == 0) return launch_tiles<GemmTile<bf16_t, 3, 64, 64, 32, 2, 2, 3>, TO, forward>(p, s);
-        if (tile == 1) return launch_tiles<GemmTile<bf16_t, 3, 128, 128, 32, 2, 4, 3>, TO, forward>(p, s);
-        return launch_tiles<GemmTile<bf16_t, 3, 256, 128, 32, 4, 2, 2>, TO, forward>(p, s);
-    } else {
-        if (tile == 0) return launch_tiles<GemmTile<T, 1, 64, 64, 64, 2, 2, 2>, TO, forward>(p, s);
-        if (tile == 1) return launch_tiles<GemmTile<T, 1, 128, 128, 64, 2, 4, 2>, TO, forward>(p, s);
-        return launch_tiles<GemmTile<T, 1, 256, 256, 64, 2, 4, 2>, TO, forward>(p, s);
-    }
+    if (tile == 0) return launch_tiles<typename Tiles<T>::Small, TO, forward>(p, s);
+    if (tile == 1) return launch_tiles<typename Tiles<T>::Middle, TO, forward>(p, s);
+    return launch_tiles<typename Tiles<T>::Large, TO, forward>(p, s);
+}
+
+template <typename T>
+hipError_t launch_pair_of(int tile, const Product& p, const Product& q, hipStream_t s) {
+    if (tile == 0) return launch_both<typename Tiles<T>::Small, T>(p, q, s);
+    return launch_both<typename Tiles<T>::Middle, T>(p, q, s);
 }
 
 // ----------------------------------------------------------------- few rows
@@ -473,25 +517,29 @@ hipError_t launch_lay_outs(int dtype, LayOuts& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+constexpr double kUnits = 256.0;
+
+static double tiles_at(const TileCost& c, const Shape& s) {
+    return (double)((s.rows + c.rows - 1) / c.rows) * (double)((s.cols + c.cols - 1) / c.cols);
+}
+
 // The cheapest cut by the costs above.  Splitting k pays where tiles are fewer
 // than compute units: its sums are written and read again (about 4 TB/s from
 // the caches) and joined in a launch of their own.
-Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
-    constexpr double kUnits = 256.0;
+static Cut cheapest_cut(int dtype, const Shape& s, double& least) {
     const TileCost* cost = dtype == BC_F32 ? kCost32 : kCost16;
-    const uint64_t steps = plane_cols(k) / kPlaneCols;
+    const uint64_t steps = plane_cols(s.k) / kPlaneCols;
     Cut best{0, 1};
-    double least = 1e30;
+    least = 1e30;
     for (int i = 0; i < 3; ++i) {
-        const double tiles = (double)((rows + cost[i].rows - 1) / cost[i].rows) *
-                             (double)((cols + cost[i].cols - 1) / cost[i].cols);
+        const double tiles = tiles_at(cost[i], s);
         for (uint32_t split = 1; split <= 32 && (split == 1 || (split * 4 <= steps && tiles * split <= 512)); split *= 2) {
             const double each = (double)((steps + split - 1) / split);
             const double full = each * cost[i].full + cost[i].ends, n = tiles * split / kUnits;
             // the largest tiles come one to a unit, in whole rounds
             const double busy = i == 2 ? std::ceil(n) * full : n <= 1.0 ? 0.0 : (n + 0.5) * full;
             double t = std::max(each * cost[i].alone + cost[i].ends, busy);
-            if (split > 1) t += 4.0 + 2.0 * 4.0 * (double)split * (double)rows * (double)cols / 4e6;
+            if (split > 1) t += 4.0 + 2.0 * 4.0 * (double)split * (double)s.rows * (double)s.cols / 4e6;
             if (t < least) {
                 least = t;
                 best = Cut{i, split};
@@ -499,6 +547,34 @@ Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
         }
     }
     return best;
+}
+
+Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
+    double least;
+    return cheapest_cut(dtype, Shape{rows, cols, k}, least);
+}
+
+int pair_tile(int dtype, const Shape& a, const Shape& b) {
+    const TileCost* cost = dtype == BC_F32 ? kCost32 : kCost16;
+    double ta, tb, least = 1e30;
+    cheapest_cut(dtype, a, ta);
+    cheapest_cut(dtype, b, tb);
+    int best = -1;
+    for (int i = 0; i < 2; ++i) {  // the largest tiles fill the chip by themselves
+        double alone = 0.0, busy = 0.0, longest = 0.0;
+        for (const Shape* s : {&a, &b}) {
+            const double steps = (double)(plane_cols(s->k) / kPlaneCols), full = steps * cost[i].full + cost[i].ends;
+            alone = std::max(alone, steps * cost[i].alone + cost[i].ends);
+            busy += tiles_at(cost[i], *s) * full / kUnits;
+            longest = std::max(longest, full);
+        }
+        const double t = std::max(alone, busy + 0.5 * longest);
+        if (t < least) {
+            least = t;
+            best = i;
+        }
+    }
+    return least < ta + tb + 2.5 ? best : -1;
 }
 
 hipError_t launch_product(int dtype, int out_dtype, bool forward, const Cut& cut, const Product& given, hipStream_t s) {
@@ -518,6 +594,19 @@ hipError_t launch_product(int dtype, int out_dtype, bool forward, const Cut& cut
     }
     if (out_dtype == BC_F32) return launch_cut<bf16_t, float, false>(t, p, s);
     return launch_cut<bf16_t, bf16_t, false>(t, p, s);
+}
+
+hipError_t launch_pair(int dtype, int tile, const Product& first, const Product& second, hipStream_t s) {
+    Product p = first, q = second;
+    p.split = q.split = 1;
+    const bool no_p = p.rows == 0 || p.cols == 0, no_q = q.rows == 0 || q.cols == 0;
+    if (no_p || no_q) {
+        const hipError_t e = launch_product(dtype, dtype, false, Cut{tile, 1}, p, s);
+        return e != hipSuccess ? e : launch_product(dtype, dtype, false, Cut{tile, 1}, q, s);
+    }
+    if (dtype == BC_F32) return launch_pair_of<float>(tile, p, q, s);
+    if (dtype == BC_F16) return launch_pair_of<f16_t>(tile, p, q, s);
+    return launch_pair_of<bf16_t>(tile, p, q, s);
 }
 
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s) {

@@ -11,9 +11,12 @@
 // That is 3/2 m^2 n + 5/2 m^3 multiply-adds for two steps (symmetric results
 // half) instead of 3 m^2 n + m^3, and one pass over X instead of two.  More than
 // two steps from one Gram matrix would lose digits: A's small eigenvalues are the
-// squares of X's and grow by a^2 a step, their rounding with them.  (Gradients
-// with dominant directions, error of fp32 products as 1: two steps 1.0 to 1.1,
-// five steps 13.)
+// squares of X's and grow by a^2 a step, their rounding with them.  Measured error
+// of the result, with that of the same steps in fp32 products: 768 x 768 1.0e-6
+// (2.4e-6); under a shorter side of 64, where fp32's is 1e-6, two steps give 1.5
+// to 2 times that and results in fp32 are made step by step.  (In 64-bit sums of
+// fp32 products five steps from one Gram matrix lose a factor of 13 where a few
+// directions dominate.)
 //
 // All matrices of the call share each launch (a workgroup finds its matrix and
 // tile in a list made with the call's table), so a model's list costs 3 launches
@@ -141,56 +144,51 @@ __global__ __launch_bounds__(256) void ortho_norm(OrthoCall a) {
     if (threadIdx.x == 0) ((double*)(a.ws + o.part))[part] = total;
 }
 
-// X_0 and its transpose as planes, a workgroup up to `run` 64 x 64 tiles of U one
-// beside the other (columns and rows past the end as zeros, as far as the planes
-// go).
+// X_0 and its transpose as planes, a workgroup a 64 x 64 tile of U (columns and
+// rows past the end as zeros, as far as the planes go).
 template <typename T>
-__global__ __launch_bounds__(256) void ortho_start(OrthoCall a, uint32_t run) {
+__global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
     __shared__ double sh[4];
     __shared__ float tile[64][65];
-    const Ortho o = a.d[owner(a.d, a.T, blockIdx.x * run, [](const Ortho& x) { return x.tile0; })];
+    const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.tile0; })];
     const double mine = threadIdx.x < o.parts ? ((const double*)(a.ws + o.part))[threadIdx.x] : 0.0;
     const float scale = (float)((double)o.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
     const uint32_t across = (o.cols + 63) / 64;
     f16_t* flat = (f16_t*)(a.ws + (o.turned ? o.xt : o.x));
     f16_t* turned = (f16_t*)(a.ws + (o.turned ? o.x : o.xt));
     const uint64_t flat_ld = plane_cols(o.cols), turned_ld = plane_cols(o.rows);
-    for (uint32_t q = 0; q < run; ++q) {
-        const uint32_t t = blockIdx.x * run + q - o.tile0;
-        if (t >= across * ((o.rows + 63) / 64)) return;  // the same for the whole workgroup
-        const uint32_t r0 = t / across * 64, c0 = t % across * 64;
-        const bool whole = o.cols % 8 == 0 || c0 + 64 <= o.cols;
-        Update<T, 8> u[2];
-        const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
+    const uint32_t t = blockIdx.x - o.tile0;
+    const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+    const bool whole = o.cols % 8 == 0 || c0 + 64 <= o.cols;
+    Update<T, 8> u[2];
+    const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t r = r0 + threadIdx.x / 8 + 32 * i;
-            const int n = r < o.rows && c < o.cols ? (int)(o.cols - c) : 0;
-            if (whole) u[i].template fetch<true>(a, o, r, c, n);
-            else u[i].template fetch<false>(a, o, r, c, n);
-        }
-        if (q) __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t r = r0 + threadIdx.x / 8 + 32 * i;
+        const int n = r < o.rows && c < o.cols ? (int)(o.cols - c) : 0;
+        if (whole) u[i].template fetch<true>(a, o, r, c, n);
+        else u[i].template fetch<false>(a, o, r, c, n);
+    }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t lr = threadIdx.x / 8 + 32 * i, r = r0 + lr;
-            u[i].template make<false>(a);
-            float (&v)[8] = u[i].g;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lr = threadIdx.x / 8 + 32 * i, r = r0 + lr;
+        u[i].template make<false>(a);
+        float (&v)[8] = u[i].g;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < u[i].left ? v[j] * scale : 0.0f;  // 0 even where scale is infinite
-            if (r < o.rows) store_two(flat + r * flat_ld + c, o.rows * flat_ld, v);
+        for (int j = 0; j < 8; ++j) v[j] = j < u[i].left ? v[j] * scale : 0.0f;  // 0 even where scale is infinite
+        if (r < o.rows) store_two(flat + r * flat_ld + c, o.rows * flat_ld, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];
-        }
-        __syncthreads();
+        for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];
+    }
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t tc = threadIdx.x / 8 + 32 * i, tr = threadIdx.x % 8 * 8;
-            if (c0 + tc < o.cols) {
-                float v[8];
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t tc = threadIdx.x / 8 + 32 * i, tr = threadIdx.x % 8 * 8;
+        if (c0 + tc < o.cols) {
+            float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = tile[tr + j][tc];
-                store_two(turned + (c0 + tc) * turned_ld + r0 + tr, o.cols * turned_ld, v);
-            }
+            for (int j = 0; j < 8; ++j) v[j] = tile[tr + j][tc];
+            store_two(turned + (c0 + tc) * turned_ld + r0 + tr, o.cols * turned_ld, v);
         }
     }
 }
@@ -363,49 +361,49 @@ double time_of(const OrthoLoad& l, int side, int cus) {
 }
 
 template <typename G, int stage>
-hipError_t launch_tiles(const OrthoPlan& p, int kind, const StageArgs& a, hipStream_t s) {
+hipError_t launch_tiles(const OrthoCall& c, const OrthoGroup& g, int kind, const StageArgs& a, hipStream_t s) {
     // more LDS than a kernel may use by default; the attribute is per device
     // and setting it again costs next to nothing
     const hipError_t e = hipFuncSetAttribute((const void*)ortho_product<G, stage>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(p.workgroups[kind]), dim3(G::kThreads), G::kLdsBytes, s, p.c, a,
-                       p.list[kind]);
+    hipLaunchKernelGGL((ortho_product<G, stage>), dim3(g.workgroups[kind]), dim3(G::kThreads), G::kLdsBytes, s, c, a,
+                       g.list[kind]);
     return hipGetLastError();
 }
 
 template <int stage>
-hipError_t launch_stage(const OrthoPlan& p, const StageArgs& a, hipStream_t s) {
+hipError_t launch_stage(const OrthoPlan& p, const OrthoGroup& g, const StageArgs& a, hipStream_t s) {
     constexpr int kind = stage == kGram ? kOrthoGram : stage == kSym ? kOrthoSym : kOrthoFull;
-    // A compute unit holds two workgroups of the one or one of the other, whose
+    // A compute unit holds two workgroups of Tile64 or one of Tile64Deep, whose
     // loads run further ahead: one 768 x 768 matrix (144 tiles) 155 us against 184,
     // ResNet-50's list 1056 against 1045.
-    if (p.side[kind] == 0 && p.workgroups[kind] <= (uint32_t)p.cus) return launch_tiles<Tile64Deep, stage>(p, kind, a, s);
-    if (p.side[kind] == 0) return launch_tiles<Tile64, stage>(p, kind, a, s);
-    if (p.side[kind] == 1) return launch_tiles<Tile128, stage>(p, kind, a, s);
-    return launch_tiles<Tile256, stage>(p, kind, a, s);
+    if (g.side[kind] == 0 && g.workgroups[kind] <= (uint32_t)p.cus)
+        return launch_tiles<Tile64Deep, stage>(p.c, g, kind, a, s);
+    if (g.side[kind] == 0) return launch_tiles<Tile64, stage>(p.c, g, kind, a, s);
+    if (g.side[kind] == 1) return launch_tiles<Tile128, stage>(p.c, g, kind, a, s);
+    return launch_tiles<Tile256, stage>(p.c, g, kind, a, s);
 }
 
 template <typename T>
 hipError_t launch_start(const OrthoPlan& p, hipStream_t s) {
     hipLaunchKernelGGL(ortho_norm<T>, dim3(p.c.parts), dim3(256), 0, s, p.c);
-    hipLaunchKernelGGL(ortho_start<T>, dim3(p.c.tiles / p.run), dim3(256), 0, s, p.c, p.run);
+    hipLaunchKernelGGL(ortho_start<T>, dim3(p.c.tiles), dim3(256), 0, s, p.c);
     return hipGetLastError();
 }
 
 }  // namespace
 
-void ortho_choose(OrthoPlan& p) {
+void ortho_choose(OrthoGroup& g, bool may_pair, int cus) {
     double time[kOrthoKinds];
     for (int kind = 0; kind < kOrthoKinds; ++kind) {
-        p.side[kind] = 0;
+        g.side[kind] = 0;
         for (int i = 1; i < kOrthoSides; ++i)
-            if (time_of(p.load[kind][i], i, p.cus) < time_of(p.load[kind][p.side[kind]], p.side[kind], p.cus))
-                p.side[kind] = i;
-        time[kind] = time_of(p.load[kind][p.side[kind]], p.side[kind], p.cus);
+            if (time_of(g.load[kind][i], i, cus) < time_of(g.load[kind][g.side[kind]], g.side[kind], cus)) g.side[kind] = i;
+        time[kind] = time_of(g.load[kind][g.side[kind]], g.side[kind], cus);
     }
-    p.pairs = 4 * time[kOrthoSym] + time[kOrthoFull] + time[kOrthoGram] + time[kOrthoSym] <
-              2 * (time[kOrthoGram] + time[kOrthoSym] + time[kOrthoFull]);
+    g.pairs = may_pair && 4 * time[kOrthoSym] + time[kOrthoFull] + time[kOrthoGram] + time[kOrthoSym] <
+                              2 * (time[kOrthoGram] + time[kOrthoSym] + time[kOrthoFull]);
 }
 
 hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
@@ -413,29 +411,33 @@ hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
     hipError_t e = c.in_dtype == BC_F32   ? launch_start<float>(p, s)
                    : c.in_dtype == BC_F16 ? launch_start<f16_t>(p, s)
                                           : launch_start<bf16_t>(p, s);
-    // out = alpha U V + beta U + gamma V, each matrix with the scale of its kind
-    auto sym = [&](int u, SymScale ku, int v, SymScale kv, int out, SymScale ko, float alpha, float beta, float gamma) {
-        const float *k = c.scale, to = k[ko];
-        if (e == hipSuccess)
-            e = launch_stage<kSym>(p, StageArgs{u, v, out, 0, alpha * to / (k[ku] * k[kv]), beta * to / k[ku],
-                                                gamma * to / k[kv]}, s);
-    };
-    int from = 0;
-    for (int left = p.steps; left > 0 && e == hipSuccess;) {
-        const bool two = p.pairs && left >= 2;
-        e = launch_stage<kGram>(p, StageArgs{0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
-        sym(0, kScaleGram, 0, kScaleGram, 1, kScalePoly, c.c, c.b, 0.0f);             // 1: B
-        StageArgs next{1, 0, 0, from, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
-        if (two) {
-            sym(1, kScalePoly, 0, kScaleGram, 2, kScaleTurn, 1.0f, 0.0f, c.a);        // 2: P A
-            sym(2, kScaleTurn, 1, kScalePoly, 0, kScaleGram, 1.0f, c.a, 0.0f);        // 0: A' = P A P
-            sym(0, kScaleGram, 0, kScaleGram, 2, kScalePoly, c.c, c.b, 0.0f);         // 2: B'
-            sym(2, kScalePoly, 1, kScalePoly, 0, kScalePair, 1.0f, c.a, c.a);         // 0: B' B + a (B + B')
-            next = StageArgs{0, 0, 0, from, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
+    for (const OrthoGroup& g : p.group) {
+        if (g.workgroups[kOrthoFull] == 0) continue;
+        // out = alpha U V + beta U + gamma V, each matrix with the scale of its kind
+        auto sym = [&](int u, SymScale ku, int v, SymScale kv, int out, SymScale ko, float alpha, float beta, float gamma) {
+            const float *k = c.scale, to = k[ko];
+            if (e == hipSuccess)
+                e = launch_stage<kSym>(p, g, StageArgs{u, v, out, 0, alpha * to / (k[ku] * k[kv]), beta * to / k[ku],
+                                                       gamma * to / k[kv]}, s);
+        };
+        int from = 0;
+        for (int left = p.steps; left > 0 && e == hipSuccess;) {
+            const bool two = g.pairs && left >= 2;
+            e = launch_stage<kGram>(p, g, StageArgs{0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
+            sym(0, kScaleGram, 0, kScaleGram, 1, kScalePoly, c.c, c.b, 0.0f);             // 1: B
+            StageArgs next{1, 0, 0, from, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
+            if (two) {
+                sym(1, kScalePoly, 0, kScaleGram, 2, kScaleTurn, 1.0f, 0.0f, c.a);        // 2: P A
+                sym(2, kScaleTurn, 1, kScalePoly, 0, kScaleGram, 1.0f, c.a, 0.0f);        // 0: A' = P A P
+                sym(0, kScaleGram, 0, kScaleGram, 2, kScalePoly, c.c, c.b, 0.0f);         // 2: B'
+                sym(2, kScalePoly, 1, kScalePoly, 0, kScalePair, 1.0f, c.a, c.a);         // 0: B' B + a (B + B')
+                next = StageArgs{0, 0, 0, from, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
+            }
+            left -= two ? 2 : 1;
+            if (e == hipSuccess)
+                e = left > 0 ? launch_stage<kNext>(p, g, next, s) : launch_stage<kLast>(p, g, next, s);
+            from = 1 - from;
         }
-        left -= two ? 2 : 1;
-        if (e == hipSuccess) e = left > 0 ? launch_stage<kNext>(p, next, s) : launch_stage<kLast>(p, next, s);
-        from = 1 - from;
     }
     return e;
 }

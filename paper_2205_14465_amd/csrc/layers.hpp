@@ -95,7 +95,19 @@ Cut product_cut(int dtype, uint64_t rows, uint64_t cols, uint64_t k);
 inline uint64_t split_bytes(const Cut& c, uint64_t rows, uint64_t cols) {
     return c.split > 1 ? c.split * rows * cols * sizeof(float) : 0;
 }
+// The tile for two products of these shapes in one launch, or -1 where two
+// launches are better.
+struct Shape {
+    uint64_t rows, cols, k;
+};
+int pair_tile(int dtype, const Shape& a, const Shape& b);
+struct Products {
+    Product of[2];
+    uint32_t first;          // workgroups before the second
+};
 hipError_t launch_product(int dtype, int out_dtype, bool forward, const Cut& cut, const Product& p, hipStream_t s);
+// Both gradients' products in one launch, neither split, both out in `dtype`.
+hipError_t launch_pair(int dtype, int tile, const Product& first, const Product& second, hipStream_t s);
 
 // The forward pass for few rows: x and w as the caller has them.
 struct FewRows {
@@ -124,7 +136,7 @@ struct Ortho {
     uint32_t rows, cols, m, n;
     uint32_t turned, parts;  // parts: partial sums of squares
     uint32_t part0;          // workgroups before this matrix's: of the norm,
-    uint32_t tile0;          // of the 64 x 64 tiles of the start (a multiple of OrthoPlan::run)
+    uint32_t tile0;          // of the 64 x 64 tiles of the start
     float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
 };
@@ -161,18 +173,25 @@ enum SymScale { kScaleGram, kScalePoly, kScaleTurn, kScalePair };
 // Products of a call by what bounds their work lists: X X^T, the symmetric
 // m x m ones, and those with X's shape.
 enum OrthoKind { kOrthoGram, kOrthoSym, kOrthoFull, kOrthoKinds };
-struct OrthoPlan {
-    OrthoCall c;
-    int steps, cus;
+// Matrices that go through the products together: [1] may take two steps from
+// one Gram matrix, [0], the small ones of a call with fp32 results, keep more
+// digits without (see kernels_ortho.hip).
+constexpr uint32_t kOrthoPairs = 64;
+struct OrthoGroup {
     OrthoLoad load[kOrthoKinds][kOrthoSides];
     int side[kOrthoKinds];             // the tile side chosen (ortho_choose)
-    uint32_t workgroups[kOrthoKinds];  // and its launch's size
-    uint32_t run;                      // tiles of the start that a workgroup makes
+    uint32_t workgroups[kOrthoKinds];  // and its launch's size (0: no matrix)
     const OrthoWork* list[kOrthoKinds];
     bool pairs;                        // two steps from one Gram matrix
 };
+struct OrthoPlan {
+    OrthoCall c;
+    int steps, cus;
+    OrthoGroup group[2];               // [1]: the larger matrices
+};
+inline int ortho_group(const OrthoCall& c, uint32_t m) { return c.out_dtype != BC_F32 || m >= kOrthoPairs; }
 // Picks tile sides and the schedule from the loads.
-void ortho_choose(OrthoPlan& p);
+void ortho_choose(OrthoGroup& g, bool may_pair, int cus);
 constexpr uint32_t kOrthoParts = 256;
 hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s);
 
