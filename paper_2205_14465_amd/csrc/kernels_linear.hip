@@ -436,14 +436,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(FewRows a) {
 }
 
 // At most four rows of x: a wave a row of w, which it reads whole kilobytes at a
-// time, the loads of kFetch pieces in flight; products and sums in fp32.  (One
-// row of 6400 by 1600 columns in fp16: 6.2 us, 7.9 with four pieces in flight,
-// 10.2 by few_rows, whose hundred workgroups read 64 bytes of a row at a time.)
+// time, the loads of kFetch pieces in flight; products and sums in fp32.  Bound
+// by the weight's bytes: one row of 6400 by 1600 columns in fp16 6.1 us (3.3
+// TB/s), of 1600 by 6400 5.9, of 6400 by 6400 14.4 (5.7 TB/s, launch
+// included).  Eight pieces take 6.0, 6.1 and 14.3, sixteen 6.0, 8.7 and
+// 14.8: their registers cost more waves than they hide time.  Rows with a part
+// at their end (a branch for each piece, waited for) do best with two: 5001 by
+// 1601 6.3, with four 6.8.  few_rows, whose hundred workgroups read 64 bytes
+// of a row at a time, takes 10.2 for 6400 by 1600.
 constexpr uint32_t kDotRows = 4;
 
-template <typename T, int kRows>
+template <typename T, int kRows, bool kWhole>
 __global__ __launch_bounds__(256) void dot_rows(FewRows a) {
-    constexpr int V = kVec<T>, kFetch = kRows == 1 ? 13 : kRows == 2 ? 8 : 5;
+    constexpr int V = kVec<T>, kFetch = kWhole ? 4 : 2;
     const int lane = threadIdx.x & 63;
     const uint32_t c = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (c >= a.cols) return;
@@ -457,10 +462,10 @@ __global__ __launch_bounds__(256) void dot_rows(FewRows a) {
         for (int u = 0; u < kFetch; ++u) {
             const uint32_t k = k0 + (u * 64 + lane) * V;
             const int left = k < a.inner ? (int)(a.inner - k) : 0;
-            fw[u].load(w + (left ? k : 0), left);
+            fw[u].template load<kWhole>(w + (left ? k : 0), left);
 #pragma unroll
             for (int m = 0; m < kRows; ++m)
-                fx[u][m].load((const T*)a.x + (uint64_t)(m < (int)a.rows ? m : 0) * a.ldx + (left ? k : 0), left);
+                fx[u][m].template load<kWhole>((const T*)a.x + (uint64_t)(m < (int)a.rows ? m : 0) * a.ldx + (left ? k : 0), left);
         }
 #pragma unroll
         for (int u = 0; u < kFetch; ++u)
@@ -484,13 +489,19 @@ __global__ __launch_bounds__(256) void dot_rows(FewRows a) {
     }
 }
 
+template <typename T, int kRows>
+void launch_dot_rows(const FewRows& a, hipStream_t s) {
+    const dim3 grid((a.cols + 3) / 4), block(256);
+    if (a.inner % kVec<T> == 0) hipLaunchKernelGGL((dot_rows<T, kRows, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((dot_rows<T, kRows, false>), grid, block, 0, s, a);
+}
+
 template <typename T>
 void few_rows_launch(const FewRows& a, hipStream_t s) {
     if (a.rows <= kDotRows) {
-        const dim3 grid((a.cols + 3) / 4), block(256);
-        if (a.rows == 1) hipLaunchKernelGGL((dot_rows<T, 1>), grid, block, 0, s, a);
-        else if (a.rows == 2) hipLaunchKernelGGL((dot_rows<T, 2>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((dot_rows<T, 4>), grid, block, 0, s, a);
+        if (a.rows == 1) launch_dot_rows<T, 1>(a, s);
+        else if (a.rows == 2) launch_dot_rows<T, 2>(a, s);
+        else launch_dot_rows<T, 4>(a, s);
         return;
     }
     const dim3 grid((a.cols + 15) / 16), block(64 * kFewWaves);

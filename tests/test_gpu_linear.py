@@ -222,3 +222,35 @@ def test_wrong_tensors_raise():
     with pytest.raises(B.BytecompError) as err:
         B.bytecomp_linear_forward(x, w, None, None, "none", y, None, None)
     assert err.value.code == -7
+
+
+@pytest.mark.parametrize("rows,inner,cols", [(1, 768, 1600), (300, 700, 90), (1024, 768, 768), (65, 1745, 3585)])
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+def test_gradients_do_not_depend_on_the_others(rows, inner, cols, dtype):
+    """dx is the same bits with dw in either type, and without dw."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    rng, x, w = setup(rows, inner, cols, dtype, 0, 0, 5)
+    dy, _ = make((rows, cols), dtype, rng, 0, 0, scale=0.05)
+    ws = B.alloc_linear_workspace(x, w, backward=True)
+    got = []
+    for gd in (None, dtype, "float32"):
+        dx = torch.empty_like(x)
+        dw = None if gd is None else torch.empty_like(w, dtype=getattr(torch, gd))
+        B.bytecomp_linear_backward(dy, None, x, w, "none", dx, dw, None, ws)
+        got.append(dx)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4])
+@pytest.mark.parametrize("inner", [1, 7, 8, 511, 512, 520, 1600, 2047, 2049, 8200])
+def test_tokens(rows, inner, dtype):
+    """A few tokens: rows of the weight that end anywhere in a wave's pieces."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    rng, x, w = setup(rows, inner, 37, dtype, 0, 0, inner)
+    y = torch.empty(rows, 37, dtype=x.dtype, device="cuda")
+    B.bytecomp_linear_forward(x, w, None, None, "none", y, None, None)
+    X, W = f64(x), f64(w)
+    close(f64(y), X @ W.T, dtype, (inner + 6) * F32 * (np.abs(X) @ np.abs(W).T))
