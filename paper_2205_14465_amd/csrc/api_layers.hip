@@ -151,8 +151,12 @@ uint64_t ortho_tiles(const Ortho& o, int kind, int side) {
     const uint64_t w = 64u << side, a = (o.m + w - 1) / w, b = (o.n + w - 1) / w;
     return kind == kOrthoFull ? a * b : a * (a + 1) / 2;
 }
-double ortho_steps(const Ortho& o, int kind) {
-    return (double)plane_cols(kind == kOrthoGram ? o.n : o.m) / 32.0;
+uint64_t ortho_k(const Ortho& o, int kind) { return plane_cols(kind == kOrthoGram ? o.n : o.m); }
+double ortho_steps(const Ortho& o, int kind) { return (double)ortho_k(o, kind) / 32.0; }
+// The parts along k that leave chains of at most `chain` steps.
+uint64_t ortho_parts(const Ortho& o, int kind, double chain) {
+    return std::min((uint64_t)std::ceil(ortho_steps(o, kind) / chain),
+                    std::max<uint64_t>(1, ortho_k(o, kind) / kOrthoPart));
 }
 
 // Workspace offsets and workgroup counts of one matrix; `at` advances.
@@ -179,6 +183,10 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.part = take(8 * o.parts);
     p.c.parts += o.parts;
     p.c.tiles += (uint32_t)tiles;
+    uint64_t slots = 0;
+    for (int kind = 0; kind < kOrthoKinds; ++kind)
+        if (const uint64_t most = ortho_parts(o, kind, 1.0); most > 1) slots = std::max(slots, ortho_tiles(o, kind, 0) * most);
+    p.c.slots = (uint32_t)std::min(kOrthoSlots, p.c.slots + slots);
     for (int i = 0; i < kOrthoSides; ++i)
         for (int kind = 0; kind < kOrthoKinds; ++kind) {
             OrthoLoad& l = p.group[ortho_group(p.c, o.m)].load[kind][i];
@@ -187,6 +195,32 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
             l.steps += (double)ortho_tiles(o, kind, i) * steps;
             l.longest = std::fmax(l.longest, steps);
         }
+}
+
+// What follows the matrices in the workspace: counters and slots for tiles cut
+// along k.
+void plan_meeting(uint64_t& at, OrthoPlan& p) {
+    p.c.meet = at;
+    if (p.c.slots) at += align256(kOrthoSlots * sizeof(uint32_t) + p.c.slots * kOrthoSlotBytes);
+}
+
+// How long a 64-wide tile's chain along k may be: about a compute unit's mean
+// share of the launch (which makes at most twice as many parts as there are
+// units), and where there are fewer tiles than units no shorter than one
+// workgroup a unit allows.  (4781 x 188 in bfloat16 141 us against 184 uncut, three
+// of 512 x 4608 with one of 2048 x 512 356 against 397; parts of 256 take 155 and
+// 412, and two parts for 136 tiles, more than a workgroup a unit, 314 against 258.)
+double ortho_chain(const OrthoPlan& p, const std::vector<Ortho>& table, int group, int kind) {
+    const OrthoLoad& l = p.group[group].load[kind][0];
+    double chain = std::fmax(l.steps / p.cus, kOrthoPart / 32.0);
+    if (l.tiles > p.cus) return chain;
+    for (; chain < l.longest; chain *= 1.1) {
+        uint64_t n = 0;
+        for (const Ortho& o : table)
+            if (ortho_group(p.c, o.m) == group) n += ortho_tiles(o, kind, 0) * ortho_parts(o, kind, chain);
+        if (n <= (uint64_t)p.cus) break;
+    }
+    return chain;
 }
 
 // The workgroups of a launch, dealt to the eight compute dies in turn, each
@@ -200,21 +234,33 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int gro
                     std::vector<OrthoWork>& list) {
     constexpr int kDies = 8;
     std::vector<OrthoWork> die[kDies];
-    auto work = [&](size_t i, uint64_t tile) {
-        const Ortho& o = table[i];
-        return OrthoWork{(uint32_t)i, (uint32_t)tile, o.m, o.n, (uint32_t)(o.x >> 8), (uint32_t)(o.xt >> 8),
-                         (uint32_t)(o.sym >> 8), o.x_scale};
-    };
     const OrthoGroup& g = p.group[group];
     const int side = g.side[kind];
     const OrthoLoad& all = g.load[kind][side];
+    uint32_t slots = 0, met = 0;
+    // the parts of a tile follow each other on one die
+    auto parts_of = [&](const Ortho& o) -> uint32_t {
+        if (side != 0) return 1;
+        const uint64_t parts = ortho_parts(o, kind, g.chain[kind]);
+        return slots + parts * ortho_tiles(o, kind, 0) <= p.c.slots ? (uint32_t)parts : 1;
+    };
+    auto push = [&](std::vector<OrthoWork>& to, size_t i, uint64_t tile, uint32_t parts) {
+        const Ortho& o = table[i];
+        for (uint32_t q = 0; q < parts; ++q)
+            to.push_back(OrthoWork{(uint32_t)i, (uint32_t)tile, o.m, o.n, (uint32_t)(o.x >> 8), (uint32_t)(o.xt >> 8),
+                                   (uint32_t)(o.sym >> 8), o.x_scale, q, parts, slots, met});
+        if (parts == 1) return;
+        slots += parts;
+        met += 1;
+    };
     if (all.longest * all.tiles <= 1.25 * all.steps) {
         double done = 0.0;
         for (size_t i = 0; i < table.size(); ++i) {
             if (ortho_group(p.c, table[i].m) != group) continue;
             const uint64_t tiles = ortho_tiles(table[i], kind, side);
+            const uint32_t parts = parts_of(table[i]);
             for (uint64_t t = 0; t < tiles; ++t) {
-                die[std::min(kDies - 1, (int)(done * kDies / all.steps))].push_back(work(i, t));
+                push(die[std::min(kDies - 1, (int)(done * kDies / all.steps))], i, t, parts);
                 done += ortho_steps(table[i], kind);
             }
         }
@@ -222,11 +268,13 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int gro
         double load[kDies] = {};
         for (size_t i = 0; i < table.size(); ++i) {
             if (ortho_group(p.c, table[i].m) != group) continue;
-            const uint64_t tiles = ortho_tiles(table[i], kind, side), pieces = tiles >= 16 ? kDies : 1;
+            const uint64_t tiles = ortho_tiles(table[i], kind, side);
+            const uint32_t parts = parts_of(table[i]);
+            const uint64_t pieces = tiles * parts >= 16 ? kDies : 1;
             for (uint64_t q = 0; q < pieces; ++q) {
                 const int to = (int)(std::min_element(load, load + kDies) - load);
                 const uint64_t lo = tiles * q / pieces, hi = tiles * (q + 1) / pieces;
-                for (uint64_t t = lo; t < hi; ++t) die[to].push_back(work(i, t));
+                for (uint64_t t = lo; t < hi; ++t) push(die[to], i, t, parts);
                 load[to] += (double)(hi - lo) * ortho_steps(table[i], kind);
             }
         }
@@ -234,7 +282,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int gro
     size_t longest = 0;
     for (const auto& d : die) longest = std::max(longest, d.size());
     for (size_t q = 0; q < longest; ++q)
-        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0, 0, 0, 0, 0, 0, 0.0f});
+        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0, 0, 0, 0, 0, 0, 0.0f, 0, 1, 0, 0});
     return (uint32_t)(kDies * longest);
 }
 
@@ -289,6 +337,7 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
         return BC_E_SIZE;
     }
     if (table.empty()) return BC_OK;
+    plan_meeting(at, p);
     if (at >= (1ull << 40)) return BC_E_SIZE;  // offsets in 256 bytes stay within 32 bits
     if (!ws || ws_bytes < at) return BC_E_WORKSPACE;
     if ((uintptr_t)ws & 255) return BC_E_ALIGN;
@@ -300,7 +349,10 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
     if (e == hipSuccess) e = device_info(dev, &di);
     if (e != hipSuccess) return BC_E_HIP;
     p.cus = di.cus;
-    for (int g = 0; g < 2; ++g) ortho_choose(p.group[g], g == 1, p.cus);
+    for (int g = 0; g < 2; ++g) {
+        for (int kind = 0; kind < kOrthoKinds; ++kind) p.group[g].chain[kind] = ortho_chain(p, table, g, kind);
+        ortho_choose(p.group[g], g == 1, p.cus);
+    }
     // the table, then the work lists, which follow from it
     struct Ctx {
         OrthoPlan* p;
@@ -537,6 +589,7 @@ int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* 
         Ortho o{};
         plan_matrix(rows[i], cols[i], at, p, o);
     }
+    plan_meeting(at, p);
     *bytes = (size_t)at;
     return BC_OK;
 }

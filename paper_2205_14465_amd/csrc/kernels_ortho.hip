@@ -150,6 +150,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
     __shared__ double sh[4];
     __shared__ float tile[64][65];
+    if (blockIdx.x == 0)  // nobody has met yet
+        for (uint32_t i = threadIdx.x; i < a.slots; i += 256) ((uint32_t*)(a.ws + a.meet))[i] = 0;
     const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.tile0; })];
     const double mine = threadIdx.x < o.parts ? ((const double*)(a.ws + o.part))[threadIdx.x] : 0.0;
     const float scale = (float)((double)o.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
@@ -265,6 +267,56 @@ struct NextEpilogue {
     }
 };
 
+// The sums of a tile's parts along k: each workgroup leaves its own in its slot
+// and counts itself; the last one gets all of them, added in the order of the
+// parts, and goes on (true).  Nobody waits.
+template <typename G>
+__device__ __forceinline__ bool meet(G& g, const OrthoCall& a, const OrthoWork& w, char* lds) {
+    constexpr uint32_t kTile = G::kBM * G::kBN;
+    static_assert(kTile * sizeof(float) == kOrthoSlotBytes, "a slot holds a tile");
+    uint32_t* met = (uint32_t*)(a.ws + a.meet) + w.met;
+    float* sums = (float*)(a.ws + a.meet + kOrthoSlots * sizeof(uint32_t)) + (uint64_t)w.sums * kTile + threadIdx.x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        __hip_atomic_store(sums + w.part * kTile + r * G::kThreads, g.acc[0][0][r], __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the sums have left for where every die sees them
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool last = __hip_atomic_fetch_add(met, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == w.parts;
+        if (last) __hip_atomic_store(met, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+        *(uint32_t*)lds = last;
+    }
+    __syncthreads();
+    const bool last = *(const uint32_t*)lds != 0;
+    __syncthreads();  // the epilogue writes LDS
+    if (!last) return false;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+#pragma unroll
+    for (int r = 0; r < 16; ++r) g.acc[0][0][r] = sums[r * G::kThreads];
+    for (uint32_t q = 1; q < w.parts; ++q)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g.acc[0][0][r] += sums[q * kTile + r * G::kThreads];
+    return true;
+}
+
+// The product's tile, or this workgroup's part of it; whether to go on with it.
+template <typename G>
+__device__ __forceinline__ bool multiply(G& g, const OrthoCall& a, const OrthoWork& w, Operand<f16_t> u,
+                                         Operand<f16_t> v, uint64_t k, char* lds) {
+    const uint32_t steps = (uint32_t)(k / G::kBK);
+    if constexpr (G::kBM == 64) {
+        const uint32_t from = steps * w.part / w.parts, to = steps * (w.part + 1) / w.parts;
+        u.p += from * G::kBK;
+        v.p += from * G::kBK;
+        g.multiply(u, v, (int)(to - from), lds);
+        return w.parts == 1 || meet(g, a, w, lds);
+    } else {
+        g.multiply(u, v, (int)steps, lds);
+        return true;
+    }
+}
+
 template <typename G, int stage>
 __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageArgs s,
                                                              const OrthoWork* __restrict__ list) {
@@ -301,18 +353,18 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         return Operand<f16_t>{p + at * ld, (uint32_t)ld, rows * ld, rows - at};
     };
     if constexpr (stage == kGram) {
-        g.multiply(rows_of(x, np, m, m0), rows_of(x, np, m, n0), (int)(np / G::kBK), lds);
+        if (!multiply(g, a, work, rows_of(x, np, m, m0), rows_of(x, np, m, n0), np, lds)) return;
         const SymmetricEpilogue e{sym(s.out), nullptr, nullptr, mp, m * mp, m, m0, n0,
                                   s.alpha / (work.x_scale * work.x_scale), 0.0f, 0.0f};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kSym) {
-        g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(sym(s.v), mp, m, n0), (int)(mp / G::kBK), lds);
+        if (!multiply(g, a, work, rows_of(sym(s.u), mp, m, m0), rows_of(sym(s.v), mp, m, n0), mp, lds)) return;
         const SymmetricEpilogue e{sym(s.out), s.beta != 0.0f ? sym(s.u) : nullptr,
                                   s.gamma != 0.0f ? sym(s.v) : nullptr, mp, m * mp, m, m0, n0,
                                   s.alpha, s.beta, s.gamma};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kNext) {
-        g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(xt[s.from], mp, n, n0), (int)(mp / G::kBK), lds);
+        if (!multiply(g, a, work, rows_of(sym(s.u), mp, m, m0), rows_of(xt[s.from], mp, n, n0), mp, lds)) return;
         const NextEpilogue e{x, xt[1 - s.from], np, mp, m, n, m0, n0, s.alpha, s.beta};
         g.finish_both_ways(lds, e);
     } else {
@@ -320,8 +372,9 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         const Ortho o = a.d[work.matrix];
         const f16_t* old = tall ? xt[s.from] : x;
         const uint64_t old_ld = tall ? mp : np, old_plane = tall ? n * mp : m * np;
-        if (tall) g.multiply(rows_of(old, mp, n, m0), rows_of(sym(s.u), mp, m, n0), (int)(mp / G::kBK), lds);
-        else g.multiply(rows_of(sym(s.u), mp, m, m0), rows_of(xt[s.from], mp, n, n0), (int)(mp / G::kBK), lds);
+        const Operand<f16_t> u = tall ? rows_of(old, mp, n, m0) : rows_of(sym(s.u), mp, m, m0);
+        const Operand<f16_t> v = tall ? rows_of(sym(s.u), mp, m, n0) : rows_of(xt[s.from], mp, n, n0);
+        if (!multiply(g, a, work, u, v, mp, lds)) return;
         const float inv = 1.0f / work.x_scale;
         g.finish(lds, [&](int row, int col, float (&v)[8]) {
             const uint64_t r = m0 + row;
@@ -352,12 +405,14 @@ typedef GemmTile<f16_t, 2, 128, 128, 64, 2, 4, 2> Tile128;
 typedef GemmTile<f16_t, 2, 256, 256, 32, 2, 4, 2> Tile256;
 constexpr double kAlone[kOrthoSides] = {0.32, 0.50, 1.55}, kFull[kOrthoSides] = {0.21, 0.63, 2.2};
 constexpr double kEnds[kOrthoSides] = {1.5, 6.0, 40.0};
-constexpr double kLaunch = 3.0;
+constexpr double kLaunch = 3.0, kMeet = 2.5;
 
-double time_of(const OrthoLoad& l, int side, int cus) {
-    const double alone = l.longest * kAlone[side] + kEnds[side];
+double time_of(const OrthoLoad& l, int side, double chain, int cus) {
+    const bool cut = side == 0 && l.longest > chain;
+    const double longest = cut ? chain : l.longest, ends = kEnds[side] + (cut ? kMeet : 0.0);
+    const double alone = longest * kAlone[side] + ends;
     const double full = (l.steps * kFull[side] + l.tiles * kEnds[side]) / cus;
-    return kLaunch + std::max(alone, full + 0.5 * (l.longest * kFull[side] + kEnds[side]));
+    return kLaunch + std::max(alone, full + 0.5 * (longest * kFull[side] + ends));
 }
 
 template <typename G, int stage>
@@ -397,10 +452,12 @@ hipError_t launch_start(const OrthoPlan& p, hipStream_t s) {
 void ortho_choose(OrthoGroup& g, bool may_pair, int cus) {
     double time[kOrthoKinds];
     for (int kind = 0; kind < kOrthoKinds; ++kind) {
-        g.side[kind] = 0;
-        for (int i = 1; i < kOrthoSides; ++i)
-            if (time_of(g.load[kind][i], i, cus) < time_of(g.load[kind][g.side[kind]], g.side[kind], cus)) g.side[kind] = i;
-        time[kind] = time_of(g.load[kind][g.side[kind]], g.side[kind], cus);
+        for (int i = 0; i < kOrthoSides; ++i) {
+            const double t = time_of(g.load[kind][i], i, g.chain[kind], cus);
+            if (i > 0 && !(t < time[kind])) continue;
+            g.side[kind] = i;
+            time[kind] = t;
+        }
     }
     g.pairs = may_pair && 4 * time[kOrthoSym] + time[kOrthoFull] + time[kOrthoGram] + time[kOrthoSym] <
                               2 * (time[kOrthoGram] + time[kOrthoSym] + time[kOrthoFull]);

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "elem.hpp"
 
 namespace bc {
@@ -144,13 +146,16 @@ static_assert(sizeof(Ortho) == 8 * 10 + 4 * 10, "Ortho layout");
 
 // What a workgroup of a product launch computes: a tile of a matrix, or
 // nothing (matrix kOrthoIdle).  It carries what all but the last product need of
-// the matrix, so that a workgroup's operands are one load from its start.
+// the matrix, so that a workgroup's operands are one load from its start.  A
+// tile of long products is cut along k into parts: a workgroup each, whose sums
+// lie from slot `sums` on, and the last to count itself at `met` adds them.
 struct OrthoWork {
     uint32_t matrix, tile, m, n;
     uint32_t x, xt, sym;     // offsets in the workspace, in 256 bytes
     float x_scale;
+    uint32_t part, parts, sums, met;
 };
-static_assert(sizeof(OrthoWork) == 32, "OrthoWork layout");
+static_assert(sizeof(OrthoWork) == 48, "OrthoWork layout");
 constexpr uint32_t kOrthoIdle = 0xFFFFFFFFu;
 
 // The work of a launch with one tile side: tiles, and steps of 32 along k, in
@@ -164,6 +169,8 @@ struct OrthoCall {
     int T;
     int in_dtype, out_dtype;
     uint32_t parts, tiles;   // workgroups of the norm and of the start
+    uint32_t slots;          // for sums of tiles cut along k: kOrthoSlots at most,
+    uint64_t meet;           // from here on in the workspace, after as many counters
     float a, b, c, eps;
     float scale[4];          // of the symmetric matrices by what they hold (SymScale)
     bool muon, nesterov;
@@ -177,8 +184,12 @@ enum OrthoKind { kOrthoGram, kOrthoSym, kOrthoFull, kOrthoKinds };
 // one Gram matrix, [0], the small ones of a call with fp32 results, keep more
 // digits without (see kernels_ortho.hip).
 constexpr uint32_t kOrthoPairs = 64;
+// Tiles 64 wide may be cut along k into parts of at least kOrthoPart, whose sums
+// meet in kOrthoSlots slots at most.
+constexpr uint64_t kOrthoPart = 512, kOrthoSlots = 512, kOrthoSlotBytes = 64 * 64 * sizeof(float);
 struct OrthoGroup {
     OrthoLoad load[kOrthoKinds][kOrthoSides];
+    double chain[kOrthoKinds];         // the most steps of 32 that a 64-wide tile is left with
     int side[kOrthoKinds];             // the tile side chosen (ortho_choose)
     uint32_t workgroups[kOrthoKinds];  // and its launch's size (0: no matrix)
     const OrthoWork* list[kOrthoKinds];

@@ -196,3 +196,24 @@ def test_other_stream_and_wrong_tensors():
                 lambda: B.MuonCall([u], [u], [u.half()], ws), lambda: B.MuonCall([u], [u], [a], ws, scales=[])):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("shapes", [[(70, 6011)], [(4099, 180)], [(33, 1023)], [(17, 5000), (150, 150)],
+                                    [(512, 4608)] * 3 + [(2048, 512)]])
+def test_long_axes(shapes):
+    """Few tiles and many steps along the longer axis: the result is the formula's
+    and every run's the same, whichever workgroup comes last."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    rng = np.random.default_rng(21)
+    ups = [torch.from_numpy(gradient(s, rng, "uneven")).float().cuda() for s in shapes]
+    outs = [torch.empty_like(u) for u in ups]
+    ws = B.alloc_orthogonalize_workspace(shapes)
+    ws.fill_(255)
+    B.bytecomp_orthogonalize(ups, outs, ws)
+    for u, o in zip(ups, outs):
+        near(f64(o), f64(u))
+    for _ in range(3):
+        again = [torch.empty_like(u) for u in ups]
+        B.bytecomp_orthogonalize(ups, again, ws)
+        assert all(torch.equal(a, b) for a, b in zip(again, outs))
