@@ -58,7 +58,7 @@ size_t sums_bytes(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
 
 size_t linear_ws(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, bool backward) {
     if (!backward)
-        return rows <= kFewRows ? 0
+        return rows <= few_rows_most(dtype) ? 0
                                 : planes_bytes(dtype, rows, inner) + planes_bytes(dtype, cols, inner) +
                                       sums_bytes(dtype, rows, cols, inner);
     return planes_bytes(dtype, rows, cols) + planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows) +
@@ -462,7 +462,7 @@ int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t c
         misaligned(y, dtype) || misaligned(z, dtype) || ((uintptr_t)ws & 15))
         return BC_E_ALIGN;
     hipStream_t s = (hipStream_t)stream;
-    if (rows <= kFewRows) {
+    if (rows <= few_rows_most(dtype)) {
         const FewRows a{x, w, bias, residual, y, z, ldx, ldw, ld_residual, ldy, ldz, (uint32_t)rows, (uint32_t)inner,
                         (uint32_t)cols, act};
         return finish_call(status_of(launch_few_rows(dtype, a, s)), s, nullptr);

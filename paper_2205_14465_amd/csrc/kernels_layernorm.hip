@@ -52,9 +52,11 @@ __device__ __forceinline__ void load_weight(const void* w, uint32_t c, int left,
 
 // ---------------------------------------------------------------- forward
 // kGroup threads a row (64: four rows a workgroup, kLnBlock: one), kPer
-// vectors a thread; kWhole: rows are whole vectors.  (Rows following each other with their weights in registers,
-// as in the backward pass, measured 14.3 us against 13.5 at 8192 x 1600: the
-// registers cost more waves than the weights cost loads.)
+// vectors a thread; kWhole: rows are whole vectors, loaded without a branch for
+// parts (8192 x 1600 in bfloat16 11.8 us, 4.4 TB/s, against 13.7 with it).  One
+// token of 768: 3.9 us, the launch.  Rows following each other with their
+// weights in registers, as in the backward pass, are 6% slower: the registers
+// cost more waves than the weights cost loads.
 template <typename T, typename WT, int kGroup, int kPer, bool kWhole>
 __global__ __launch_bounds__(kLnBlock) void ln_forward(LnForward a) {
     constexpr int V = kVec<T>;
@@ -162,6 +164,9 @@ __global__ __launch_bounds__(kWideBlock) void ln_forward_wide(LnForward a) {
 // j, j + kGroup, ...  The next row's loads are in flight under the arithmetic of
 // the last; weights stay in registers.  The waves of a workgroup then meet in
 // LDS, and the workgroup's sums go to part[block] (cols of dw, then cols of db).
+// Bound by memory and by the few waves that its registers leave to hide it:
+// 8192 x 1600 in fp16 20 us, 3.9 TB/s, and 4 more for sum_parts (33 in all without
+// the loads ahead); 1237 x 1001 in fp32 7 and 3.
 template <typename T, typename WT, int kGroup, int kPer, bool kWhole>
 __global__ __launch_bounds__(kLnBlock) void ln_backward(LnBackward a) {
     constexpr int V = kVec<T>;
@@ -388,7 +393,12 @@ hipError_t launch_sum_parts(int dtype, const float* part, uint32_t parts, uint64
 }
 
 // Rows of up to 64 * kPer vectors go to a wave, of up to kLnBlock * kPer to a
-// workgroup, longer ones to the wide kernels.
+// workgroup, longer ones to the wide kernels.  Measured in bfloat16, us:
+//   forward   8192 x 2048  wave 12.9, workgroup 14.0;  8192 x 4096  22.7, 22.4;
+//             512 x 4096 (fp16)  6.3, 4.2;  2048 x 16384  workgroup 23.7, wide 30.0
+//   backward  8192 x 2048  wave 23.6, workgroup 30.5;  8192 x 4096  66.5, 49.6;
+//             2048 x 8192  workgroup 33.1, wide 54.4;  2048 x 16384  90.7, 89.2,
+//             500 x 12001 (fp16)  48.4, 33.6;  fp32, 4096 x 8192  103, 133
 template <typename T, typename WT, bool kWhole>
 static void ln_forward_launch(const LnForward& a, hipStream_t s) {
     const uint32_t vecs = (a.cols + kVec<T> - 1) / kVec<T>;
@@ -402,6 +412,11 @@ static void ln_forward_launch(const LnForward& a, hipStream_t s) {
     else hipLaunchKernelGGL((ln_forward_wide<T, WT>), rows, dim3(kWideBlock), 0, s, a);
 }
 
+// Vectors of the longest rows that the backward pass holds in registers: twice
+// as many where two arrays of fp32 need no widening and no masks.
+template <typename T>
+static uint32_t ln_longest(uint32_t cols) { return sizeof(T) == 4 && cols % kVec<T> == 0 ? 2048 : 1024; }
+
 template <typename T, typename WT, bool kWhole>
 static void ln_backward_launch(const LnBackward& a, hipStream_t s) {
     const uint32_t vecs = (a.cols + kVec<T> - 1) / kVec<T>;
@@ -411,17 +426,23 @@ static void ln_backward_launch(const LnBackward& a, hipStream_t s) {
     else if (vecs <= 256) hipLaunchKernelGGL((ln_backward<T, WT, 64, 4, kWhole>), grid, block, 0, s, a);
     else if (vecs <= 512) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 2, kWhole>), grid, block, 0, s, a);
     else if (vecs <= 1024) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 4, kWhole>), grid, block, 0, s, a);
-    else {
+    else if (vecs <= ln_longest<T>(a.cols)) {
+        if constexpr (sizeof(T) == 4 && kWhole) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 8, true>), grid, block, 0, s, a);
+    } else {
         if (a.dx) hipLaunchKernelGGL((ln_backward_wide<T, WT>), dim3((uint32_t)a.rows), dim3(kWideBlock), 0, s, a);
         if (a.part)
             hipLaunchKernelGGL((ln_column_sums<T>), dim3((vecs + kLnBlock - 1) / kLnBlock, a.parts), block, 0, s, a);
     }
 }
 
+// Workgroups that leave partial sums of columns.  (The wide kernel's take eight
+// rows each at least: 500 x 12001 in fp16 33.6 us, with four the same, with 32
+// rows 61.5.)
 uint32_t ln_parts(uint64_t rows, uint32_t cols, int dtype) {
     const uint32_t V = dtype == BC_F32 ? 4 : 8, vecs = (cols + V - 1) / V;
-    const uint64_t units = vecs <= 256 ? (rows + kLnWaves - 1) / kLnWaves : vecs <= 1024 ? rows : (rows + 31) / 32;
-    const uint64_t most = vecs <= 1024 ? 512 : 64;
+    const bool held = vecs <= (dtype == BC_F32 ? ln_longest<float>(cols) : ln_longest<f16_t>(cols));
+    const uint64_t units = vecs <= 256 ? (rows + kLnWaves - 1) / kLnWaves : held ? rows : (rows + 7) / 8;
+    const uint64_t most = held ? 512 : 64;
     return (uint32_t)(units < most ? units : most);
 }
 

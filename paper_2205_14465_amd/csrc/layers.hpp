@@ -119,7 +119,11 @@ struct FewRows {
     uint32_t rows, inner, cols;
     int act;
 };
-constexpr uint32_t kFewRows = 64;
+// Up to so many rows.  (32 rows of 768 by 768 in fp16 4.2 us, by tiles 6.1; of
+// 1600 by 6400 11.3, 14.6; of 6400 by 1600 19.1, 13.8; 64 rows 5.9, 17.5 and 30.7
+// against 6.2, 14.8 and 14.1.  fp32, which tiles take as planes: 64 rows of 4096
+// by 4096 38.7 us against 61.2.)
+inline uint32_t few_rows_most(int dtype) { return dtype == BC_F32 ? 64 : 32; }
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s);
 
 // -------------------------------------------------- orthogonalised updates
