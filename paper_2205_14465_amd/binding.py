@@ -727,8 +727,8 @@ def _activation(name):
 class LinearCall(_Call):
     """bytecomp_linear_forward: y = act(x w^T + bias) + residual, z the sum
     before the activation; bias, residual and z may be None.  activation: a
-    key of ACTIVATION; ws from alloc_linear_workspace (None where that is
-    empty: up to 32 rows, of fp32 64)."""
+    key of ACTIVATION; ws from alloc_linear_workspace (None for at most 64
+    rows)."""
 
     def __init__(self, x, w, bias, residual, activation, y, z=None, ws=None, stream=None):
         rows, inner = x.shape

@@ -58,7 +58,7 @@ size_t sums_bytes(int dtype, uint64_t rows, uint64_t cols, uint64_t k) {
 
 size_t linear_ws(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, bool backward) {
     if (!backward)
-        return rows <= few_rows_most(dtype) ? 0
+        return rows <= kFewRows ? 0
                                 : planes_bytes(dtype, rows, inner) + planes_bytes(dtype, cols, inner) +
                                       sums_bytes(dtype, rows, cols, inner);
     return planes_bytes(dtype, rows, cols) + planes_bytes(dtype, cols, rows) + planes_bytes(dtype, inner, rows) +
@@ -183,9 +183,13 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.part = take(8 * o.parts);
     p.c.parts += o.parts;
     p.c.tiles += (uint32_t)tiles;
+    // (a matrix of as many tiles as there are units is not cut: its chain is no
+    // longer than the mean)
     uint64_t slots = 0;
-    for (int kind = 0; kind < kOrthoKinds; ++kind)
-        if (const uint64_t most = ortho_parts(o, kind, 1.0); most > 1) slots = std::max(slots, ortho_tiles(o, kind, 0) * most);
+    for (int kind = 0; kind < kOrthoKinds; ++kind) {
+        const uint64_t most = ortho_parts(o, kind, 1.0), n = ortho_tiles(o, kind, 0);
+        if (most > 1 && n < kOrthoSlots / 2) slots = std::max(slots, n * most);
+    }
     p.c.slots = (uint32_t)std::min(kOrthoSlots, p.c.slots + slots);
     for (int i = 0; i < kOrthoSides; ++i)
         for (int kind = 0; kind < kOrthoKinds; ++kind) {
@@ -462,7 +466,7 @@ int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t c
         misaligned(y, dtype) || misaligned(z, dtype) || ((uintptr_t)ws & 15))
         return BC_E_ALIGN;
     hipStream_t s = (hipStream_t)stream;
-    if (rows <= few_rows_most(dtype)) {
+    if (rows <= kFewRows) {
         const FewRows a{x, w, bias, residual, y, z, ldx, ldw, ld_residual, ldy, ldz, (uint32_t)rows, (uint32_t)inner,
                         (uint32_t)cols, act};
         return finish_call(status_of(launch_few_rows(dtype, a, s)), s, nullptr);

@@ -329,7 +329,7 @@ hipError_t launch_pair_of(int tile, const Product& p, const Product& q, hipStrea
 }
 
 // ----------------------------------------------------------------- few rows
-// Up to few_rows_most rows of x: the weight's bytes are the cost, and every
+// At most kFewRows rows of x: the weight's bytes are the cost, and every
 // workgroup reads its 16 rows of w once, straight into the first operand of the
 // 16x16x32 matrix instruction; its waves share out the inner axis and meet in
 // LDS.  The second operand holds kGroups groups of 16 rows of x.  Bound by the
@@ -514,8 +514,8 @@ void few_rows_launch(const FewRows& a, hipStream_t s) {
     }
     const dim3 grid((a.cols + 15) / 16), block(64 * kFewWaves);
     if (a.rows <= 16) hipLaunchKernelGGL((few_rows<T, 1>), grid, block, 0, s, a);
-    else if (sizeof(T) == 2 || a.rows <= 32) hipLaunchKernelGGL((few_rows<T, 2>), grid, block, 0, s, a);
-    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_rows<T, 4>), grid, block, 0, s, a);
+    else if (a.rows <= 32) hipLaunchKernelGGL((few_rows<T, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_rows<T, 4>), grid, block, 0, s, a);
 }
 
 }  // namespace

@@ -119,11 +119,12 @@ struct FewRows {
     uint32_t rows, inner, cols;
     int act;
 };
-// Up to so many rows.  (32 rows of 768 by 768 in fp16 4.2 us, by tiles 6.1; of
-// 1600 by 6400 11.3, 14.6; of 6400 by 1600 19.1, 13.8; 64 rows 5.9, 17.5 and 30.7
-// against 6.2, 14.8 and 14.1.  fp32, which tiles take as planes: 64 rows of 4096
-// by 4096 38.7 us against 61.2.)
-inline uint32_t few_rows_most(int dtype) { return dtype == BC_F32 ? 64 : 32; }
+// Up to so many rows, which then need no workspace.  (64 rows of 4096 by 4096 in
+// fp32 38.7 us, by tiles, which take fp32 as planes, 61.2; in fp16 32 rows of 768
+// by 768 4.2 and 6.1, of 1600 by 6400 11.3 and 14.6; 64 rows 5.9 and 6.2, 17.5 and
+// 14.8, but of 6400 by 1600 30.7 and 14.1, with tiles cut along k and 3 MB of
+// workspace: a small batch without one is worth that to its caller.)
+constexpr uint32_t kFewRows = 64;
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t s);
 
 // -------------------------------------------------- orthogonalised updates
