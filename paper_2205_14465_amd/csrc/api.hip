@@ -66,12 +66,14 @@ uint64_t count_of(int kind, uint64_t n, uint64_t ppm) {
 size_t align256(size_t x) { return (x + 255u) & ~(size_t)255u; }
 
 // ----------------------------------------------------- descriptor cache
-// Device copies of descriptor tables, keyed by their exact bytes and the
-// device; a hit costs no copy.  Entries are uploaded from pinned host
-// memory on the calling stream; other streams wait on the upload event.
+// Device copies of descriptor tables, keyed by their exact bytes, the length
+// of what was derived from them, and the device; a hit costs no copy.
+// Entries are uploaded from pinned host memory on the calling stream; other
+// streams wait on the upload event.
 struct Entry {
     int device = -1;
     std::vector<unsigned char> key;
+    size_t extra = 0;
     void* dev = nullptr;
     void* pinned = nullptr;
     size_t cap = 0;
@@ -96,7 +98,8 @@ hipError_t cache_get(const void* bytes, size_t len, size_t extra, Fill fill, hip
     if (e != hipSuccess) return e;
     Entry* victim = nullptr;
     for (Entry& en : g_cache) {
-        if (en.device == dev && en.key.size() == len && std::memcmp(en.key.data(), bytes, len) == 0) {
+        if (en.device == dev && en.key.size() == len && en.extra == extra &&
+            std::memcmp(en.key.data(), bytes, len) == 0) {
             if (en.upload_stream != s) {
                 e = hipStreamWaitEvent(s, en.ready, 0);
                 if (e != hipSuccess) return e;
@@ -139,6 +142,7 @@ hipError_t cache_get(const void* bytes, size_t len, size_t extra, Fill fill, hip
     std::memcpy(en.pinned, bytes, len);
     fill((unsigned char*)en.pinned + len);
     en.key.assign((const unsigned char*)bytes, (const unsigned char*)bytes + len);
+    en.extra = extra;
     e = hipMemcpyAsync(en.dev, en.pinned, total, hipMemcpyHostToDevice, s);
     if (e == hipSuccess) e = hipEventRecord(en.ready, s);
     if (e != hipSuccess) { en.key.clear(); return e; }

@@ -171,6 +171,7 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     o.turned = rows > cols;
     o.m = o.turned ? o.cols : o.rows;
     o.n = o.turned ? o.rows : o.cols;
+    o.group = ortho_group(p.c, o.m);
     o.part0 = p.c.parts;
     o.tile0 = p.c.tiles;
     if (rows == 0 || cols == 0) return;
@@ -193,7 +194,7 @@ void plan_matrix(uint64_t rows, uint64_t cols, uint64_t& at, OrthoPlan& p, Ortho
     p.c.slots = (uint32_t)std::min(kOrthoSlots, p.c.slots + slots);
     for (int i = 0; i < kOrthoSides; ++i)
         for (int kind = 0; kind < kOrthoKinds; ++kind) {
-            OrthoLoad& l = p.group[ortho_group(p.c, o.m)].load[kind][i];
+            OrthoLoad& l = p.group[o.group].load[kind][i];
             const double steps = ortho_steps(o, kind);
             l.tiles += (double)ortho_tiles(o, kind, i);
             l.steps += (double)ortho_tiles(o, kind, i) * steps;
@@ -214,14 +215,14 @@ void plan_meeting(uint64_t& at, OrthoPlan& p) {
 // workgroup a unit allows.  (4781 x 188 in bfloat16 141 us against 184 uncut, three
 // of 512 x 4608 with one of 2048 x 512 356 against 397; parts of 256 take 155 and
 // 412, and two parts for 136 tiles, more than a workgroup a unit, 314 against 258.)
-double ortho_chain(const OrthoPlan& p, const std::vector<Ortho>& table, int group, int kind) {
+double ortho_chain(const OrthoPlan& p, const std::vector<Ortho>& table, uint32_t group, int kind) {
     const OrthoLoad& l = p.group[group].load[kind][0];
     double chain = std::fmax(l.steps / p.cus, kOrthoPart / 32.0);
     if (l.tiles > p.cus) return chain;
     for (; chain < l.longest; chain *= 1.1) {
         uint64_t n = 0;
         for (const Ortho& o : table)
-            if (ortho_group(p.c, o.m) == group) n += ortho_tiles(o, kind, 0) * ortho_parts(o, kind, chain);
+            if (o.group == group) n += ortho_tiles(o, kind, 0) * ortho_parts(o, kind, chain);
         if (n <= (uint64_t)p.cus) break;
     }
     return chain;
@@ -234,7 +235,7 @@ double ortho_chain(const OrthoPlan& p, const std::vector<Ortho>& table, int grou
 // smaller ones go whole to the least loaded die, the long tiles first.  `list`
 // receives 8 x the longest die's count entries, the others' ends idle; returns
 // that count.
-uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int group, int kind,
+uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, uint32_t group, int kind,
                     std::vector<OrthoWork>& list) {
     constexpr int kDies = 8;
     std::vector<OrthoWork> die[kDies];
@@ -260,7 +261,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int gro
     if (all.longest * all.tiles <= 1.25 * all.steps) {
         double done = 0.0;
         for (size_t i = 0; i < table.size(); ++i) {
-            if (ortho_group(p.c, table[i].m) != group) continue;
+            if (table[i].group != group) continue;
             const uint64_t tiles = ortho_tiles(table[i], kind, side);
             const uint32_t parts = parts_of(table[i]);
             for (uint64_t t = 0; t < tiles; ++t) {
@@ -271,7 +272,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, int gro
     } else {
         double load[kDies] = {};
         for (size_t i = 0; i < table.size(); ++i) {
-            if (ortho_group(p.c, table[i].m) != group) continue;
+            if (table[i].group != group) continue;
             const uint64_t tiles = ortho_tiles(table[i], kind, side);
             const uint32_t parts = parts_of(table[i]);
             const uint64_t pieces = tiles * parts >= 16 ? kDies : 1;
@@ -353,11 +354,13 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
     if (e == hipSuccess) e = device_info(dev, &di);
     if (e != hipSuccess) return BC_E_HIP;
     p.cus = di.cus;
-    for (int g = 0; g < 2; ++g) {
+    for (uint32_t g = 0; g < 2; ++g) {
         for (int kind = 0; kind < kOrthoKinds; ++kind) p.group[g].chain[kind] = ortho_chain(p, table, g, kind);
         ortho_choose(p.group[g], g == 1, p.cus);
     }
-    // the table, then the work lists, which follow from it
+    // The table, then the work lists.  The lists follow from the table's bytes (shapes,
+    // offsets and groups: the type of the results counts through the groups alone)
+    // and the device, which together are what the copy is found again by.
     struct Ctx {
         OrthoPlan* p;
         hipStream_t s;
@@ -365,7 +368,7 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
         size_t at;
     } ctx{&p, s, {}, table.size() * sizeof(Ortho)};
     try {
-        for (int g = 0; g < 2; ++g)
+        for (uint32_t g = 0; g < 2; ++g)
             for (int kind = 0; kind < kOrthoKinds; ++kind)
                 p.group[g].workgroups[kind] = ortho_list(p, table, g, kind, ctx.list);
         e = with_table(table.data(), ctx.at, ctx.list.size() * sizeof(OrthoWork),

@@ -146,8 +146,10 @@ struct Ortho {
     uint32_t tile0;          // of the 64 x 64 tiles of the start
     float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
+    uint32_t group;          // OrthoPlan's group that it goes through the products with
+    uint32_t unused;         // (the table is compared by its bytes: no padding)
 };
-static_assert(sizeof(Ortho) == 8 * 10 + 4 * 10, "Ortho layout");
+static_assert(sizeof(Ortho) == 8 * 10 + 4 * 12, "Ortho layout");
 
 // What a workgroup of a product launch computes: a tile of a matrix, or
 // nothing (matrix kOrthoIdle).  It carries what all but the last product need of
@@ -205,7 +207,7 @@ struct OrthoPlan {
     int steps, cus;
     OrthoGroup group[2];               // [1]: the larger matrices
 };
-inline int ortho_group(const OrthoCall& c, uint32_t m) { return c.out_dtype != BC_F32 || m >= kOrthoPairs; }
+inline uint32_t ortho_group(const OrthoCall& c, uint32_t m) { return c.out_dtype != BC_F32 || m >= kOrthoPairs; }
 // Picks tile sides and the schedule from the loads.
 void ortho_choose(OrthoGroup& g, bool may_pair, int cus);
 constexpr uint32_t kOrthoParts = 256;

@@ -1,0 +1,63 @@
+"""Orthogonalised updates where calls follow each other on the same memory and
+where a matrix's entries differ widely, against the formulas in 64 bits
+(tolerances: tests/test_gpu_orthogonalize.py)."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_layernorm import UNIT, f64
+from tests.test_gpu_orthogonalize import gradient, near, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def views(space, dtype, shapes):
+    """Matrices of `dtype` at places in `space` that do not depend on it."""
+    import torch
+    t, out, at = getattr(torch, dtype), [], 0
+    for r, c in shapes:
+        out.append(space[at:at + r * c * t.itemsize].view(t).view(r, c))
+        at += (r * c * 4 + 255) // 256 * 256
+    return out
+
+
+@pytest.mark.parametrize("order", [("float32", "bfloat16", "float32"), ("float16", "float32", "bfloat16", "float16")])
+@pytest.mark.parametrize("shapes", [[(40, 500), (200, 300)], [(32, 32), (64, 64)], [(17, 5000), (150, 150), (63, 640)]])
+def test_same_memory_in_another_type(shapes, order):
+    """A list on both sides of the shorter side that fp32 results are told
+    apart by, its memory seen in one type after the other."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    size = sum((r * c * 4 + 255) // 256 * 256 for r, c in shapes)
+    a, b = (torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ws = B.alloc_orthogonalize_workspace(shapes)
+    for step, dtype in enumerate(order):
+        rng = np.random.default_rng(step)
+        ups, outs = views(a, dtype, shapes), views(b, dtype, shapes)
+        b.fill_(255)
+        for u in ups:
+            u.copy_(torch.from_numpy(gradient(tuple(u.shape), rng)))
+        B.bytecomp_orthogonalize(ups, outs, ws)
+        for u, o in zip(ups, outs):
+            near(f64(o), f64(u), dtype)
+
+
+def test_same_weights_memory_in_another_type():
+    import torch
+    from paper_2205_14465_amd import binding as B
+    shapes = [(40, 500), (200, 300)]
+    rng = np.random.default_rng(8)
+    a = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    grads = [torch.from_numpy(gradient(s, rng)).float().cuda() for s in shapes]
+    momenta = [torch.empty_like(g) for g in grads]
+    ws = B.alloc_orthogonalize_workspace(shapes)
+    for wdtype in ("float32", "bfloat16", "float32"):
+        weights = views(a, wdtype, shapes)
+        for w, m in zip(weights, momenta):
+            w.copy_(torch.from_numpy(rng.standard_normal(tuple(w.shape)) * 0.1))
+            m.zero_()
+        before = [f64(w) for w in weights]
+        B.bytecomp_muon_step(weights, grads, momenta, 0.02, ws, nesterov=False, scales=[1.0, 1.0])
+        for w, b, g in zip(weights, before, grads):
+            want, noisy = (b - 0.02 * reference(f64(g), noise=n) for n in (None, np.random.default_rng(1)))
+            off = np.linalg.norm(f64(w) - want)
+            assert off <= 8 * np.linalg.norm(noisy - want) + (UNIT[wdtype] + 2.0 ** -22) * np.linalg.norm(want)
