@@ -529,8 +529,12 @@ int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inne
  *   X = U / (|U| + eps), |U| the Frobenius norm,
  *   `steps` times: A = X X^T, X <- a X + (b A + c A^2) X,
  * which drives every singular value of X towards 1.
- * Factors are kept as pairs of fp16 (22 bits), sums in fp32, the norm in
- * fp64: the results are as close to the exact ones as fp32 arithmetic's. */
+ * Factors are kept as pairs of fp16 (22 bits of an entry, or 2^-39 of |X|
+ * where that is more; coefficients that take singular values far past 1
+ * raise it with them), sums in fp32, the norm in fp64: the results are as
+ * close to the exact ones as fp32 arithmetic's, until one entry of U is
+ * thousands of times the norm of all others (then 2e-7 to 4e-7 off, as a
+ * share of the result's norm, where fp32 arithmetic is 2e-8 to 1e-7). */
 
 /* One matrix: out [rows, cols] receives the orthogonalised update
  * [rows, cols]; out may be update itself (same stride). */

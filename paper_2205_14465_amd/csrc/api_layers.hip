@@ -101,11 +101,12 @@ Planes turned(int dtype, const void* p, uint64_t ld, uint64_t rows, uint64_t col
 // -------------------------------------------------- orthogonalised updates
 constexpr int kMaxMatrices = 1 << 20;
 
-// The scales that keep X and the symmetric matrices (kernels_ortho.hip) in
-// fp16's range: bounds on their largest singular values, rounded up to powers of
-// two.  `reach` bounds X's within the steps, from [0, 1] at the start.  False:
-// the coefficients are not finite, or reach passes 64.
-bool ortho_scales(int steps, const double* k, float& top, float* scale) {
+// The scales that keep X and the symmetric matrices (kernels_ortho.hip) at the
+// top of fp16's range, where small entries beside large ones keep the most of
+// their second part: bounds on their largest singular values, and so on their
+// entries, rounded up to powers of two.  `reach` bounds X's within the steps, from
+// [0, 1] at the start.  False: the coefficients are not finite, or reach passes 64.
+bool ortho_scales(int steps, const double* k, float& x_scale, float* scale) {
     const double a = k[0], b = k[1], c = k[2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
     double reach = 1.0, most = 1.0;
@@ -142,7 +143,7 @@ bool ortho_scales(int steps, const double* k, float& top, float* scale) {
         if (!(bounds[i] <= 0x1p40)) return false;
         scale[i] = below(bounds[i]);
     }
-    top = below(most);
+    x_scale = below(most);
     return true;
 }
 
@@ -253,7 +254,7 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, uint32_
         const Ortho& o = table[i];
         for (uint32_t q = 0; q < parts; ++q)
             to.push_back(OrthoWork{(uint32_t)i, (uint32_t)tile, o.m, o.n, (uint32_t)(o.x >> 8), (uint32_t)(o.xt >> 8),
-                                   (uint32_t)(o.sym >> 8), o.x_scale, q, parts, slots, met});
+                                   (uint32_t)(o.sym >> 8), q, parts, slots, met});
         if (parts == 1) return;
         slots += parts;
         met += 1;
@@ -287,16 +288,16 @@ uint32_t ortho_list(const OrthoPlan& p, const std::vector<Ortho>& table, uint32_
     size_t longest = 0;
     for (const auto& d : die) longest = std::max(longest, d.size());
     for (size_t q = 0; q < longest; ++q)
-        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0, 0, 0, 0, 0, 0, 0.0f, 0, 1, 0, 0});
+        for (const auto& d : die) list.push_back(q < d.size() ? d[q] : OrthoWork{kOrthoIdle, 0, 0, 0, 0, 0, 0, 0, 1, 0, 0});
     return (uint32_t)(kDies * longest);
 }
 
-int check_ortho(int T, int steps, const double* k, double eps, float& top, OrthoPlan& p) {
+int check_ortho(int T, int steps, const double* k, double eps, OrthoPlan& p) {
     OrthoCall& c = p.c;
     if (T < 0 || T > kMaxMatrices) return BC_E_COUNT;
     if (!k) return BC_E_NULL;
     if (steps < 1 || steps > 64 || !(eps >= 0.0) || std::isinf(eps)) return BC_E_VALUE;
-    if (!ortho_scales(steps, k, top, c.scale)) return BC_E_VALUE;
+    if (!ortho_scales(steps, k, c.x_scale, c.scale)) return BC_E_VALUE;
     c.a = (float)k[0];
     c.b = (float)k[1];
     c.c = (float)k[2];
@@ -310,7 +311,7 @@ int check_ortho(int T, int steps, const double* k, double eps, float& top, Ortho
 // error.  The rest of the call: plan, table, launch.  Long products come first
 // in the table, so that a launch ends on short ones.
 template <typename Get>
-int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s, Get get) {
+int run_ortho(OrthoPlan& p, void* ws, size_t ws_bytes, hipStream_t s, Get get) {
     std::vector<Ortho> table;
     uint64_t at = 0, tiles = 0;
     try {
@@ -335,8 +336,6 @@ int run_ortho(OrthoPlan& p, float top, void* ws, size_t ws_bytes, hipStream_t s,
             table.push_back(given[(size_t)i]);
             Ortho& o = table.back();
             plan_matrix(o.rows, o.cols, at, p, o);
-            const double side = std::sqrt((double)o.rows * (double)o.cols);
-            o.x_scale = std::fmin(top, (float)std::exp2(std::floor(std::log2(side))));
         }
     } catch (const std::bad_alloc&) {
         return BC_E_SIZE;
@@ -607,12 +606,11 @@ int bytecomp_orthogonalize(int dtype, const bc_update* t, int T, int steps, cons
     if (!dtype_ok(dtype)) return BC_E_DTYPE;
     OrthoPlan p{};
     OrthoCall& c = p.c;
-    float top = 0.0f;
-    if (const int rc = check_ortho(T, steps, coefficients, eps, top, p)) return rc;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, p)) return rc;
     if (T == 0) return BC_OK;
     if (!t) return BC_E_NULL;
     c.in_dtype = c.out_dtype = dtype;
-    return run_ortho(p, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+    return run_ortho(p, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
         const bc_update& u = t[i];
         rows = u.rows;
         cols = u.cols;
@@ -635,8 +633,7 @@ int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double 
     if (!dtype_ok(wdtype) || !dtype_ok(gdtype)) return BC_E_DTYPE;
     OrthoPlan p{};
     OrthoCall& c = p.c;
-    float top = 0.0f;
-    if (const int rc = check_ortho(T, steps, coefficients, eps, top, p)) return rc;
+    if (const int rc = check_ortho(T, steps, coefficients, eps, p)) return rc;
     if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay)) return BC_E_VALUE;
     if (T == 0) return BC_OK;
     if (!t) return BC_E_NULL;
@@ -647,7 +644,7 @@ int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double 
     c.momentum = (float)momentum;
     c.keep = (float)(1.0 - lr * weight_decay);
     c.lr = (float)lr;
-    return run_ortho(p, top, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
+    return run_ortho(p, ws, ws_bytes, (hipStream_t)stream, [&](int i, uint64_t& rows, uint64_t& cols, Ortho& o) {
         const bc_param& u = t[i];
         rows = u.rows;
         cols = u.cols;

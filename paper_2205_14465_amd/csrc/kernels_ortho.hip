@@ -26,10 +26,14 @@
 // Precision: singular values under one grow by up to a per step, and with them
 // every rounding made before, so 16-bit factors are not enough (in one fp16 part
 // the result of a gradient with a few dominant directions is 2% off, in bfloat16
-// 18%).  Every factor is kept as two fp16 parts (22 bits) scaled by powers of
-// two to the middle of fp16's range, a product is three matrix-core products
-// (leading x leading, leading x rest both ways), sums are fp32: the result is as
-// close to the exact one as fp32 arithmetic's.
+// 18%).  Every factor is kept as two fp16 parts scaled by powers of two to the
+// top of fp16's range: 22 bits of each entry, or 2^-39 of |X| where an entry is
+// so small beside it that its second part falls under fp16's smallest number (one
+// entry 100 times the norm of the others: 1e-7 to 2e-7 off; scaled to the middle
+// of the range, a typical entry near 1, 2e-6).  A product is three matrix-core
+// products (leading x leading, leading x rest both ways), sums are fp32: the
+// result is as close to the exact one as fp32 arithmetic's, until one entry is
+// thousands of times the rest.
 #include "gemm.hpp"
 #include "launch.hpp"
 #include "layers.hpp"
@@ -156,7 +160,7 @@ __global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
         for (uint32_t i = threadIdx.x; i < a.slots; i += 256) ((uint32_t*)(a.ws + a.meet))[i] = 0;
     const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.tile0; })];
     const double mine = threadIdx.x < o.parts ? ((const double*)(a.ws + o.part))[threadIdx.x] : 0.0;
-    const float scale = (float)((double)o.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
+    const float scale = (float)((double)a.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
     const uint32_t across = (o.cols + 63) / 64;
     f16_t* flat = (f16_t*)(a.ws + (o.turned ? o.xt : o.x));
     f16_t* turned = (f16_t*)(a.ws + (o.turned ? o.x : o.xt));
@@ -202,8 +206,8 @@ enum Stage { kGram, kSym, kNext, kLast };
 
 // What a launch computes: kSym: matrix `out` = alpha U V + beta U + gamma V of
 // the symmetric matrices u and v; kGram: matrix `out`, kNext and kLast:
-// X <- alpha X + U X / scale, read from copy `from` of X^T.  The factors
-// contain the scales of what they multiply.
+// X <- alpha X + beta U X, X^T read from its copy `from`.  The factors contain
+// the scales of what they multiply.
 struct StageArgs {
     int u, v, out, from;
     float alpha, beta, gamma;
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
     if constexpr (stage == kGram) {
         if (!multiply(g, a, work, rows_of(x, np, m, m0), rows_of(x, np, m, n0), np, lds)) return;
         const SymmetricEpilogue e{sym(s.out), nullptr, nullptr, mp, m * mp, m, m0, n0,
-                                  s.alpha / (work.x_scale * work.x_scale), 0.0f, 0.0f};
+                                  s.alpha, 0.0f, 0.0f};
         g.finish_both_ways(lds, e);
     } else if constexpr (stage == kSym) {
         if (!multiply(g, a, work, rows_of(sym(s.u), mp, m, m0), rows_of(sym(s.v), mp, m, n0), mp, lds)) return;
@@ -381,7 +385,6 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
         const Operand<f16_t> u = tall ? rows_of(old, mp, n, m0) : rows_of(sym(s.u), mp, m, m0);
         const Operand<f16_t> v = tall ? rows_of(sym(s.u), mp, m, n0) : rows_of(xt[s.from], mp, n, n0);
         if (!multiply(g, a, work, u, v, mp, lds)) return;
-        const float inv = 1.0f / work.x_scale;
         g.finish(lds, [&](int row, int col, float (&v)[8]) {
             const uint64_t r = m0 + row;
             const uint32_t c = n0 + col;
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(G::kThreads) void ortho_product(OrthoCall a, StageA
             float t[8];
             load_two(old + r * old_ld + c, old_plane, t);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (s.alpha * t[i] + v[i] * s.beta) * inv;
+            for (int i = 0; i < 8; ++i) v[i] = s.alpha * t[i] + v[i] * s.beta;
             if (a.muon) {
                 load_any(a.out_dtype, o.out, r * o.ld_out + c, left, t);
 #pragma unroll
@@ -486,7 +489,7 @@ hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
         int from = 0;
         for (int left = p.steps; left > 0 && e == hipSuccess;) {
             const bool two = g.pairs && left >= 2;
-            e = launch_stage<kGram>(p, g, StageArgs{0, 0, 0, 0, c.scale[kScaleGram], 0.0f, 0.0f}, s);
+            e = launch_stage<kGram>(p, g, StageArgs{0, 0, 0, 0, c.scale[kScaleGram] / (c.x_scale * c.x_scale), 0.0f, 0.0f}, s);
             sym(0, kScaleGram, 0, kScaleGram, 1, kScalePoly, c.c, c.b, 0.0f);             // 1: B
             StageArgs next{1, 0, 0, from, c.a, 1.0f / c.scale[kScalePoly], 0.0f};
             if (two) {
@@ -497,6 +500,10 @@ hipError_t launch_orthogonalize(const OrthoPlan& p, hipStream_t s) {
                 next = StageArgs{0, 0, 0, from, c.a * c.a, 1.0f / c.scale[kScalePair], 0.0f};
             }
             left -= two ? 2 : 1;
+            if (left == 0) {  // the caller's X has no scale
+                next.alpha /= c.x_scale;
+                next.beta /= c.x_scale;
+            }
             if (e == hipSuccess)
                 e = left > 0 ? launch_stage<kNext>(p, g, next, s) : launch_stage<kLast>(p, g, next, s);
             from = 1 - from;

@@ -144,12 +144,11 @@ struct Ortho {
     uint32_t turned, parts;  // parts: partial sums of squares
     uint32_t part0;          // workgroups before this matrix's: of the norm,
     uint32_t tile0;          // of the 64 x 64 tiles of the start
-    float x_scale;           // X is kept times this power of two
     float step_scale;        // the update's factor beside the learning rate
     uint32_t group;          // OrthoPlan's group that it goes through the products with
-    uint32_t unused;         // (the table is compared by its bytes: no padding)
 };
-static_assert(sizeof(Ortho) == 8 * 10 + 4 * 12, "Ortho layout");
+// (the table is compared by its bytes: no padding)
+static_assert(sizeof(Ortho) == 8 * 10 + 4 * 10, "Ortho layout");
 
 // What a workgroup of a product launch computes: a tile of a matrix, or
 // nothing (matrix kOrthoIdle).  It carries what all but the last product need of
@@ -159,10 +158,9 @@ static_assert(sizeof(Ortho) == 8 * 10 + 4 * 12, "Ortho layout");
 struct OrthoWork {
     uint32_t matrix, tile, m, n;
     uint32_t x, xt, sym;     // offsets in the workspace, in 256 bytes
-    float x_scale;
     uint32_t part, parts, sums, met;
 };
-static_assert(sizeof(OrthoWork) == 48, "OrthoWork layout");
+static_assert(sizeof(OrthoWork) == 44, "OrthoWork layout");
 constexpr uint32_t kOrthoIdle = 0xFFFFFFFFu;
 
 // The work of a launch with one tile side: tiles, and steps of 32 along k, in
@@ -179,6 +177,7 @@ struct OrthoCall {
     uint32_t slots;          // for sums of tiles cut along k: kOrthoSlots at most,
     uint64_t meet;           // from here on in the workspace, after as many counters
     float a, b, c, eps;
+    float x_scale;           // X is kept times this power of two
     float scale[4];          // of the symmetric matrices by what they hold (SymScale)
     bool muon, nesterov;
     float momentum, keep, lr;   // keep: 1 - lr * weight decay

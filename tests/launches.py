@@ -77,12 +77,11 @@ def fields(names, kind):
 # Layouts of csrc/layers.hpp, as far as they are read here.
 class Ortho(ctypes.Structure):
     _fields_ = fields("in_ out momentum", ptr) + fields("ld_in ld_out ld_momentum x xt sym part", u64) + \
-        fields("rows cols m n turned parts part0 tile0", u32) + [("x_scale", f32), ("step_scale", f32)] + \
-        fields("group unused", u32)
+        fields("rows cols m n turned parts part0 tile0", u32) + [("step_scale", f32), ("group", u32)]
 
 
 class OrthoWork(ctypes.Structure):
-    _fields_ = fields("matrix tile m n x xt sym", u32) + [("x_scale", f32)] + fields("part parts sums met", u32)
+    _fields_ = fields("matrix tile m n x xt sym part parts sums met", u32)
 
 
 class OrthoCall(ctypes.Structure):

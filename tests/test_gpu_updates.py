@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests.test_gpu_layernorm import UNIT, f64
-from tests.test_gpu_orthogonalize import gradient, near, reference
+from tests.test_gpu_orthogonalize import ABC, gradient, near, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,59 @@ def test_same_weights_memory_in_another_type():
             want, noisy = (b - 0.02 * reference(f64(g), noise=n) for n in (None, np.random.default_rng(1)))
             off = np.linalg.norm(f64(w) - want)
             assert off <= 8 * np.linalg.norm(noisy - want) + (UNIT[wdtype] + 2.0 ** -22) * np.linalg.norm(want)
+
+
+def fp32_arithmetic(u):
+    x = (u.T if u.shape[0] > u.shape[1] else u)
+    x = (x / np.sqrt((x * x).sum())).astype(np.float32)
+    a, b, c = (np.float32(k) for k in ABC)
+    for _ in range(5):
+        g = x @ x.T
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.T.astype(np.float64) if u.shape[0] > u.shape[1] else x.astype(np.float64)
+
+
+def two_parts(u):
+    """The formulas in 64 bits with every factor stored as two fp16 parts at the
+    top of fp16's range (X and A at most 2, B at most 8)."""
+    def held(v, scale):
+        s = v * scale
+        hi = s.astype(np.float16)
+        return (hi + (s - hi).astype(np.float16).astype(np.float64)) / scale
+    x = (u.T if u.shape[0] > u.shape[1] else u)
+    x = held(x / np.sqrt((x * x).sum()), 2.0 ** 14)
+    a, b, c = ABC
+    for _ in range(5):
+        g = held(x @ x.T, 2.0 ** 13)
+        x = held(a * x + held(b * g + c * (g @ g), 2.0 ** 12) @ x, 2.0 ** 14)
+    return x.T if u.shape[0] > u.shape[1] else x
+
+
+@pytest.mark.parametrize("kind", ["spike", "spikes", "higher spike", "rows", "columns"])
+@pytest.mark.parametrize("shape", [(16, 16), (17, 90), (64, 64), (128, 512), (512, 300)])
+def test_entries_of_many_sizes(shape, kind):
+    """One entry or a few with almost all of the norm, or rows or columns over
+    four decades.  Tolerance: the kernel rounds its sums as fp32 arithmetic does
+    and its factors as two_parts does, each in another order; three times what
+    both lose together, and one rounding of the result."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    rng = np.random.default_rng(shape[0] + len(kind))
+    g = rng.standard_normal(shape)
+    size = np.linalg.norm(g)
+    if "spike" in kind:
+        g[3, 5] = (1000 if kind == "higher spike" else 100) * size
+    if kind == "spikes":
+        g[9, 2], g[3, 7] = -30 * size, 10 * size
+    if kind == "rows":
+        g *= 10.0 ** -np.linspace(0, 4, shape[0])[:, None]
+    if kind == "columns":
+        g *= 10.0 ** -np.linspace(0, 4, shape[1])[None, :]
+    u = torch.from_numpy(g).float().cuda()
+    out = torch.empty_like(u)
+    B.bytecomp_orthogonalize([u], [out], B.alloc_orthogonalize_workspace([shape]), eps=0.0)
+    want = reference(f64(u), eps=0.0)
+    size = np.linalg.norm(want)
+    lost = [np.linalg.norm(form(f64(u)) - want) / size for form in (fp32_arithmetic, two_parts)]
+    off = np.linalg.norm(f64(out) - want) / size
+    assert off <= 3 * sum(lost) + 2.0 ** -24, (off, lost)
