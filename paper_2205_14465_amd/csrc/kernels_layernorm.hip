@@ -392,6 +392,18 @@ hipError_t launch_sum_parts(int dtype, const float* part, uint32_t parts, uint64
     return hipGetLastError();
 }
 
+// Calls launch(part) for parts of the rows with fewer than 2^32 threads each, which
+// is what HIP takes along an axis, at `threads` a row; from(r) is the call from row r on.
+template <typename A, typename From, typename Launch>
+static void by_rows(const A& a, uint32_t threads, From from, Launch launch) {
+    const uint64_t most = (1ull << 31) / threads;
+    for (uint64_t r = 0; r < a.rows; r += most) {
+        A part = from(r);
+        part.rows = a.rows - r < most ? a.rows - r : most;
+        launch(part, (uint32_t)part.rows);
+    }
+}
+
 // Rows of up to 64 * kPer vectors go to a wave, of up to kLnBlock * kPer to a
 // workgroup, longer ones to the wide kernels.  Measured in bfloat16, us:
 //   forward   8192 x 2048  wave 12.9, workgroup 14.0;  8192 x 4096  22.7, 22.4;
@@ -400,16 +412,35 @@ hipError_t launch_sum_parts(int dtype, const float* part, uint32_t parts, uint64
 //             2048 x 8192  workgroup 33.1, wide 54.4;  2048 x 16384  90.7, 89.2,
 //             500 x 12001 (fp16)  48.4, 33.6;  fp32, 4096 x 8192  103, 133
 template <typename T, typename WT, bool kWhole>
-static void ln_forward_launch(const LnForward& a, hipStream_t s) {
-    const uint32_t vecs = (a.cols + kVec<T> - 1) / kVec<T>;
-    const dim3 block(kLnBlock), waves((uint32_t)((a.rows + kLnWaves - 1) / kLnWaves)), rows((uint32_t)a.rows);
-    if (vecs <= 64) hipLaunchKernelGGL((ln_forward<T, WT, 64, 1, kWhole>), waves, block, 0, s, a);
-    else if (vecs <= 128) hipLaunchKernelGGL((ln_forward<T, WT, 64, 2, kWhole>), waves, block, 0, s, a);
-    else if (vecs <= 256) hipLaunchKernelGGL((ln_forward<T, WT, 64, 4, kWhole>), waves, block, 0, s, a);
-    else if (vecs <= 512) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 2, kWhole>), rows, block, 0, s, a);
-    else if (vecs <= 1024) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 4, kWhole>), rows, block, 0, s, a);
-    else if (vecs <= 2048) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 8, kWhole>), rows, block, 0, s, a);
-    else hipLaunchKernelGGL((ln_forward_wide<T, WT>), rows, dim3(kWideBlock), 0, s, a);
+static void ln_forward_launch(const LnForward& all, hipStream_t s) {
+    const uint32_t vecs = (all.cols + kVec<T> - 1) / kVec<T>;
+    const auto from = [&](uint64_t r) {
+        LnForward a = all;
+        a.x = (const T*)a.x + r * a.ldx;
+        a.y = (T*)a.y + r * a.ldy;
+        if (a.mean) a.mean += r;
+        if (a.rstd) a.rstd += r;
+        return a;
+    };
+    const dim3 block(kLnBlock);
+    if (vecs <= 256) {
+        by_rows(all, 64, from, [&](const LnForward& a, uint32_t rows) {
+            const dim3 waves((rows + kLnWaves - 1) / kLnWaves);
+            if (vecs <= 64) hipLaunchKernelGGL((ln_forward<T, WT, 64, 1, kWhole>), waves, block, 0, s, a);
+            else if (vecs <= 128) hipLaunchKernelGGL((ln_forward<T, WT, 64, 2, kWhole>), waves, block, 0, s, a);
+            else hipLaunchKernelGGL((ln_forward<T, WT, 64, 4, kWhole>), waves, block, 0, s, a);
+        });
+    } else if (vecs <= 2048) {
+        by_rows(all, kLnBlock, from, [&](const LnForward& a, uint32_t rows) {
+            if (vecs <= 512) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 2, kWhole>), dim3(rows), block, 0, s, a);
+            else if (vecs <= 1024) hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 4, kWhole>), dim3(rows), block, 0, s, a);
+            else hipLaunchKernelGGL((ln_forward<T, WT, kLnBlock, 8, kWhole>), dim3(rows), block, 0, s, a);
+        });
+    } else {
+        by_rows(all, kWideBlock, from, [&](const LnForward& a, uint32_t rows) {
+            hipLaunchKernelGGL((ln_forward_wide<T, WT>), dim3(rows), dim3(kWideBlock), 0, s, a);
+        });
+    }
 }
 
 // Vectors of the longest rows that the backward pass holds in registers: twice
@@ -429,7 +460,19 @@ static void ln_backward_launch(const LnBackward& a, hipStream_t s) {
     else if (vecs <= ln_longest<T>(a.cols)) {
         if constexpr (sizeof(T) == 4 && kWhole) hipLaunchKernelGGL((ln_backward<T, WT, kLnBlock, 8, true>), grid, block, 0, s, a);
     } else {
-        if (a.dx) hipLaunchKernelGGL((ln_backward_wide<T, WT>), dim3((uint32_t)a.rows), dim3(kWideBlock), 0, s, a);
+        const auto from = [&](uint64_t r) {
+            LnBackward p = a;
+            p.dy = (const T*)p.dy + r * p.lddy;
+            p.x = (const T*)p.x + r * p.ldx;
+            p.dx = (T*)p.dx + r * p.lddx;
+            p.mean += r;
+            p.rstd += r;
+            return p;
+        };
+        if (a.dx)
+            by_rows(a, kWideBlock, from, [&](const LnBackward& p, uint32_t rows) {
+                hipLaunchKernelGGL((ln_backward_wide<T, WT>), dim3(rows), dim3(kWideBlock), 0, s, p);
+            });
         if (a.part)
             hipLaunchKernelGGL((ln_column_sums<T>), dim3((vecs + kLnBlock - 1) / kLnBlock, a.parts), block, 0, s, a);
     }

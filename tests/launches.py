@@ -199,6 +199,62 @@ def work_lists_of_the_same_memory_in_another_type():
             check_products(s, shapes)
 
 
+class LnForward(ctypes.Structure):
+    _fields_ = fields("x weight bias y mean rstd", ptr) + fields("rows ldx ldy", u64)
+
+
+class LnBackward(ctypes.Structure):
+    _fields_ = fields("dy x weight mean rstd dx part", ptr) + fields("rows lddy ldx lddx", u64)
+
+
+def check_rows(launches, rows, bytes_of, kind, names):
+    """The launches take the rows one after the other: as many as the grid has
+    waves or workgroups for, every pointer at its own row."""
+    at = 0
+    for l in launches:
+        a = l.arg(0, kind)
+        threads = 64 if re.search(r"Li64ELi\dE", l.name) else l.block[0]
+        assert l.grid[0] * l.block[0] < 1 << 32 and l.grid[1:] == [1, 1]
+        assert l.grid[0] * l.block[0] // threads >= a.rows > (l.grid[0] - 1) * l.block[0] // threads
+        for n in names:
+            assert getattr(a, n) == bytes_of[n][0] + at * bytes_of[n][1], (n, at)
+        at += a.rows
+    assert at == rows
+
+
+def layer_norm_rows():
+    s = Session()
+    s.want("ln_forward", LnForward)
+    s.want("ln_backward", LnBackward)
+    fwd, bwd = s.lib.bytecomp_layernorm_forward, s.lib.bytecomp_layernorm_backward
+    fwd.argtypes = [ctypes.c_int] * 2 + [u64] * 2 + [ptr, u64, ptr, ptr, f64, ptr, u64] + [ptr] * 3
+    bwd.argtypes = [ctypes.c_int] * 2 + [u64] * 2 + [ptr, u64, ptr, u64] + [ptr] * 4 + [u64] + [ptr] * 3 + \
+        [ctypes.c_size_t, ptr]
+    X, Y, Z, M, R, W = (i << 52 for i in range(1, 7))
+    for dtype, size in ((0, 4), (1, 2), (2, 2)):
+        for cols in (1, 8, 64, 1001, 2048, 2049, 8200, 16384, 70001):
+            for rows in (1, 5, (1 << 21) - 1, 1 << 21, (1 << 22) + 1, 1 << 24, (1 << 26) + 5, (1 << 31) - 1):
+                s.clear()
+                assert fwd(dtype, 0, rows, cols, X, cols + 3, W, W, 1e-5, Y, cols + 5, M, R, None) == 0, (rows, cols)
+                places = {"x": (X, (cols + 3) * size), "y": (Y, (cols + 5) * size), "mean": (M, 4), "rstd": (R, 4)}
+                check_rows(s.take(), rows, places, LnForward, places)
+                s.clear()
+                assert bwd(dtype, 0, rows, cols, Z, cols, X, cols + 3, W, M, R, Y, cols + 5, W, W, W, 1 << 50, None) == 0
+                wide = [l for l in s.take() if "ln_backward_wide" in l.name]
+                assert all(l.grid[0] * l.block[0] < 1 << 32 for l in s.take())
+                if wide:
+                    places = {"dy": (Z, cols * size), "x": (X, (cols + 3) * size), "dx": (Y, (cols + 5) * size),
+                              "mean": (M, 4), "rstd": (R, 4)}
+                    check_rows(wide, rows, places, LnBackward, places)
+                else:  # the workgroups visit rows a fixed step apart
+                    l, = (l for l in s.take() if "ln_backward" in l.name)
+                    assert l.arg(0, LnBackward).rows == rows
+        # nothing kept
+        s.clear()
+        assert fwd(dtype, 0, (1 << 26) + 1, 8, X, 8, None, None, 1e-5, Y, 8, None, None, None) == 0
+        assert all(l.arg(0, LnForward).mean is None and l.arg(0, LnForward).rstd is None for l in s.take())
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]]()
     print("done:", sys.argv[1])
