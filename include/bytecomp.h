@@ -496,9 +496,9 @@ enum bc_act { BC_ACT_NONE = 0, BC_ACT_RELU = 1, BC_ACT_GELU = 2, BC_ACT_GELU_TAN
  *             backward pass; NULL: not kept.  y comes from the unrounded z.
  *   ws        at least bytecomp_linear_workspace_size bytes, 16-byte aligned;
  *             NULL is fine where that is 0
- * fp32 products are sums of bfloat16 products of the operands' three parts
- * (24 bits) and as exact as fp32 ones; with an infinite operand such a
- * product is NaN, and parts under the smallest normal number may be lost.
+ * fp32 products of more than 64 rows (and all of the backward pass) are sums
+ * of bfloat16 products of the operands' three parts (24 bits) and as exact as
+ * fp32 ones; parts under the smallest normal number may be lost.
  * rows, inner and cols < 2^22 (BC_E_SIZE).  Zero rows or columns: nothing to
  * do; zero inner: the product is zero. */
 int bytecomp_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* x, uint64_t ldx,

@@ -8,6 +8,8 @@
 //   P = 1: a0 b0
 //   P = 2: a0 b0 + a0 b1 + a1 b0            (fp16: 22 bits of each operand)
 //   P = 3: the same + a1 b1 + a0 b2 + a2 b0 (bfloat16: 24 bits)
+// With an infinity or NaN among the values a0 b0 alone says what the sum is: the
+// other products would make NaN of infinity times a zero part.
 //
 // Per step of kBK along K the tile's rows of A and B go from memory to LDS
 // without passing registers (global_load_lds, 16 bytes a lane), up to kStages
@@ -85,9 +87,10 @@ struct GemmTile {
     static_assert(kLoadA * kRows * kWaves == kBM && kLoadB * kRows * kWaves == kBN, "loads cover the tile");
 
     f32x16 acc[kFM][kFN];
-    // Small tiles have the registers to add the products of lesser planes apart:
-    // two thirds (P = 2) of the roundings at the size of the sum fall away.
-    static constexpr bool kApart = P > 1 && kFM * kFN <= 2;
+    // Tiles that have the registers add the products of lesser planes apart: two
+    // thirds (P = 2) of the roundings at the size of the sum fall away.
+    static constexpr bool kApart = P > 1 && kFM * kFN <= 4;
+    static_assert(P < 3 || kApart, "bfloat16 planes hold infinities, which lesser products must not reach");
 
     static __device__ __forceinline__ int swizzle(int row) { return kBK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
@@ -223,7 +226,12 @@ struct GemmTile {
 #pragma unroll
             for (int m = 0; m < kFM; ++m)
 #pragma unroll
-                for (int n = 0; n < kFN; ++n) acc[m][n] += lesser[m][n];
+                for (int n = 0; n < kFN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float x = acc[m][n][r];
+                        acc[m][n][r] = P < 3 || fabsf(x) < INFINITY ? x + lesser[m][n][r] : x;
+                    }
         }
         lds_barrier();  // every wave has read its last fragments: the epilogue may write LDS
     }

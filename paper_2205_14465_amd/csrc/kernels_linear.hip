@@ -87,6 +87,17 @@ struct PlaneOf<float> {
     static constexpr int P = 3;
 };
 
+// v rounded to a plane's type, toward zero where the nearest is an infinity (fp32
+// numbers past bfloat16's largest: the next planes hold what is left of them).
+template <typename E>
+__device__ __forceinline__ E lead(float v) {
+    if constexpr (__is_same(E, bf16_t)) {
+        const uint32_t bits = __float_as_uint(v);
+        if ((bits & 0x7fffffffu) - 0x7f7f8000u < 0x8000u) v = __uint_as_float(bits & 0xffff0000u);
+    }
+    return (E)v;
+}
+
 // v as P planes of eight elements at p, p + plane, ...
 template <typename T>
 __device__ __forceinline__ void store_planes(typename PlaneOf<T>::type* p, uint64_t plane, const float (&v)[8]) {
@@ -100,7 +111,7 @@ __device__ __forceinline__ void store_planes(typename PlaneOf<T>::type* p, uint6
         vec w;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w[i] = (E)rest[i];
+            w[i] = PlaneOf<T>::P > 1 && q == 0 ? lead<E>(rest[i]) : (E)rest[i];
             rest[i] -= (float)w[i];  // exact
         }
         *(vec*)(p + q * plane) = w;
