@@ -61,7 +61,8 @@ __device__ __forceinline__ float act_slope(int act, float z) {
                    z * (0.5f * kTanhScale) * (exact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
         case BC_ACT_GELU_TANH: {
             const float p = logistic<exact>(2.0f * kTanhScale * (z + kTanhCubic * z * z * z));
-            return p + z * p * (1.0f - p) * (2.0f * kTanhScale) * (1.0f + 3.0f * kTanhCubic * z * z);
+            // (where z z would pass fp32's range p (1 - p) has long been 0)
+            return p + z * p * (1.0f - p) * (2.0f * kTanhScale) * (1.0f + 3.0f * kTanhCubic * fminf(z * z, 1e30f));
         }
         case BC_ACT_SILU: {
             const float p = logistic<exact>(z);
