@@ -301,7 +301,7 @@ int check_ortho(int T, int steps, const double* k, double eps, OrthoPlan& p) {
     c.a = (float)k[0];
     c.b = (float)k[1];
     c.c = (float)k[2];
-    c.eps = (float)eps;
+    c.eps = eps;
     p.steps = steps;
     c.T = T;
     return BC_OK;

@@ -160,7 +160,14 @@ __global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
         for (uint32_t i = threadIdx.x; i < a.slots; i += 256) ((uint32_t*)(a.ws + a.meet))[i] = 0;
     const Ortho o = a.d[owner(a.d, a.T, blockIdx.x, [](const Ortho& x) { return x.tile0; })];
     const double mine = threadIdx.x < o.parts ? ((const double*)(a.ws + o.part))[threadIdx.x] : 0.0;
-    const float scale = (float)((double)a.x_scale / (sqrt(block_sum_f64(mine, sh)) + (double)a.eps));
+    // The scale in two factors, the first a power of two that keeps the second and
+    // their products with U in fp32's range.  (A sum so small that its scale still
+    // passes that range is eps alone, of a matrix of zeros.)
+    double size = sqrt(block_sum_f64(mine, sh)) + a.eps;
+    const float first = size < 0x1p-100 ? 0x1p64f : size > 0x1p100 ? 0x1p-64f : 1.0f;
+    size *= first;
+    const double second = (double)a.x_scale / size;  // infinite for 0, NaN for NaN
+    const float scale = size > 0.0 && second > (double)__FLT_MAX__ ? __FLT_MAX__ : (float)second;
     const uint32_t across = (o.cols + 63) / 64;
     f16_t* flat = (f16_t*)(a.ws + (o.turned ? o.xt : o.x));
     f16_t* turned = (f16_t*)(a.ws + (o.turned ? o.x : o.xt));
@@ -183,7 +190,7 @@ __global__ __launch_bounds__(256) void ortho_start(OrthoCall a) {
         u[i].template make<false>(a);
         float (&v)[8] = u[i].g;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < u[i].left ? v[j] * scale : 0.0f;  // 0 even where scale is infinite
+        for (int j = 0; j < 8; ++j) v[j] = j < u[i].left ? v[j] * first * scale : 0.0f;  // 0 even where scale is infinite
         if (r < o.rows) store_two(flat + r * flat_ld + c, o.rows * flat_ld, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) tile[lr][lc + j] = v[j];

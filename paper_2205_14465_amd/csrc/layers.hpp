@@ -176,7 +176,8 @@ struct OrthoCall {
     uint32_t parts, tiles;   // workgroups of the norm and of the start
     uint32_t slots;          // for sums of tiles cut along k: kOrthoSlots at most,
     uint64_t meet;           // from here on in the workspace, after as many counters
-    float a, b, c, eps;
+    double eps;
+    float a, b, c;
     float x_scale;           // X is kept times this power of two
     float scale[4];          // of the symmetric matrices by what they hold (SymScale)
     bool muon, nesterov;

@@ -117,3 +117,31 @@ def test_entries_of_many_sizes(shape, kind):
     lost = [np.linalg.norm(form(f64(u)) - want) / size for form in (fp32_arithmetic, two_parts)]
     off = np.linalg.norm(f64(out) - want) / size
     assert off <= 3 * sum(lost) + 2.0 ** -24, (off, lost)
+
+
+def test_norms_at_the_ends_of_the_range():
+    """The update's scale does not matter without eps, from numbers under the
+    smallest normal one to the largest: the bits of the same matrix near 1 where
+    its numbers keep theirs (powers of two).  A zero matrix gives zero for any
+    eps above 0, a NaN for 0 / 0; a NaN or an infinity spoils all of its matrix."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    rng = np.random.default_rng(6)
+    shape = (50, 70)
+    # eight bits an entry: exact down to 2^-141
+    base = torch.from_numpy(np.clip(np.round(gradient(shape, rng) * 32), -127, 127)).float().cuda()
+    ups = [base] + [base * 2.0 ** k for k in (60, 100, 120, -60, -100, -115, -126)]
+    ups.append(base * 2.0 ** -100 * 2.0 ** -41)
+    ups += [torch.zeros_like(base), base.clone(), base.clone(), base]
+    ups[-3][3, 4], ups[-2][49, 69] = float("nan"), -float("inf")
+    outs = [torch.empty_like(u) for u in ups]
+    ws = B.alloc_orthogonalize_workspace([shape] * len(ups))
+    B.bytecomp_orthogonalize(ups, outs, ws, eps=0.0)
+    near(f64(outs[0]), f64(base), eps=0.0)
+    for o in outs[1:9] + outs[-1:]:
+        assert torch.equal(o, outs[0])
+    assert outs[9].isnan().all() and outs[10].isnan().all() and outs[11].isnan().all()
+    for eps in (1e-7, 1e-30, 1e-50, 1e-300):
+        B.bytecomp_orthogonalize([ups[9], base], outs[:2], ws, eps=eps)
+        assert not outs[0].any()
+        near(f64(outs[1]), f64(base), eps=eps)
