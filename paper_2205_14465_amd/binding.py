@@ -620,7 +620,19 @@ def _vector(name, t, n, dtype):
 
 
 def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    if ws is None:
+        return None, 0
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous device tensor, got strides {tuple(ws.stride())} on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _one_device(tensors):
+    """Raises unless all tensors (None and lists among them) are on one device."""
+    found = {str(t.device) for each in tensors if each is not None
+             for t in (each if isinstance(each, (list, tuple)) else [each]) if t is not None}
+    if len(found) > 1:
+        raise ValueError(f"tensors on several devices: {', '.join(sorted(found))}")
 
 
 def _alloc_bytes(n, device):
@@ -644,6 +656,7 @@ class _Call:
     tensors that the pointers belong to."""
 
     def __init__(self, fn, args, keep):
+        _one_device(keep)
         self._fn, self._args, self._keep = fn, args, keep
         self._entry = getattr(lib(), fn)
 
