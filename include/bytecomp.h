@@ -517,8 +517,10 @@ int bytecomp_linear_workspace_size(int dtype, uint64_t rows, uint64_t inner, uin
  *   gdtype  element type of dw and dbias: dtype or BC_F32
  *   z       of the forward pass; may be NULL with BC_ACT_NONE
  *   dx, dw, dbias  overwritten; NULL: not wanted
- * In fp16 and bfloat16, dz is rounded to dtype for the products (dbias sums
- * it unrounded).  Zero rows: dw and dbias become zero. */
+ * In fp16 and bfloat16, dz is rounded to dtype for the products, also where dw
+ * is fp32 (half a unit of dtype in each term of its sums); dbias sums it
+ * unrounded, with activations and slopes up to |t| 2^-24 of their exponential
+ * of t off.  Zero rows: dw and dbias become zero. */
 int bytecomp_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inner, uint64_t cols, const void* dy,
                              uint64_t lddy, const void* z, uint64_t ldz, int act, const void* x, uint64_t ldx,
                              const void* w, uint64_t ldw, void* dx, uint64_t lddx, void* dw, uint64_t lddw,
@@ -559,7 +561,11 @@ typedef struct bc_param {
 
 /* Bytes of workspace that the two calls below need for matrices of these
  * shapes (host arrays of T row and column counts; host only): 12 bytes an
- * element and 12 for each of min(rows, cols)^2, rounded up to whole 64s. */
+ * element and 12 for each of min(rows, cols)^2, with sides rounded up to whole
+ * 64s; up to 3 KB a matrix for the norm's partial sums and alignment; and where
+ * a side is 1024 or more and the matrix has few tiles of 64 by 64, 16 KB for
+ * every part of a product's tile that is cut along that side, up to 8.4 MB for
+ * the call.  (512 by 4608: 36.8 MB, of which 5.2 MB parts.) */
 int bytecomp_orthogonalize_workspace_size(const uint64_t* rows, const uint64_t* cols, int T, size_t* bytes);
 
 /* Orthogonalise T updates.

@@ -27,8 +27,10 @@ namespace {
 
 // ------------------------------------------------------------- activations
 // Both in fp32; `exact` keeps fp32's last places (fp32 tensors), otherwise the
-// hardware's exponential and reciprocal do (1 unit of fp32, far below a unit of
-// fp16 or bfloat16).
+// hardware's exponential and reciprocal do.  The hardware's exponential takes its
+// argument t times log2(e), rounded to fp32: up to about |t| 2^-24 of its value off
+// (2^-19 at t = 30), still far below a unit of fp16 or bfloat16.  dbias in fp32
+// carries it, which sums what was never rounded to them.
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kTanhScale = 0.79788456080286536f;      // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
