@@ -236,10 +236,11 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t index, c
 
 // One product.  Bound by the matrix cores in its main loop, by whole rounds of
 // tiles over the chip and, forward, by the writes between them: 8192 x 1600 x 6400
-// in bfloat16 211 to 218 us (about 780 TFLOP/s) with gelu and z kept, 162 and 188 us
-// (1030 and 890) for the two products of its backward pass.  The two of a pair have a kernel of their own: choosing between
-// them at run time costs the single one its arguments in scalar registers
-// (8192x1600x6400 forward, bf16: 211 us, against 227).
+// in bfloat16 211 to 222 us (760 to 800 TFLOP/s) with gelu and z kept, 162 to 167 and
+// 188 to 212 us (1030 to 790) for the two products of its backward pass.  The two of
+// a pair have a kernel of their own: choosing between them at run time costs the
+// single one its arguments in scalar registers (8192x1600x6400 forward, bf16: 211
+// us, against 227).
 template <typename G, typename TO, bool forward>
 __global__ __launch_bounds__(G::kThreads) void product(Product p) {
     extern __shared__ char lds[];
