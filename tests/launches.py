@@ -24,7 +24,8 @@ def build(folder):
 
 def run(recorder, check):
     """The check's output; raises with it where the check failed."""
-    env = dict(os.environ, LD_PRELOAD=recorder, HIP_RECORDER=recorder, PYTHONPATH=ROOT)
+    others = os.environ.get("LD_PRELOAD")  # stay, behind it
+    env = dict(os.environ, LD_PRELOAD=recorder + (":" + others if others else ""), HIP_RECORDER=recorder, PYTHONPATH=ROOT)
     p = subprocess.run([sys.executable, os.path.abspath(__file__), check], env=env, cwd=ROOT, text=True,
                        stdout=subprocess.PIPE, stderr=subprocess.STDOUT, timeout=300)
     assert p.returncode == 0, p.stdout[-4000:]
