@@ -592,6 +592,168 @@ int bytecomp_muon_step(int wdtype, int gdtype, const bc_param* t, int T, double 
                        double weight_decay, int steps, const double* coefficients, double eps, void* ws,
                        size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A block of experts: rows of a batch, each sent to k of many layers of its
+ * own, and the router that chooses them.  The conventions are the layers'.
+ * Whole numbers on the device (offsets, slots, rows) are int32; the library
+ * cannot check them on the host, and the kernels read and write nothing
+ * outside the tensors whatever they hold. */
+
+/* Router.  For each of `rows` rows of `experts` logits x, with
+ * p = softmax(x), the k largest logits (of equals the lower expert) in
+ * descending order: expert[row][j] and
+ *   weight[row][j] = normalise ? p_j / sum of the k chosen p : p_j.
+ * A logit of -inf is masked out: no probability, never chosen.  Where fewer than
+ * k are left, the rest of the k have expert -1, weight 0 and no slot (-1).  A NaN
+ * counts as the largest logit; it, or an infinity, makes its row's weights NaN.
+ * The choices, sorted by expert and by row within an expert, are numbered: the
+ * slots.
+ *   slot     [rows][k], the choice's place in that order, or -1
+ *   source   [rows * k], each slot's row; those behind the last slot are left
+ *            as they were
+ *   offsets  [experts + 1]: expert e has the slots offsets[e] to
+ *            offsets[e + 1] - 1
+ *   ws       4-byte aligned; NULL is fine where bytecomp_route_workspace_size
+ *            is 0
+ * 1 <= experts <= 1024, 1 <= k <= min(experts, 32) (BC_E_COUNT); rows < 2^29
+ * and rows * k < 2^31 (BC_E_SIZE).  Zero rows: offsets become zero. */
+int bytecomp_route_forward(int dtype, uint64_t rows, uint32_t experts, uint32_t k, const void* logits, uint64_t ld,
+                           int normalise, float* weight, int32_t* expert, int32_t* slot, int32_t* source,
+                           int32_t* offsets, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace of the call above (host only). */
+int bytecomp_route_workspace_size(uint64_t rows, uint32_t experts, uint32_t k, size_t* bytes);
+
+/* The logits' gradient from the weights':
+ *   normalised: dlogits_e = weight_e (dweight_e - sum_j weight_j dweight_j)
+ *   for the chosen experts, 0 for the others;
+ *   otherwise:  dlogits_e = p_e (dweight_e - sum_j p_j dweight_j), dweight_e 0
+ *   for those not chosen; 0 for a logit of -inf.
+ *   weight, expert  of the forward pass; a choice of -1 is passed over
+ *   logits     may be NULL when normalised */
+int bytecomp_route_backward(int dtype, uint64_t rows, uint32_t experts, uint32_t k, const void* logits, uint64_t ld,
+                            int normalise, const float* weight, const int32_t* expert, const float* dweight,
+                            void* dlogits, uint64_t ld_dlogits, void* stream);
+
+/* Combination of the experts' results:
+ *   out[row] = residual[row] + sum over j of weight[row][j] y[slot[row][j]],
+ * the terms added in the order of j; a slot outside [0, slots) adds nothing.
+ *   y         [slots, cols]
+ *   weight    NULL: 1 (the gradient of rows read through `source`)
+ *   residual  [rows, cols], or NULL: 0; may be out itself (same stride)
+ * 1 <= k <= 32 (BC_E_COUNT); rows < 2^29, slots < 2^31, cols < 2^24
+ * (BC_E_SIZE). */
+int bytecomp_combine_forward(int dtype, uint64_t rows, uint64_t cols, uint32_t k, uint64_t slots, const void* y,
+                             uint64_t ldy, const int32_t* slot, const float* weight, const void* residual,
+                             uint64_t ld_residual, void* out, uint64_t ld_out, void* stream);
+
+/* Its gradients: dy[slot[row][j]] = weight[row][j] dout[row] and
+ * dweight[row][j] = the inner product of dout[row] and y[slot[row][j]] (0
+ * where there is no slot); the residual's is dout.  No slot may be given twice.
+ *   dy, dweight  NULL: not wanted; rows of dy that are no slot of any row are
+ *                left as they were
+ *   y            may be NULL when dweight is not wanted */
+int bytecomp_combine_backward(int dtype, uint64_t rows, uint64_t cols, uint32_t k, uint64_t slots, const void* dout,
+                              uint64_t ld_dout, const void* y, uint64_t ldy, const int32_t* slot, const float* weight,
+                              void* dy, uint64_t lddy, float* dweight, void* stream);
+
+/* Linear layer grouped by expert.  Of the call's `rows` rows, those from
+ * offsets[e] to offsets[e + 1] - 1 (offsets on the device, ascending, at most
+ * `rows`) are expert e's:
+ *   z[r] = x[source ? source[r] : r] w_e^T + bias_e, y[r] = act(z[r]).
+ *   dtype     of every tensor
+ *   x         [rows, inner], or [x_rows, inner] with source; a source outside
+ *             [0, x_rows) gives a row of zeros
+ *   w         experts matrices [cols, inner], expert_w elements apart (at least
+ *             one matrix)
+ *   bias      [experts, cols], or NULL: 0
+ *   y, z      [rows, cols]; z NULL: not kept.  Rows before the first offset and
+ *             behind the last are left as they were.  y comes from the unrounded z.
+ *   ws        at least bytecomp_grouped_linear_workspace_size bytes, 16-byte
+ *             aligned; NULL is fine where that is 0
+ * fp32 products are sums of bfloat16 products of the operands' three parts,
+ * as the linear layer's; at most 64 rows are summed in fp32.
+ * 1 <= experts <= 1024 (BC_E_COUNT); rows < 2^22, x_rows < 2^31, inner and
+ * cols < 2^20, and as many elements as rows + 64 experts rows of inner or of cols,
+ * and as the weights, have: less than 2^35, with inner and cols as whole 64s
+ * (BC_E_SIZE).  Zero inner: the products are zero. */
+int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, uint32_t experts,
+                                    const int32_t* offsets, const void* x, uint64_t ldx, const int32_t* source,
+                                    uint64_t x_rows, const void* w, uint64_t ldw, uint64_t expert_w, const void* bias,
+                                    uint64_t ld_bias, int act, void* y, uint64_t ldy, void* z, uint64_t ldz, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Bytes of workspace that the forward (backward = 0) or backward pass needs at
+ * most, whatever the strides and alignment, with or without source (x_rows is
+ * checked as the calls check it; host only). */
+int bytecomp_grouped_linear_workspace_size(int dtype, uint64_t rows, uint64_t x_rows, uint64_t inner, uint64_t cols,
+                                           uint32_t experts, int backward, size_t* bytes);
+
+/* The gradients, with dz = dy act'(z) and e the row's expert:
+ *   dx[r] = dz[r] w_e  (in the order of the call's rows, also with source:
+ *           bytecomp_combine_forward without weights adds up those of a row of x),
+ *   dw_e = sum over e's rows of dz[r]^T x[source[r]], dbias_e = sum of dz[r].
+ *   gdtype  element type of dw and dbias: dtype or BC_F32
+ *   z       of the forward pass; may be NULL with BC_ACT_NONE
+ *   dx, dw, dbias  overwritten; NULL: not wanted.  dw: matrices expert_dw
+ *           elements apart.  An expert without rows has dw and dbias of zeros; rows
+ *           of dx before the first offset and behind the last are left as they were.
+ * In fp16 and bfloat16, dz is rounded to dtype for the products, as in the linear
+ * layer; dbias sums it unrounded. */
+int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inner, uint64_t cols,
+                                     uint32_t experts, const int32_t* offsets, const void* dy, uint64_t lddy,
+                                     const void* z, uint64_t ldz, int act, const void* x, uint64_t ldx,
+                                     const int32_t* source, uint64_t x_rows, const void* w, uint64_t ldw,
+                                     uint64_t expert_w, void* dx, uint64_t lddx, void* dw, uint64_t lddw,
+                                     uint64_t expert_dw, void* dbias, uint64_t ld_dbias, void* ws, size_t ws_bytes,
+                                     void* stream);
+
+/* Norm of a whole list of gradients, and clipping by it: between the aggregate
+ * and the optimizer step, for any kind of compression.  (The DGC step of the
+ * sparse kinds clips a worker's own gradients, before its momentum.)
+ *   BC_NORM_L2   norm = sqrt(sum of g^2): squares exact in fp64, summed in fp64
+ *                in a fixed order
+ *   BC_NORM_MAX  norm = max |g|; a NaN is the largest */
+enum bc_norm { BC_NORM_L2 = 0, BC_NORM_MAX = 1 };
+
+/* One gradient [rows, cols] of element type dtype (any mix in a list); out
+ * [rows, cols], of the same type, receives the clipped one and may be grad itself
+ * (same stride); the norm alone does not look at it. */
+typedef struct bc_grad {
+    const void* grad;
+    void* out;
+    uint64_t ld_grad, ld_out;
+    uint64_t rows, cols;
+    uint32_t dtype;
+    uint32_t reserved;
+} bc_grad;
+
+/* Bytes of workspace of the two calls below for T gradients (host only). */
+int bytecomp_grad_norm_workspace_size(int T, size_t* bytes);
+
+/* The norm of T gradients.
+ *   norm  device, one fp64 value
+ *   ws    16-byte aligned
+ * rows * cols < 2^48 (BC_E_SIZE); empty gradients are skipped, an empty list
+ * has norm 0.  Under stream capture the call writes its table into the workspace
+ * (further launches), so the graph stands by itself as long as the workspace
+ * does; graphs that share one must not run at the same time. */
+int bytecomp_grad_norm(const bc_grad* t, int T, int kind, double* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* Clips T gradients: c = norm > max_norm ? fl32(max_norm / norm) : 1,
+ * out = c g, the product in fp32 and rounded to the gradient's type.  In place
+ * and with c = 1 nothing is written.  A NaN norm clips nothing; an infinite one
+ * gives c = 0.
+ *   max_norm  >= 0 (BC_E_VALUE); +inf never clips
+ *   given     device, the norm to clip by, for a list that is only a part of the
+ *             model (with the squares of all parts' norms added up); NULL: the
+ *             norm of this list
+ *   norm, factor  device, receive the norm and c; NULL: not wanted.  norm may
+ *             be given itself
+ * Everything else is bytecomp_grad_norm's. */
+int bytecomp_clip_grads(const bc_grad* t, int T, int kind, double max_norm, const double* given, double* norm,
+                        float* factor, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

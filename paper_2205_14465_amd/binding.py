@@ -19,6 +19,7 @@ BC_TOPK, BC_TOPK_SAMPLED, BC_RANDK, BC_SIGN1 = 0, 1, 2, 3
 BC_TERNGRAD, BC_QSGD4, BC_QSGD8 = 4, 5, 6
 BC_F32, BC_F16, BC_BF16 = 0, 1, 2
 ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+NORM = {"l2": 0, "max": 1}
 KIND = {"topk": BC_TOPK, "topk_sampled": BC_TOPK_SAMPLED, "randk": BC_RANDK, "sign": BC_SIGN1,
         "terngrad": BC_TERNGRAD, "qsgd4": BC_QSGD4, "qsgd8": BC_QSGD8}
 # kinds whose payload is packed words plus one scale per tensor
@@ -47,6 +48,12 @@ class bc_param(ctypes.Structure):
     _fields_ = [("weight", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
                 ("ld_weight", ctypes.c_uint64), ("ld_grad", ctypes.c_uint64), ("ld_momentum", ctypes.c_uint64),
                 ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("scale", ctypes.c_double)]
+
+
+class bc_grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("ld_grad", ctypes.c_uint64),
+                ("ld_out", ctypes.c_uint64), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64),
+                ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 class BytecompError(RuntimeError):
@@ -143,6 +150,31 @@ def lib():
         L.bytecomp_muon_step.restype = i32
         L.bytecomp_muon_step.argtypes = [i32, i32, ctypes.POINTER(bc_param), i32, dbl, dbl, i32, dbl, i32, vp, dbl, vp,
                                          sz, vp]
+        u32 = ctypes.c_uint32
+        L.bytecomp_route_workspace_size.restype = i32
+        L.bytecomp_route_workspace_size.argtypes = [u64, u32, u32, ctypes.POINTER(sz)]
+        L.bytecomp_route_forward.restype = i32
+        L.bytecomp_route_forward.argtypes = [i32, u64, u32, u32, vp, u64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.bytecomp_route_backward.restype = i32
+        L.bytecomp_route_backward.argtypes = [i32, u64, u32, u32, vp, u64, i32, vp, vp, vp, vp, u64, vp]
+        L.bytecomp_combine_forward.restype = i32
+        L.bytecomp_combine_forward.argtypes = [i32, u64, u64, u32, u64, vp, u64, vp, vp, vp, u64, vp, u64, vp]
+        L.bytecomp_combine_backward.restype = i32
+        L.bytecomp_combine_backward.argtypes = [i32, u64, u64, u32, u64, vp, u64, vp, u64, vp, vp, vp, u64, vp, vp]
+        L.bytecomp_grouped_linear_workspace_size.restype = i32
+        L.bytecomp_grouped_linear_workspace_size.argtypes = [i32, u64, u64, u64, u64, u32, i32, ctypes.POINTER(sz)]
+        L.bytecomp_grouped_linear_forward.restype = i32
+        L.bytecomp_grouped_linear_forward.argtypes = [i32, u64, u64, u64, u32, vp, vp, u64, vp, u64, vp, u64, u64, vp, u64,
+                                                      i32, vp, u64, vp, u64, vp, sz, vp]
+        L.bytecomp_grouped_linear_backward.restype = i32
+        L.bytecomp_grouped_linear_backward.argtypes = [i32, i32, u64, u64, u64, u32, vp, vp, u64, vp, u64, i32, vp, u64, vp,
+                                                       u64, vp, u64, u64, vp, u64, vp, u64, u64, vp, u64, vp, sz, vp]
+        L.bytecomp_grad_norm_workspace_size.restype = i32
+        L.bytecomp_grad_norm_workspace_size.argtypes = [i32, ctypes.POINTER(sz)]
+        L.bytecomp_grad_norm.restype = i32
+        L.bytecomp_grad_norm.argtypes = [ctypes.POINTER(bc_grad), i32, i32, vp, vp, sz, vp]
+        L.bytecomp_clip_grads.restype = i32
+        L.bytecomp_clip_grads.argtypes = [ctypes.POINTER(bc_grad), i32, i32, dbl, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -889,3 +921,310 @@ def bytecomp_muon_step(weights, grads, momenta, lr, ws, momentum=0.95, nesterov=
     """One optimizer step, in place; see MuonCall."""
     MuonCall(weights, grads, momenta, ws, momentum, nesterov, weight_decay, scales, steps, coefficients, eps,
              stream)(lr)
+
+
+# ------------------------------------------------------- a block of experts
+# rows, experts and choices of each follow from the tensors' shapes; whole
+# numbers (slots, rows, offsets) are int32 tensors on the device.
+
+def _table(name, t, rows, cols, dtype):
+    """Pointer of a contiguous rows x cols tensor, None for None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (rows, cols) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {rows} x {cols} {dtype} device tensor, got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device}")
+    return t.data_ptr() if t.numel() else None
+
+
+def _stack(name, t, experts, rows, cols, dtype):
+    """(pointer, row stride, stride from matrix to matrix) of a tensor [experts, rows, cols]."""
+    if t is None:
+        return None, cols, rows * cols
+    if tuple(t.shape) != (experts, rows, cols) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: expected a {experts} x {rows} x {cols} {dtype} device tensor, got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device}")
+    if cols > 1 and t.stride(2) != 1 and t.numel():
+        raise ValueError(f"{name}: columns must be contiguous")
+    ld = t.stride(1) if rows > 1 else cols
+    each = t.stride(0) if experts > 1 else max(rows - 1, 0) * ld + cols
+    if ld < cols or each < max(rows - 1, 0) * ld + cols:
+        raise ValueError(f"{name}: strides {tuple(t.stride())} of {rows} x {cols} matrices that overlap")
+    return (t.data_ptr() if t.numel() else None), ld, each
+
+
+def bytecomp_route_workspace_size(rows, experts, k):
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_route_workspace_size",
+           lib().bytecomp_route_workspace_size(int(rows), int(experts), int(k), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_route_workspace(rows, experts, k, device="cuda"):
+    return _alloc_bytes(bytecomp_route_workspace_size(rows, experts, k), device)
+
+
+class RouteCall(_Call):
+    """bytecomp_route_forward: of logits [rows, experts] the k largest of each
+    row: weight (fp32), expert and slot (int32) [rows, k], source [rows * k] and
+    offsets [experts + 1] (int32); ws from alloc_route_workspace."""
+
+    def __init__(self, logits, weight, expert, slot, source, offsets, ws, normalise=True, stream=None):
+        import torch
+        rows, experts = logits.shape
+        k = weight.shape[1]
+        pl, ld = _matrix("logits", logits, rows, experts, logits.dtype)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_route_forward",
+                         (_dtype(logits), rows, experts, k, pl, ld, int(bool(normalise)),
+                          _table("weight", weight, rows, k, torch.float32), _table("expert", expert, rows, k, torch.int32),
+                          _table("slot", slot, rows, k, torch.int32), _vector("source", source, rows * k, torch.int32),
+                          _vector("offsets", offsets, experts + 1, torch.int32), p, n, _stream_handle(stream)),
+                         (logits, weight, expert, slot, source, offsets, ws))
+
+
+class RouteGradCall(_Call):
+    """bytecomp_route_backward: dlogits [rows, experts] from dweight [rows, k] and
+    the weight and expert of a RouteCall with these logits and this normalise
+    (normalised, logits give the type alone and may be dlogits)."""
+
+    def __init__(self, logits, weight, expert, dweight, dlogits, normalise=True, stream=None):
+        import torch
+        rows, experts = logits.shape
+        k = weight.shape[1]
+        pl, ld = _matrix("logits", logits, rows, experts, logits.dtype)
+        pd, ldd = _matrix("dlogits", dlogits, rows, experts, logits.dtype)
+        super().__init__("bytecomp_route_backward",
+                         (_dtype(logits), rows, experts, k, pl, ld, int(bool(normalise)),
+                          _table("weight", weight, rows, k, torch.float32), _table("expert", expert, rows, k, torch.int32),
+                          _table("dweight", dweight, rows, k, torch.float32), pd, ldd, _stream_handle(stream)),
+                         (logits, weight, expert, dweight, dlogits))
+
+
+class CombineCall(_Call):
+    """bytecomp_combine_forward: out [rows, cols] = residual (None: 0) + the rows
+    slot [rows, k] of y [slots, cols], times weight [rows, k] (None: 1)."""
+
+    def __init__(self, y, slot, weight, residual, out, stream=None):
+        import torch
+        slots, cols = y.shape
+        rows, k = slot.shape
+        py, ldy = _matrix("y", y, slots, cols, y.dtype)
+        pr, ldr = _matrix("residual", residual, rows, cols, y.dtype)
+        po, ldo = _matrix("out", out, rows, cols, y.dtype)
+        super().__init__("bytecomp_combine_forward",
+                         (_dtype(y), rows, cols, k, slots, py, ldy, _table("slot", slot, rows, k, torch.int32),
+                          _table("weight", weight, rows, k, torch.float32), pr, ldr, po, ldo, _stream_handle(stream)),
+                         (y, slot, weight, residual, out))
+
+
+class CombineGradCall(_Call):
+    """bytecomp_combine_backward: dy [slots, cols] and dweight [rows, k] (None: not
+    wanted) from dout [rows, cols]; y [slots, cols] may be None without dweight."""
+
+    def __init__(self, dout, y, slot, weight, dy, dweight, stream=None):
+        import torch
+        rows, cols = dout.shape
+        k = slot.shape[1]
+        like = next((t for t in (dy, y) if t is not None), None)
+        slots = 0 if like is None else like.shape[0]
+        pd, ldd = _matrix("dout", dout, rows, cols, dout.dtype)
+        py, ldy = _matrix("y", y, slots, cols, dout.dtype)
+        pdy, lddy = _matrix("dy", dy, slots, cols, dout.dtype)
+        super().__init__("bytecomp_combine_backward",
+                         (_dtype(dout), rows, cols, k, slots, pd, ldd, py, ldy,
+                          _table("slot", slot, rows, k, torch.int32), _table("weight", weight, rows, k, torch.float32), pdy,
+                          lddy, _table("dweight", dweight, rows, k, torch.float32), _stream_handle(stream)),
+                         (dout, y, slot, weight, dy, dweight))
+
+
+def bytecomp_route_forward(logits, weight, expert, slot, source, offsets, ws, normalise=True, stream=None):
+    """The k experts of every row and their order; see RouteCall."""
+    RouteCall(logits, weight, expert, slot, source, offsets, ws, normalise, stream)()
+
+
+def bytecomp_route_backward(logits, weight, expert, dweight, dlogits, normalise=True, stream=None):
+    """The gradient of bytecomp_route_forward's weights; see RouteGradCall."""
+    RouteGradCall(logits, weight, expert, dweight, dlogits, normalise, stream)()
+
+
+def bytecomp_combine_forward(y, slot, weight, residual, out, stream=None):
+    """out = residual + the weighted sum of each row's slots; see CombineCall."""
+    CombineCall(y, slot, weight, residual, out, stream)()
+
+
+def bytecomp_combine_backward(dout, y, slot, weight, dy, dweight, stream=None):
+    """The gradients of bytecomp_combine_forward; see CombineGradCall."""
+    CombineGradCall(dout, y, slot, weight, dy, dweight, stream)()
+
+
+def bytecomp_grouped_linear_workspace_size(dtype, rows, x_rows, inner, cols, experts, backward=False):
+    """dtype: BC_F32, BC_F16 or BC_BF16."""
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_grouped_linear_workspace_size",
+           lib().bytecomp_grouped_linear_workspace_size(int(dtype), int(rows), int(x_rows), int(inner), int(cols),
+                                                        int(experts), int(bool(backward)), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_grouped_linear_workspace(x, w, rows, backward=False):
+    """Workspace for the layer's forward or backward pass on `rows` rows (of x, or
+    read from it through a source) and w [experts, cols, inner]."""
+    experts, cols, inner = w.shape
+    return _alloc_bytes(bytecomp_grouped_linear_workspace_size(_dtype(x), rows, x.shape[0], inner, cols, experts,
+                                                               backward), x.device)
+
+
+class GroupedLinearCall(_Call):
+    """bytecomp_grouped_linear_forward: y [rows, cols] = act(x w_e^T + bias_e) for the
+    rows from offsets[e] to offsets[e + 1] of every e, with w [experts, cols,
+    inner] and bias [experts, cols]; x [rows, inner], or through source [rows] of
+    any number of rows.  bias, source and z may be None; activation: a key of
+    ACTIVATION; ws from alloc_grouped_linear_workspace (None for at most 64 rows)."""
+
+    def __init__(self, x, source, offsets, w, bias, activation, y, z=None, ws=None, stream=None):
+        import torch
+        experts, cols, inner = w.shape
+        rows, dt = y.shape[0], x.dtype
+        x_rows = rows if source is None else x.shape[0]
+        px, ldx = _matrix("x", x, x_rows, inner, dt)
+        pwt, ldw, each = _stack("w", w, experts, cols, inner, dt)
+        pb, ldb = _matrix("bias", bias, experts, cols, dt)
+        py, ldy = _matrix("y", y, rows, cols, dt)
+        pz, ldz = _matrix("z", z, rows, cols, dt)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_grouped_linear_forward",
+                         (_dtype(x), rows, inner, cols, experts, _vector("offsets", offsets, experts + 1, torch.int32), px,
+                          ldx, _vector("source", source, rows, torch.int32), x_rows, pwt, ldw, each, pb, ldb,
+                          _activation(activation), py, ldy, pz, ldz, p, n, _stream_handle(stream)),
+                         (x, source, offsets, w, bias, y, z, ws))
+
+
+class GroupedLinearGradCall(_Call):
+    """bytecomp_grouped_linear_backward: dx [rows, inner], dw [experts, cols, inner]
+    and dbias [experts, cols] (None: not wanted) of a GroupedLinearCall with this
+    x, source, offsets, w, activation and z.  dw and dbias in x's type or fp32; ws
+    from alloc_grouped_linear_workspace(x, w, rows, backward=True)."""
+
+    def __init__(self, dy, z, x, source, offsets, w, activation, dx, dw, dbias, ws, stream=None):
+        import torch
+        experts, cols, inner = w.shape
+        rows, dt = dy.shape[0], x.dtype
+        x_rows = rows if source is None else x.shape[0]
+        pdy, lddy = _matrix("dy", dy, rows, cols, dt)
+        pz, ldz = _matrix("z", z, rows, cols, dt)
+        px, ldx = _matrix("x", x, x_rows, inner, dt)
+        pwt, ldw, each = _stack("w", w, experts, cols, inner, dt)
+        pdx, lddx = _matrix("dx", dx, rows, inner, dt)
+        gd = next((t for t in (dw, dbias) if t is not None), x)
+        pdw, lddw, each_d = _stack("dw", dw, experts, cols, inner, gd.dtype)
+        pdb, lddb = _matrix("dbias", dbias, experts, cols, gd.dtype)
+        p, n = _ws(ws)
+        super().__init__("bytecomp_grouped_linear_backward",
+                         (_dtype(x), _dtype(gd), rows, inner, cols, experts,
+                          _vector("offsets", offsets, experts + 1, torch.int32), pdy, lddy, pz, ldz,
+                          _activation(activation), px, ldx, _vector("source", source, rows, torch.int32), x_rows, pwt, ldw,
+                          each, pdx, lddx, pdw, lddw, each_d, pdb, lddb, p, n, _stream_handle(stream)),
+                         (dy, z, x, source, offsets, w, dx, dw, dbias, ws))
+
+
+def bytecomp_grouped_linear_forward(x, source, offsets, w, bias, activation, y, z=None, ws=None, stream=None):
+    """y = act(x w_e^T + bias_e), e each row's expert; see GroupedLinearCall."""
+    GroupedLinearCall(x, source, offsets, w, bias, activation, y, z, ws, stream)()
+
+
+def bytecomp_grouped_linear_backward(dy, z, x, source, offsets, w, activation, dx, dw, dbias, ws, stream=None):
+    """The gradients of bytecomp_grouped_linear_forward; see GroupedLinearGradCall."""
+    GroupedLinearGradCall(dy, z, x, source, offsets, w, activation, dx, dw, dbias, ws, stream)()
+
+
+# ------------------------------------------------ norm and clipping of a list
+
+def bytecomp_grad_norm_workspace_size(T):
+    out = ctypes.c_size_t(0)
+    _check("bytecomp_grad_norm_workspace_size", lib().bytecomp_grad_norm_workspace_size(int(T), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_grad_norm_workspace(grads):
+    """Workspace for the norm and the clipping of a list of gradients."""
+    return _alloc_bytes(bytecomp_grad_norm_workspace_size(len(grads)), grads[0].device if grads else "cuda")
+
+
+def _norm_kind(kind):
+    if kind not in NORM:
+        raise ValueError(f"norm {kind!r}: one of {', '.join(NORM)}")
+    return NORM[kind]
+
+
+def _grad_rows(name, t):
+    """(rows, cols, row stride) of a contiguous tensor, or of a matrix with contiguous columns."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a device tensor, got one on {t.device}")
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() != 2:
+        raise ValueError(f"{name}: neither contiguous nor a matrix: shape {tuple(t.shape)}, strides {tuple(t.stride())}")
+    rows, cols = t.shape
+    return (rows, cols, _matrix(name, t, rows, cols, t.dtype)[1])
+
+
+def _grad_list(grads, outs):
+    arr = (bc_grad * max(len(grads), 1))()
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} grads, {len(outs)} outs")
+    for i, g in enumerate(grads):
+        rows, cols, ld = _grad_rows(f"grads[{i}]", g)
+        arr[i].grad, arr[i].ld_grad, arr[i].rows, arr[i].cols = g.data_ptr() if g.numel() else None, ld, rows, cols
+        arr[i].dtype = _dtype(g)
+        if outs is None:
+            continue
+        o = outs[i]
+        if tuple(o.shape) != tuple(g.shape) or o.dtype != g.dtype:
+            raise ValueError(f"outs[{i}]: expected {tuple(g.shape)} {g.dtype}, got {tuple(o.shape)} {o.dtype}")
+        o_rows, o_cols, o_ld = _grad_rows(f"outs[{i}]", o)
+        if o_rows != rows:  # one of the two is contiguous: both as matrices
+            rows, cols = g.shape
+            arr[i].rows, arr[i].cols = rows, cols
+            arr[i].ld_grad = _matrix(f"grads[{i}]", g, rows, cols, g.dtype)[1]
+            o_ld = _matrix(f"outs[{i}]", o, rows, cols, g.dtype)[1]
+        arr[i].out, arr[i].ld_out = o.data_ptr() if o.numel() else None, o_ld
+    return arr
+
+
+class GradNormCall(_Call):
+    """bytecomp_grad_norm: norm (one fp64 value) of a list of gradients of any types,
+    contiguous or matrices with a row stride.  kind: a key of NORM; ws from
+    alloc_grad_norm_workspace."""
+
+    def __init__(self, grads, norm, ws, kind="l2", stream=None):
+        import torch
+        p, n = _ws(ws)
+        super().__init__("bytecomp_grad_norm",
+                         (_grad_list(grads, None), len(grads), _norm_kind(kind), _vector("norm", norm, 1, torch.float64),
+                          p, n, _stream_handle(stream)), (grads, norm, ws))
+
+
+class ClipGradsCall(_Call):
+    """bytecomp_clip_grads: outs[i] (which may be grads[i]) = grads[i] times
+    min(1, max_norm / norm), the norm that of the list, or `given` (one fp64 value);
+    norm (one fp64 value) and factor (one fp32 value) receive both, or None."""
+
+    def __init__(self, grads, outs, max_norm, ws, kind="l2", given=None, norm=None, factor=None, stream=None):
+        import torch
+        p, n = _ws(ws)
+        super().__init__("bytecomp_clip_grads",
+                         (_grad_list(grads, outs), len(grads), _norm_kind(kind), float(max_norm),
+                          _vector("given", given, 1, torch.float64), _vector("norm", norm, 1, torch.float64),
+                          _vector("factor", factor, 1, torch.float32), p, n, _stream_handle(stream)),
+                         (grads, outs, ws, given, norm, factor))
+
+
+def bytecomp_grad_norm(grads, norm, ws, kind="l2", stream=None):
+    """The norm of a list of gradients; see GradNormCall."""
+    GradNormCall(grads, norm, ws, kind, stream)()
+
+
+def bytecomp_clip_grads(grads, outs, max_norm, ws, kind="l2", given=None, norm=None, factor=None, stream=None):
+    """A list of gradients clipped by its norm; see ClipGradsCall."""
+    ClipGradsCall(grads, outs, max_norm, ws, kind, given, norm, factor, stream)()

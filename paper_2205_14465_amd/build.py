@@ -16,7 +16,8 @@ BUILD = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "kernels_sign.hip", "kernels_topk.hip", "kernels_randk.hip", "kernels_agg_sparse.hip",
            "kernels_agg_sign.hip", "kernels_resid.hip", "kernels_part.hip", "kernels_quant.hip",
            "kernels_dgc.hip", "noalloc.hip", "cpu_ops.hip", "plan_sim.hip", "api_layers.hip",
-           "kernels_layernorm.hip", "kernels_linear.hip", "kernels_ortho.hip"]
+           "kernels_layernorm.hip", "kernels_linear.hip", "kernels_ortho.hip", "api_experts.hip", "kernels_route.hip",
+           "kernels_grouped.hip", "kernels_clip.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

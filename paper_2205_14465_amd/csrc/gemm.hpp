@@ -313,7 +313,7 @@ struct GemmTile {
                     make_float4(acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]);
     }
 
-  private:
+  protected:
     // Byte offset of what this lane loads with the wave's load instruction for
     // row group g.
     static __device__ __forceinline__ uint32_t lane_offset(int g, int lane, uint32_t rows, uint32_t ld) {

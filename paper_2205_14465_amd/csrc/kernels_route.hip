@@ -1,0 +1,495 @@
+// kernels_route.hip -- the router of a block of experts and the combination of
+// the experts' results.
+//
+// Router: for each row x of logits, p = softmax(x); the k largest (ties to the
+// lower expert), their weights p_j, or p_j over the chosen ones' sum; then the
+// order of the choices by expert, and by row within an expert.  A logit of -inf
+// has no probability and is never chosen.
+//
+// The order is a count: route_gate gives each choice its rank among those of
+// the same expert in its block of rows (a bit mask of the block's rows for each
+// expert, so that the rank is a count of bits and no order of atomics shows),
+// route_scan adds the blocks' counts up, route_place adds what lies before.
+//
+// Combination: out = residual + sum_j weight_j y[slot_j], the sum in fp32 in the
+// order of j, and its gradient.  Bound by memory: a row's results are k whole
+// rows elsewhere.
+#include "common.hpp"
+#include "experts.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace bc {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Order of logits as unsigned numbers: -inf 0, then ascending; zeros are equal, a
+// NaN is the largest.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x != x) return 0xffffffffu;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
+    return o - 0x007fffffu;  // -inf's
+}
+
+// A row of logits over G lanes, V consecutive ones each.
+template <typename T, int V>
+__device__ __forceinline__ void load_logits(const T* row, uint32_t experts, uint32_t lane, bool there, float (&x)[V]) {
+    const uint32_t e = lane * V;
+    const int left = there && e < experts ? (int)(experts - e) : 0;
+    load_vec(row + (left > 0 ? e : 0), left, x);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i >= left) x[i] = -INFINITY;
+}
+
+template <int G>
+__device__ __forceinline__ float group_sum(float x) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+template <int G>
+__device__ __forceinline__ uint64_t group_max(uint64_t x) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) {
+        const uint64_t y = __shfl_xor(x, o, 64);
+        x = x > y ? x : y;
+    }
+    return x;
+}
+
+// exp(x - top), 0 for a logit that is masked out (also where all of them are).
+__device__ __forceinline__ float chance(float x, float top) { return x == -INFINITY ? 0.0f : expf(x - top); }
+
+// Writes a block's choices: weight and expert of its rows, their ranks (slot),
+// and, in LDS, the mask of the rows of each expert.
+template <typename T, int G, int V>
+__device__ __forceinline__ void gate_rows(const Route& a, uint64_t row0, uint32_t rows, uint32_t words, uint32_t* mask) {
+    constexpr uint32_t kRows = kThreads / G;
+    const uint32_t lane = threadIdx.x % G;
+    for (uint32_t r0 = 0; r0 < rows; r0 += kRows) {
+        const uint32_t r = r0 + threadIdx.x / G;
+        const bool there = r < rows;
+        const uint64_t row = row0 + (there ? r : 0);
+        float x[V];
+        load_logits<T, V>((const T*)a.logits + row * a.ld, a.experts, lane, there, x);
+        uint32_t left = (1u << V) - 1;  // not chosen yet
+        float top = 0.0f, chosen = 0.0f, all = 1.0f, mine = 0.0f;
+        int32_t e_mine = -1;
+        for (uint32_t j = 0; j < a.k; ++j) {
+            uint64_t best = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t o = order_of(x[i]);
+                const uint64_t key = (uint64_t)o << 32 | (0xffffffffu - (lane * V + i));
+                if ((left >> i & 1) && o != 0 && key > best) best = key;
+            }
+            best = group_max<G>(best);
+            const uint32_t e = 0xffffffffu - (uint32_t)best;
+            const bool found = best != 0;
+            // the chosen logit, from the lane that holds it
+            float value = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (found && e == lane * V + i) {
+                    value = x[i];
+                    left &= ~(1u << i);
+                }
+            value = __shfl(value, (int)((threadIdx.x & 63) / G * G + (found ? e / V : 0)), 64);
+            if (j == 0) {
+                top = value;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum += chance(x[i], top);
+                all = group_sum<G>(sum);
+            }
+            const float p = found ? expf(value - top) : 0.0f;
+            chosen += p;
+            if (lane == j % G) {
+                mine = p;
+                e_mine = found ? (int32_t)e : -1;
+            }
+            if (j % G == G - 1 || j + 1 == a.k) {
+                // G choices, one a lane (a lane's weight is divided when the sum is known)
+                const uint32_t at = j - j % G + lane;
+                if (there && at <= j) {
+                    a.weight[row * a.k + at] = mine;
+                    a.expert[row * a.k + at] = e_mine;
+                    if (e_mine >= 0) atomicOr(&mask[(uint32_t)e_mine * words + r / 32], 1u << (r % 32));
+                }
+            }
+        }
+        // a row without a chosen expert has weights of 0 and nothing to divide by
+        const float by = a.normalise ? chosen : all;
+        if (there)
+            for (uint32_t j = lane; j < a.k; j += G) {
+                const float p = a.weight[row * a.k + j];
+                a.weight[row * a.k + j] = by == 0.0f ? 0.0f : p / by;
+            }
+    }
+}
+
+// Rank of row r in the mask of one expert.
+__device__ __forceinline__ uint32_t rank_of(const uint32_t* mask, uint32_t r) {
+    uint32_t n = 0;
+    for (uint32_t w = 0; w < r / 32; ++w) n += __popc(mask[w]);
+    return n + __popc(mask[r / 32] & ((1u << (r % 32)) - 1));
+}
+
+template <typename T, int G, int V>
+__global__ __launch_bounds__(kThreads) void route_gate(Route a) {
+    extern __shared__ uint32_t mask[];
+    const uint64_t row0 = (uint64_t)blockIdx.x * a.block_rows;
+    const uint32_t rows = a.rows - row0 < a.block_rows ? (uint32_t)(a.rows - row0) : a.block_rows;
+    const uint32_t words = a.block_rows / 32;
+    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kThreads) mask[i] = 0;
+    __syncthreads();
+    gate_rows<T, G, V>(a, row0, rows, words, mask);
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kThreads) {
+        uint32_t n = 0;
+        for (uint32_t w = 0; w < words; ++w) n += __popc(mask[e * words + w]);
+        a.count[(uint64_t)e * a.blocks + blockIdx.x] = n;
+    }
+    for (uint32_t i = threadIdx.x; i < rows * a.k; i += kThreads) {
+        const int32_t e = a.expert[row0 * a.k + i];
+        a.slot[row0 * a.k + i] = e < 0 ? -1 : (int32_t)rank_of(mask + (uint32_t)e * words, i / a.k);
+    }
+}
+
+// Exclusive sums of x over a workgroup; *total: the sum.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* total) {
+    __shared__ uint32_t sh[kThreads / 64];
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(s, o, 64);
+        if (lane >= (uint32_t)o) s += y;
+    }
+    __syncthreads();
+    if (lane == 63) sh[threadIdx.x >> 6] = s;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 64; ++w) {
+        if (w < threadIdx.x >> 6) before += sh[w];
+        all += sh[w];
+    }
+    *total = all;
+    return before + s - x;
+}
+
+// A workgroup an expert: its blocks' counts become what lies before each of them.
+__global__ __launch_bounds__(kThreads) void route_scan(Route a) {
+    uint32_t* c = a.count + (uint64_t)blockIdx.x * a.blocks;
+    uint32_t sum = 0;
+    for (uint32_t b0 = 0; b0 < a.blocks; b0 += kThreads) {
+        const uint32_t b = b0 + threadIdx.x;
+        uint32_t total;
+        const uint32_t before = block_scan(b < a.blocks ? c[b] : 0, &total);
+        if (b < a.blocks) c[b] = sum + before;
+        sum += total;
+    }
+    if (threadIdx.x == 0) a.count[(uint64_t)a.experts * a.blocks + blockIdx.x] = sum;
+}
+
+// Offsets of the experts from their totals, into LDS.
+template <typename F>
+__device__ __forceinline__ void offsets_of(uint32_t experts, uint32_t* offsets, F total_of) {
+    uint32_t sum = 0;
+    for (uint32_t e0 = 0; e0 < experts; e0 += kThreads) {
+        const uint32_t e = e0 + threadIdx.x;
+        uint32_t total;
+        const uint32_t before = block_scan(e < experts ? total_of(e) : 0, &total);
+        if (e < experts) offsets[e] = sum + before;
+        sum += total;
+    }
+    if (threadIdx.x == 0) offsets[experts] = sum;
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kThreads) void route_place(Route a) {
+    __shared__ uint32_t offsets[kMaxExperts + 1];
+    const uint64_t row0 = (uint64_t)blockIdx.x * a.block_rows;
+    const uint32_t rows = a.rows - row0 < a.block_rows ? (uint32_t)(a.rows - row0) : a.block_rows;
+    offsets_of(a.experts, offsets, [&](uint32_t e) { return a.count[(uint64_t)a.experts * a.blocks + e]; });
+    if (blockIdx.x == 0)
+        for (uint32_t e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = (int32_t)offsets[e];
+    for (uint32_t i = threadIdx.x; i < rows * a.k; i += kThreads) {
+        const uint64_t at = row0 * a.k + i;
+        const int32_t e = a.expert[at];
+        if (e < 0) continue;
+        const uint32_t slot = offsets[e] + a.count[(uint64_t)e * a.blocks + blockIdx.x] + (uint32_t)a.slot[at];
+        a.slot[at] = (int32_t)slot;
+        a.source[slot] = (int32_t)(row0 + i / a.k);
+    }
+}
+
+// All of it in one workgroup.
+template <typename T, int G, int V>
+__global__ __launch_bounds__(kThreads) void route_small(Route a) {
+    extern __shared__ uint32_t mask[];
+    __shared__ uint32_t offsets[kMaxExperts + 1];
+    const uint32_t rows = (uint32_t)a.rows, words = a.block_rows / 32;
+    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kThreads) mask[i] = 0;
+    __syncthreads();
+    gate_rows<T, G, V>(a, 0, rows, words, mask);
+    __syncthreads();
+    offsets_of(a.experts, offsets, [&](uint32_t e) {
+        uint32_t n = 0;
+        for (uint32_t w = 0; w < words; ++w) n += __popc(mask[e * words + w]);
+        return n;
+    });
+    for (uint32_t e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = (int32_t)offsets[e];
+    for (uint32_t i = threadIdx.x; i < rows * a.k; i += kThreads) {
+        const int32_t e = a.expert[i];
+        if (e < 0) {
+            a.slot[i] = -1;
+            continue;
+        }
+        const uint32_t slot = offsets[e] + rank_of(mask + (uint32_t)e * words, i / a.k);
+        a.slot[i] = (int32_t)slot;
+        a.source[slot] = (int32_t)(i / a.k);
+    }
+}
+
+// dlogits: normalised over the chosen, w_e (dw_e - sum_j w_j dw_j) for them;
+// otherwise p_e ([chosen] dw_e - sum_j p_j dw_j).  Logits of -inf get 0, whatever
+// the sum is.
+template <typename T, int G, int V>
+__device__ __forceinline__ void grad_row(const RouteGrad& a, uint64_t row, uint32_t lane) {
+    const bool there = row < a.rows;
+    float up[V], p[V];
+    bool live[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        up[i] = p[i] = 0.0f;
+        live[i] = false;
+    }
+    float dot = 0.0f;
+    for (uint32_t j = 0; j < a.k; ++j) {
+        const uint64_t at = there ? row * a.k + j : 0;
+        const int32_t e = there ? a.expert[at] : -1;
+        if (e < 0 || (uint32_t)e >= a.experts) continue;
+        const float w = a.weight[at], d = a.dweight[at];
+        dot += w * d;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if ((uint32_t)e == lane * V + i) {
+                up[i] = d;
+                p[i] = w;
+                live[i] = true;
+            }
+    }
+    if (!a.normalise) {
+        float x[V], top = -INFINITY, sum = 0.0f;
+        load_logits<T, V>((const T*)a.logits + (there ? row : 0) * a.ld, a.experts, lane, there, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = x[i] > top || x[i] != x[i] ? x[i] : top;
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) {
+            const float y = __shfl_xor(top, o, 64);
+            top = y > top || y != y ? y : top;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            live[i] = x[i] != -INFINITY;
+            sum += p[i] = chance(x[i], top);
+        }
+        sum = group_sum<G>(sum);
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[i] /= sum;  // 0 / 0 where nothing is live
+    }
+    const uint32_t e = lane * V;
+    if (!there || e >= a.experts) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = live[i] ? p[i] * (up[i] - dot) : 0.0f;
+    store_vec((T*)a.dlogits + row * a.ld_d + e, (int)(a.experts - e), p);
+}
+
+template <typename T, int G, int V>
+__global__ __launch_bounds__(kThreads) void route_grad(RouteGrad a) {
+    constexpr uint32_t kRows = kThreads / G;
+    // (the lanes of a wave go round together: the sums need every one of them)
+    for (uint64_t row0 = (uint64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (uint64_t)gridDim.x * kRows)
+        grad_row<T, G, V>(a, row0 + threadIdx.x / G, threadIdx.x % G);
+}
+
+// ------------------------------------------------------------ combination
+// Lanes of a row: a power of two that its pieces of eight fill, up to a workgroup.
+inline uint32_t row_lanes(uint32_t cols) {
+    uint32_t n = 1;
+    while (n < kThreads && n * 8 < cols) n *= 2;
+    return n;
+}
+
+template <typename T, bool kWhole>
+__device__ __forceinline__ void combine_row(const Combine& a, uint64_t row, uint32_t from, uint32_t step) {
+    for (uint32_t c = from; c < a.cols; c += step) {
+        const int left = (int)(a.cols - c);
+        float sum[8];
+        if (a.residual) {
+            load_vec<kWhole>((const T*)a.residual + row * a.ldr + c, left, sum);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+        }
+        for (uint32_t j = 0; j < a.k; ++j) {
+            const uint32_t slot = (uint32_t)a.slot[row * a.k + j];
+            if (slot >= a.slots) continue;  // none
+            const float w = a.weight ? a.weight[row * a.k + j] : 1.0f;
+            float y[8];
+            load_vec<kWhole>((const T*)a.y + slot * a.ldy + c, left, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += w * y[i];
+        }
+        store_vec((T*)a.out + row * a.ld_out + c, left, sum, a.nt);
+    }
+}
+
+template <typename T, bool kWhole>
+__global__ __launch_bounds__(kThreads) void combine(Combine a, uint32_t lanes) {
+    const uint64_t step = (uint64_t)gridDim.x * kThreads / lanes;
+    for (uint64_t row = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / lanes; row < a.rows; row += step)
+        combine_row<T, kWhole>(a, row, threadIdx.x % lanes * 8, lanes * 8);
+}
+
+// dy[slot_j] = weight_j dout, dweight_j = <dout, y[slot_j]>: a wave a row, its
+// part of dout read once for each choice (from the caches after the first).
+template <typename T, bool kWhole>
+__global__ __launch_bounds__(kThreads) void combine_grad(CombineGrad a) {
+    const uint32_t lane = threadIdx.x & 63;
+    constexpr uint32_t kRows = kThreads / 64;
+    const uint64_t first = (uint64_t)blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (uint64_t row = first; row < a.rows; row += (uint64_t)gridDim.x * kRows)
+    for (uint32_t j = 0; j < a.k; ++j) {
+        const uint32_t slot = (uint32_t)a.slot[row * a.k + j];
+        float dot = 0.0f;
+        if (slot < a.slots) {
+            const float w = a.weight ? a.weight[row * a.k + j] : 1.0f;
+            for (uint32_t c = lane * 8; c < a.cols; c += 64 * 8) {
+                const int left = (int)(a.cols - c);
+                float d[8], y[8];
+                load_vec<kWhole>((const T*)a.dout + row * a.ldd + c, left, d);
+                if (a.dweight) {
+                    load_vec<kWhole>((const T*)a.y + slot * a.ldy + c, left, y);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dot = fmaf(d[i], y[i], dot);
+                }
+                if (a.dy) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] *= w;
+                    store_vec((T*)a.dy + slot * a.lddy + c, left, d, a.nt);
+                }
+            }
+        }
+        if (a.dweight) {
+            dot = wave_sum(dot);
+            if (lane == 0) a.dweight[row * a.k + j] = dot;
+        }
+    }
+}
+
+// Workgroups of a launch whose kernel goes round: HIP takes fewer than 2^32 threads.
+uint32_t capped(uint64_t blocks) { return (uint32_t)std::min<uint64_t>(blocks, 1u << 22); }
+
+// Calls fn(G, V) as constants for this many experts.
+template <typename F>
+hipError_t with_group(uint32_t experts, F fn) {
+    using std::integral_constant;
+    if (experts <= 8) return fn(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    if (experts <= 16) return fn(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+    if (experts <= 32) return fn(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+    if (experts <= 64) return fn(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+    if (experts <= 128) return fn(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    if (experts <= 256) return fn(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+    if (experts <= 512) return fn(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+    return fn(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+}
+
+template <typename T>
+hipError_t route_of(const Route& a, hipStream_t s) {
+    return with_group(a.experts, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value;
+        const size_t lds = (size_t)a.experts * (a.block_rows / 32) * 4;
+        if (a.blocks == 1) {
+            hipLaunchKernelGGL((route_small<T, G, V>), dim3(1), dim3(kThreads), lds, s, a);
+            return hipGetLastError();
+        }
+        hipLaunchKernelGGL((route_gate<T, G, V>), dim3(a.blocks), dim3(kThreads), lds, s, a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(route_scan, dim3(a.experts), dim3(kThreads), 0, s, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(route_place, dim3(a.blocks), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t route_grad_of(const RouteGrad& a, hipStream_t s) {
+    return with_group(a.experts, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value;
+        const uint64_t blocks = (a.rows + kThreads / G - 1) / (kThreads / G);
+        hipLaunchKernelGGL((route_grad<T, G, V>), dim3(capped(blocks)), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t combine_of(const Combine& a, hipStream_t s) {
+    const uint32_t lanes = row_lanes(a.cols);
+    const uint64_t blocks = (a.rows * lanes + kThreads - 1) / kThreads;
+    if (a.cols % 8 == 0) hipLaunchKernelGGL((combine<T, true>), dim3(capped(blocks)), dim3(kThreads), 0, s, a, lanes);
+    else hipLaunchKernelGGL((combine<T, false>), dim3(capped(blocks)), dim3(kThreads), 0, s, a, lanes);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t combine_grad_of(const CombineGrad& a, hipStream_t s) {
+    const uint64_t blocks = (a.rows + kThreads / 64 - 1) / (kThreads / 64);
+    if (a.cols % 8 == 0) hipLaunchKernelGGL((combine_grad<T, true>), dim3(capped(blocks)), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((combine_grad<T, false>), dim3(capped(blocks)), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Rows of a workgroup of route_gate: 64, more where there would be more than 256
+// workgroups and the masks of the experts (a bit a row) leave room.
+uint32_t route_block_rows(uint64_t rows, uint32_t experts) {
+    uint32_t n = 64;
+    while (n < 1024 && (uint64_t)n * 2 * experts <= 32768ull * 8 && (rows + n - 1) / n > 256) n *= 2;
+    return n;
+}
+
+hipError_t launch_route(int dtype, const Route& a, hipStream_t s) {
+    if (dtype == BC_F32) return route_of<float>(a, s);
+    if (dtype == BC_F16) return route_of<f16_t>(a, s);
+    return route_of<bf16_t>(a, s);
+}
+
+hipError_t launch_route_grad(int dtype, const RouteGrad& a, hipStream_t s) {
+    if (dtype == BC_F32) return route_grad_of<float>(a, s);
+    if (dtype == BC_F16) return route_grad_of<f16_t>(a, s);
+    return route_grad_of<bf16_t>(a, s);
+}
+
+hipError_t launch_combine(int dtype, const Combine& a, hipStream_t s) {
+    if (dtype == BC_F32) return combine_of<float>(a, s);
+    if (dtype == BC_F16) return combine_of<f16_t>(a, s);
+    return combine_of<bf16_t>(a, s);
+}
+
+hipError_t launch_combine_grad(int dtype, const CombineGrad& a, hipStream_t s) {
+    if (dtype == BC_F32) return combine_grad_of<float>(a, s);
+    if (dtype == BC_F16) return combine_grad_of<f16_t>(a, s);
+    return combine_grad_of<bf16_t>(a, s);
+}
+
+}  // namespace bc
