@@ -107,7 +107,8 @@ size_t grouped_ws(int dtype, uint64_t rows, uint64_t x_rows, uint64_t inner, uin
     const size_t x = planes_bytes(dtype, std::max(rows, x_rows <= rows ? x_rows : 0), inner);
     const size_t w = planes_bytes(dtype, experts * cols, inner);
     if (!backward) return rows <= kGroupedFewRows ? 0 : x + w;
-    return x + w + planes_bytes(dtype, rows, cols) + part_bytes(rows, experts, cols) + where_bytes(rows, experts);
+    return x + w + planes_bytes(dtype, rows, cols) + part_bytes(rows, experts, cols) + where_bytes(rows, experts) +
+           align256(kGroupedCounters * sizeof(uint32_t));
 }
 
 struct GroupedX {
@@ -117,17 +118,15 @@ struct GroupedX {
     uint64_t rows, call_rows, inner;
 };
 // x for the tiles; `source` becomes NULL where its rows now follow each other.
-GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, Carver& c, LayRows& lay, bool& do_lay) {
+GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, Carver& c, LayRows& lay) {
     const bool gather = x.source != nullptr;
     a_rows = (uint32_t)(gather ? x.rows : x.call_rows);
-    do_lay = false;
     if (readable(dtype, x.x, x.ld, x.inner) && (!gather || x.rows * x.ld * 2 <= kGatherBytes))
         return GroupedSide{x.x, x.ld, 0, 0};
     const uint64_t n = laid_rows(gather, x.call_rows, x.rows, x.inner), pc = plane_cols(x.inner);
     const bool own = lay_own_rows(gather, x.call_rows, x.rows, x.inner);
     void* to = c.take(planes_bytes(dtype, n, x.inner));
     lay = LayRows{x.x, own ? nullptr : x.source, to, x.ld, 0, n, n, (uint32_t)x.inner, (uint32_t)x.rows};
-    do_lay = true;
     if (!own) {
         x.source = nullptr;
         a_rows = (uint32_t)x.call_rows;
@@ -135,13 +134,11 @@ GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, Carver& c, LayRo
     return GroupedSide{to, pc, n * pc, 0};
 }
 GroupedSide side_of_w(int dtype, const void* w, uint64_t ld, uint64_t expert, uint32_t experts, uint64_t cols, uint64_t inner,
-                      Carver& c, LayRows& lay, bool& do_lay) {
-    do_lay = false;
+                      Carver& c, LayRows& lay) {
     if (readable(dtype, w, ld, inner) && expert % 8 == 0) return GroupedSide{w, ld, 0, expert};
     const uint64_t pc = plane_cols(inner), n = experts * cols;
     void* to = c.take(planes_bytes(dtype, n, inner));
     lay = LayRows{w, nullptr, to, ld, expert, n, cols, (uint32_t)inner, 0};
-    do_lay = true;
     return GroupedSide{to, pc, n * pc, cols * pc};
 }
 
@@ -335,12 +332,12 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
     }
     Carver c{(char*)ws, 0};
     GroupedX gx{x, ldx, source, x_rows, rows, inner};
-    LayRows lay[2];
-    bool do_lay[2];
+    Prepare pre{};
+    pre.g = g;
     GroupedProduct p{};
     p.g = g;
-    p.a = side_of_x(dtype, gx, p.a_rows, c, lay[0], do_lay[0]);
-    p.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, lay[1], do_lay[1]);
+    p.a = side_of_x(dtype, gx, p.a_rows, c, pre.lay[0]);
+    p.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, pre.lay[1]);
     if (c.used > 0 && (!ws || ws_bytes < c.used)) return BC_E_WORKSPACE;
     p.source = gx.source;
     p.cols = (uint32_t)cols;
@@ -353,9 +350,7 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
     p.ld_z = ldz;
     p.act = act;
     p.nt = streams(rows * cols * dtype_bytes(dtype));
-    hipError_t e = hipSuccess;
-    for (int i = 0; i < 2 && e == hipSuccess; ++i)
-        if (do_lay[i]) e = launch_lay_rows(dtype, lay[i], s);
+    hipError_t e = launch_prepare(dtype, pre, s);
     if (e == hipSuccess) e = launch_grouped(kGroupedForward, dtype, dtype, p, s);
     return finish_call(status_of(e), s, nullptr);
 }
@@ -392,24 +387,24 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
     const uint64_t pc = plane_cols(cols);
     // dz can be read as dy
     const bool same = act == BC_ACT_NONE && readable(dtype, dy, lddy, cols);
-    GroupedSlope slope{g, dy, act != BC_ACT_NONE ? z : nullptr, nullptr, nullptr, lddy, ldz, (uint32_t)cols, act};
+    Prepare pre{};
+    pre.g = g;
+    GroupedSlope& slope = pre.slope;
+    slope = GroupedSlope{dy, act != BC_ACT_NONE ? z : nullptr, nullptr, nullptr, lddy, ldz, (uint32_t)cols, act};
     if (!same && (dx || dw)) slope.dz = c.take(planes_bytes(dtype, rows, cols));
     if (dbias) slope.part = (float*)c.take(part_bytes(rows, experts, cols));
     const GroupedSide dz = slope.dz ? GroupedSide{slope.dz, pc, rows * pc, 0} : GroupedSide{dy, lddy, 0, 0};
-    LayRows lay[2];
-    bool do_lay[2] = {false, false};
     GroupedProduct px{}, pw{};
     px.g = pw.g = g;
     px.a = pw.a = dz;
     px.a_rows = (uint32_t)rows;
-    GroupedWhere where{g, nullptr, nullptr, 0, 0};
     if (dw) {
         GroupedX gx{x, ldx, source, x_rows, rows, inner};
         uint32_t n = 0;
-        pw.b = side_of_x(dtype, gx, n, c, lay[0], do_lay[0]);
+        pw.b = side_of_x(dtype, gx, n, c, pre.lay[0]);
         if (gx.source) {
-            where = GroupedWhere{g, gx.source, (uint32_t*)c.take(where_bytes(rows, experts)), n, (uint32_t)pw.b.ld};
-            pw.where = where.where;
+            pre.where = GroupedWhere{gx.source, (uint32_t*)c.take(where_bytes(rows, experts)), n, (uint32_t)pw.b.ld};
+            pw.where = pre.where.where;
         }
         pw.rows = (uint32_t)cols;
         pw.cols = (uint32_t)inner;
@@ -419,25 +414,24 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
         pw.nt = streams(experts * cols * inner * dtype_bytes(gdtype));
     }
     if (dx) {
-        px.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, lay[1], do_lay[1]);
+        px.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, pre.lay[1]);
         px.cols = (uint32_t)inner;
         px.k = (uint32_t)cols;
         px.out = dx;
         px.ld_out = lddx;
         px.nt = streams(rows * inner * dtype_bytes(dtype));
     }
+    if (dx && dw) pre.counters = (uint32_t*)c.take(kGroupedCounters * sizeof(uint32_t));
     if (c.used > 0 && rows > 0 && (!ws || ws_bytes < c.used)) return BC_E_WORKSPACE;
-    hipError_t e = hipSuccess;
-    if (rows > 0) {
-        if (cols > 0 && (slope.dz || slope.part)) e = launch_grouped_slope(dtype, slope, s);
-        for (int i = 0; i < 2 && e == hipSuccess; ++i)
-            if (do_lay[i]) e = launch_lay_rows(dtype, lay[i], s);
-        if (e == hipSuccess && where.where) e = launch_grouped_where(where, s);
-    }
     // (no rows: dw and dbias are zeros)
-    if (e == hipSuccess && dbias) e = launch_grouped_bias(gdtype, slope, dbias, ld_dbias, s);
-    if (e == hipSuccess && dx) e = launch_grouped(kGroupedRows, dtype, dtype, px, s);
-    if (e == hipSuccess && dw) e = launch_grouped(kGroupedWeights, dtype, gdtype, pw, s);
+    hipError_t e = rows > 0 ? launch_prepare(dtype, pre, s) : hipSuccess;
+    if (e == hipSuccess && dbias) e = launch_grouped_bias(gdtype, g, slope, dbias, ld_dbias, s);
+    if (e == hipSuccess && dx && dw) {
+        e = launch_grouped_pair(dtype, gdtype, px, pw, pre.counters, s);
+    } else {
+        if (e == hipSuccess && dx) e = launch_grouped(kGroupedRows, dtype, dtype, px, s);
+        if (e == hipSuccess && dw) e = launch_grouped(kGroupedWeights, dtype, gdtype, pw, s);
+    }
     return finish_call(status_of(e), s, nullptr);
 }
 

@@ -96,6 +96,10 @@ struct GroupedProduct {
     bool nt;
 };
 hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProduct& p, hipStream_t s);
+// Both gradients' products.  counters: kGroupedCounters words, zero (launch_prepare).
+constexpr uint32_t kGroupedCounters = 8;
+hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
+                               uint32_t* counters, hipStream_t s);
 
 // The forward pass for few rows in all.
 constexpr uint32_t kGroupedFewRows = 64;
@@ -110,6 +114,7 @@ struct GroupedFew {
 };
 hipError_t launch_grouped_few(int dtype, const GroupedFew& a, hipStream_t s);
 
+// What the products need first, in one launch; a part whose output is NULL is left out.
 // Rows laid out as planes [count][plane_cols(cols)]: row r is row r % group of
 // the matrix r / group, or row source[r] of the only one (zeros where there is none).
 struct LayRows {
@@ -119,12 +124,9 @@ struct LayRows {
     uint64_t ld, matrix, count, group;
     uint32_t cols, in_rows;
 };
-hipError_t launch_lay_rows(int dtype, const LayRows& a, hipStream_t s);
-
-// dz = dy act'(z) of the experts' rows as planes [rows][plane_cols(cols)], its
-// sums over every tile of 64 rows, and the experts' sums of those.
+// dz = dy act'(z) of the experts' rows as planes [rows][plane_cols(cols)], and its
+// sums over every tile of 64 rows.
 struct GroupedSlope {
-    Groups g;
     const void *dy, *z;      // z NULL: dz = dy
     void* dz;                // NULL: sums only
     float* part;             // [group_tiles(rows, experts, 64)][cols], NULL: not wanted
@@ -132,18 +134,24 @@ struct GroupedSlope {
     uint32_t cols;
     int act;
 };
-hipError_t launch_grouped_slope(int dtype, const GroupedSlope& a, hipStream_t s);
-hipError_t launch_grouped_bias(int out_dtype, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s);
-
 // Byte offsets of the rows source[r] of a matrix of row stride ld (16-bit
 // elements), every expert's from a multiple of 64 on, kNowhere in between.
 struct GroupedWhere {
-    Groups g;
     const int32_t* source;
     uint32_t* where;         // [64 (group_tiles(rows, experts, 64) + 1)]
     uint32_t x_rows, ld;
 };
-hipError_t launch_grouped_where(const GroupedWhere& a, hipStream_t s);
+struct Prepare {
+    Groups g;
+    GroupedSlope slope;
+    LayRows lay[2];
+    GroupedWhere where;
+    uint32_t* counters;      // set to zero
+    uint32_t first[5];       // workgroups before lay[0], lay[1], where and counters, and in all
+};
+hipError_t launch_prepare(int dtype, Prepare& a, hipStream_t s);
+// The experts' sums of slope.part, rows ld apart.
+hipError_t launch_grouped_bias(int out_dtype, const Groups& g, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s);
 
 // --------------------------------------------------- norm and clipping
 // One matrix of a list (device table; compared by its bytes: no padding).

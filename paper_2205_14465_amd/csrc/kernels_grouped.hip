@@ -57,6 +57,32 @@ __device__ __forceinline__ bool run_of(const Groups& g, uint32_t t, Run& r) {
     return t >= before && r.from >= at && r.from < to;
 }
 
+// The same for tile t of a product that is tiles_n tiles wide: the experts' tiles one
+// expert after the other, an expert's down columns of at most kBand tiles.
+constexpr uint32_t kBand = 8;
+template <uint32_t kHigh>
+__device__ __forceinline__ bool tile_run(const Groups& g, uint32_t t, uint32_t tiles_n, Run& r, uint32_t& tn) {
+    const uint32_t lane = threadIdx.x & 63, first = offset_of(g, 0), row = t / tiles_n;
+    uint32_t n = 0;
+    for (uint32_t e0 = 0; e0 < g.experts; e0 += 64) {
+        const uint32_t e = e0 + lane;
+        n += __popcll(__ballot(e < g.experts && tiles_before<kHigh>(first, offset_of(g, e), e) <= row));
+    }
+    r.expert = __builtin_amdgcn_readfirstlane(n > 0 ? n - 1 : 0);
+    const uint32_t at = offset_of(g, r.expert), to = offset_of(g, r.expert + 1);
+    const uint32_t before = tiles_before<kHigh>(first, at, r.expert);
+    if (row < before || to <= at) return false;
+    const uint32_t high = (to - at + kHigh - 1) / kHigh, in = t - before * tiles_n;
+    const uint32_t band = in / (kBand * tiles_n), rows = band * kBand;
+    if (rows >= high) return false;
+    const uint32_t here = high - rows < kBand ? high - rows : kBand, i = in - rows * tiles_n;
+    if (i >= here * tiles_n) return false;
+    tn = i / here;
+    r.from = at + (rows + i % here) * kHigh;
+    r.to = to;
+    return true;
+}
+
 // The tiles there are, given the offsets.
 template <uint32_t kHigh>
 __device__ __forceinline__ uint32_t tiles_in_all(const Groups& g) {
@@ -65,6 +91,18 @@ __device__ __forceinline__ uint32_t tiles_in_all(const Groups& g) {
 }
 
 // ----------------------------------------------------------------- products
+// The activation for a 16-bit result: as activate<false>, with fused multiplications
+// and the exponential's factor log2(e) among the constants, as the epilogue of large
+// products is bound by these instructions.
+__device__ __forceinline__ float quick_act(int act, float z) {
+    constexpr float kLog2e = 1.44269504088896f;
+    float t;
+    if (act == BC_ACT_GELU_TANH) t = z * fmaf(z * z, -2.0f * kTanhScale * kTanhCubic * kLog2e, -2.0f * kTanhScale * kLog2e);
+    else if (act == BC_ACT_SILU) t = -kLog2e * z;
+    else return activate<false>(act, z);
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+}
+
 // Eight columns of a row of the result from the fp32 sums v.
 template <typename TO, bool forward>
 __device__ __forceinline__ void finish_row(const GroupedProduct& p, uint32_t e, uint64_t m, uint32_t n, float (&v)[8]) {
@@ -80,35 +118,63 @@ __device__ __forceinline__ void finish_row(const GroupedProduct& p, uint32_t e, 
         if (p.z) store_vec((TO*)p.z + m * p.ld_z + n, left, v, p.nt);
         if (p.act != BC_ACT_NONE)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate<exact>(p.act, v[i]);
+            for (int i = 0; i < 8; ++i) v[i] = exact ? activate<true>(p.act, v[i]) : quick_act(p.act, v[i]);
     }
     store_vec((TO*)p.out + m * p.ld_out + n, left, v, p.nt);
 }
 
-// The experts' rows times their weight: forward with k along the rows of both,
-// for dx with k down the columns of w.
-template <typename G, typename TO, bool forward>
-__global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
-    typedef RunTile<G, false, !forward> R;
-    typedef typename G::T T;
-    extern __shared__ char lds[];
-    const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN, tiles_m = tiles_in_all<G::kBM>(p.g);
-    if (blockIdx.x >= tiles_m * tiles_n) return;
-    uint32_t tm, tn;
-    tile_of<8>(blockIdx.x, tiles_m, tiles_n, tm, tn);
-    Run run;
-    if (!run_of<G::kBM>(p.g, tm, run)) return;
-    const uint32_t m0 = run.from, n0 = tn * G::kBN;
+// How the operands of a product lie: forward k along the rows of both, for dx
+// down the columns of w, for dw down those of dz and x.
+template <bool forward>
+using RowsLie = Lie<false, !forward>;
+template <bool kTable>
+using WeightsLie = Lie<true, true, kTable>;
+
+// Takes up the tile with rows `run` and columns n0 on of the experts' rows times
+// their weight.
+template <bool forward, typename R>
+__device__ __forceinline__ void begin_rows(R& g, const GroupedProduct& p, const Run& run, uint32_t n0, char* lds) {
+    typedef typename R::T T;
     const bool gather = forward && p.source;
+    const uint32_t m0 = run.from;
     const Side<T> a{(const T*)p.a.p + (gather ? 0 : m0 * p.a.ld), p.a.plane, (uint32_t)p.a.ld, run.to - m0};
     const Side<T> b{(const T*)p.b.p + run.expert * p.b.expert + (forward ? n0 * p.b.ld : n0), p.b.plane, (uint32_t)p.b.ld,
                     p.cols - n0};
-    R g;
-    g.template multiply<false>(a, b, p.k, lds, [&](int r) -> uint32_t {
+    g.template begin<RowsLie<forward>>(a, b, p.k, nullptr, lds, [&](int r) -> uint32_t {
         if (!gather) return (uint32_t)r * (uint32_t)p.a.ld * 2;
         const uint32_t row = (uint32_t)p.source[m0 + r];
         return row < p.a_rows ? row * (uint32_t)p.a.ld * 2 : kNowhere;
-    }, nullptr);
+    });
+}
+
+// The same for rows m0 and columns n0 on of expert e's dw.
+template <bool kTable, typename R>
+__device__ __forceinline__ void begin_weights(R& g, const GroupedProduct& p, uint32_t e, uint32_t m0, uint32_t n0, char* lds) {
+    typedef typename R::T T;
+    const uint32_t first = offset_of(p.g, 0), from = offset_of(p.g, e), to = offset_of(p.g, e + 1);
+    const Side<T> a{(const T*)p.a.p + (uint64_t)from * p.a.ld + m0, p.a.plane, (uint32_t)p.a.ld, p.rows - m0};
+    const Side<T> b{(const T*)p.b.p + (kTable ? 0 : (uint64_t)from * p.b.ld) + n0, p.b.plane, (uint32_t)p.b.ld, p.cols - n0};
+    const uint32_t* where = kTable ? p.where + (uint64_t)tiles_before<64>(first, from, e) * 64 : nullptr;
+    // (offsets that do not ascend: no rows)
+    g.template begin<WeightsLie<kTable>>(a, b, to > from && from >= first ? to - from : 0, where, lds, [](int) { return 0u; });
+}
+
+template <typename G, typename TO, bool forward>
+__global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
+    extern __shared__ char lds[];
+    const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN, tiles_m = tiles_in_all<G::kBM>(p.g);
+    if (blockIdx.x >= tiles_m * tiles_n) return;
+    // a die's tiles are consecutive ones, expert by expert
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
+    const uint32_t t = die * q + (die < rest ? die : rest) + blockIdx.x / 8;
+    Run run;
+    uint32_t tn;
+    if (!tile_run<G::kBM>(p.g, t, tiles_n, run, tn)) return;
+    const uint32_t m0 = run.from, n0 = tn * G::kBN;
+    RunTile<G> g;
+    begin_rows<forward>(g, p, run, n0, lds);
+    g.template rest<RowsLie<forward>>(lds);
+    g.template run<RowsLie<forward>>(lds);
     g.finish(lds, [&](int row, int col, float (&v)[8]) {
         const uint32_t m = m0 + row, n = n0 + col;
         if (m < run.to && n < p.cols) finish_row<TO, forward>(p, run.expert, m, n, v);
@@ -118,27 +184,281 @@ __global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
 // dw: every expert's tiles, over its rows.
 template <typename G, typename TO, bool kTable>
 __global__ __launch_bounds__(G::kThreads) void weights_product(GroupedProduct p) {
-    typedef RunTile<G, true, true> R;
-    typedef typename G::T T;
     extern __shared__ char lds[];
     const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
-    // a die works on one expert at a time: its tiles one after the other
-    const uint32_t each = tiles_m * tiles_n, total = each * p.g.experts, q = total / 8, rest = total % 8;
-    const uint32_t die = blockIdx.x % 8, t = die * q + (die < rest ? die : rest) + blockIdx.x / 8;
-    const uint32_t e = t / each, in = t - e * each, tm = in / tiles_n, tn = in - tm * tiles_n;
-    const uint32_t first = offset_of(p.g, 0), from = offset_of(p.g, e), to = offset_of(p.g, e + 1);
-    const uint32_t m0 = tm * G::kBM, n0 = tn * G::kBN;
-    const Side<T> a{(const T*)p.a.p + (uint64_t)from * p.a.ld + m0, p.a.plane, (uint32_t)p.a.ld, p.rows - m0};
-    const Side<T> b{(const T*)p.b.p + (kTable ? 0 : (uint64_t)from * p.b.ld) + n0, p.b.plane, (uint32_t)p.b.ld, p.cols - n0};
-    const uint32_t* where = kTable ? p.where + (uint64_t)tiles_before<64>(first, from, e) * 64 : nullptr;
-    // (offsets that do not ascend: no rows)
-    R g;
-    g.template multiply<kTable>(a, b, to > from && from >= first ? to - from : 0, lds, [](int) { return 0u; }, where);
+    // an expert's tiles go to all dies, each a run of consecutive ones
+    const uint32_t each = tiles_m * tiles_n, e = blockIdx.x / each, j = blockIdx.x - e * each;
+    const uint32_t in = j % 8 * (each / 8) + (j % 8 < each % 8 ? j % 8 : each % 8) + j / 8;
+    const uint32_t m0 = in / tiles_n * G::kBM, n0 = in % tiles_n * G::kBN;
+    RunTile<G> g;
+    begin_weights<kTable>(g, p, e, m0, n0, lds);
+    g.template rest<WeightsLie<kTable>>(lds);
+    g.template run<WeightsLie<kTable>>(lds);
     g.finish(lds, [&](int row, int col, float (&v)[8]) {
         const uint32_t m = m0 + row, n = n0 + col;
         if (m < p.rows && n < p.cols)
             store_vec((TO*)p.out + e * p.expert_out + m * p.ld_out + n, (int)(p.cols - n), v, p.nt);
     });
+}
+
+// ---------------------------------------------------------- large products
+// The largest tiles fill a compute unit, so nothing runs beside one's epilogue.
+// Workgroups stay: before a tile's epilogue a workgroup takes up its next tile and
+// asks for its first step, the other stage of LDS serves as the strips.
+
+// The experts' tiles and rows, in LDS.
+struct RunTable {
+    uint32_t tiles[kMaxExperts + 1];   // before each expert
+    uint32_t rows[kMaxExperts + 1];    // its first
+    uint32_t order[kMaxExperts];       // experts by their rows, the most first
+    uint32_t next;                     // a workgroup's next tile
+};
+// Experts by their rows, where it takes few comparisons; fill_runs has run.
+constexpr uint32_t kSortExperts = 128;
+__device__ __forceinline__ void sort_runs(uint32_t experts, RunTable& t) {
+    for (uint32_t e = threadIdx.x; e < experts; e += blockDim.x) {
+        uint32_t at = e;
+        if (experts <= kSortExperts) {
+            const int32_t n = (int32_t)(t.rows[e + 1] - t.rows[e]);
+            at = 0;
+            for (uint32_t i = 0; i < experts; ++i) {
+                const int32_t m = (int32_t)(t.rows[i + 1] - t.rows[i]);
+                at += m > n || (m == n && i < e);
+            }
+        }
+        t.order[at] = e;
+    }
+    __syncthreads();
+}
+template <uint32_t kHigh>
+__device__ __forceinline__ void fill_runs(const Groups& g, RunTable& t) {
+    if (threadIdx.x < 64) {
+        uint32_t sum = 0;
+        for (uint32_t e0 = 0; e0 <= g.experts; e0 += 64) {
+            const uint32_t e = e0 + threadIdx.x;
+            uint32_t at = 0, n = 0;
+            if (e <= g.experts) at = offset_of(g, e);
+            if (e < g.experts) {
+                const uint32_t to = offset_of(g, e + 1);
+                n = to > at ? (to - at + kHigh - 1) / kHigh : 0;
+            }
+            uint32_t s = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t y = __shfl_up(s, o, 64);
+                if (threadIdx.x >= (uint32_t)o) s += y;
+            }
+            if (e <= g.experts) {
+                t.tiles[e] = sum + s - n;
+                t.rows[e] = at;
+            }
+            sum += __shfl(s, 63, 64);
+        }
+    }
+    __syncthreads();
+}
+// Tile t of a product that is tiles_n tiles wide: as tile_run, without empty ones.
+template <uint32_t kHigh>
+__device__ __forceinline__ void run_in(const RunTable& table, uint32_t experts, uint32_t t, uint32_t tiles_n, Run& r,
+                                       uint32_t& tn) {
+    const uint32_t lane = threadIdx.x & 63, row = t / tiles_n;
+    uint32_t n = 0;
+    for (uint32_t e0 = 0; e0 < experts; e0 += 64)
+        n += __popcll(__ballot(e0 + lane < experts && table.tiles[e0 + lane] <= row));
+    r.expert = __builtin_amdgcn_readfirstlane(n - 1);
+    const uint32_t before = __builtin_amdgcn_readfirstlane(table.tiles[r.expert]);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(table.rows[r.expert]);
+    r.to = __builtin_amdgcn_readfirstlane(table.rows[r.expert + 1]);
+    const uint32_t high = (r.to - at + kHigh - 1) / kHigh, in = t - before * tiles_n;
+    const uint32_t first = in / (kBand * tiles_n) * kBand, here = high - first < kBand ? high - first : kBand;
+    const uint32_t i = in - first * tiles_n;
+    tn = i / here;
+    r.from = at + (first + i % here) * kHigh;
+}
+
+// LDS of a large product: two stages, and of the strips what one does not hold; the
+// table comes behind (everything before is 16-byte aligned).
+template <typename G>
+constexpr int kLargeLds = G::kStageBytes + (G::kStageBytes > G::kEpiBytes ? G::kStageBytes : G::kEpiBytes);
+
+// The first tile's first step has landed (its second may be on the way).
+template <typename G>
+__device__ __forceinline__ void wait_first() {
+    wait_vmcnt<0>();
+    lds_barrier();
+}
+// The epilogue, strips in the second stage.  The next tile's first step, asked for
+// before, is waited for before the last stores: those are not waited for, as
+// memory operations count down in order.
+template <typename R, typename E>
+__device__ __forceinline__ void finish_large(R& g, char* lds, const E& epi) {
+    g.template finish_blocks<0, R::kFM - 1>(lds + R::kStageBytes, epi);
+    wait_vmcnt<0>();
+    g.template finish_blocks<R::kFM - 1, R::kFM>(lds + R::kStageBytes, epi);
+    lds_barrier();  // every wave has read its strip, and its part of the next step is there
+}
+
+template <typename G, typename TO, bool forward>
+__global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
+    typedef RowsLie<forward> L;
+    extern __shared__ char lds[];
+    RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
+    fill_runs<G::kBM>(p.g, table);
+    const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN;
+    // (offsets that do not ascend make more tiles than there can be: those are left out)
+    const uint32_t tiles_m = min((uint32_t)__builtin_amdgcn_readfirstlane(table.tiles[p.g.experts]),
+                                 group_tiles(p.g.rows, p.g.experts, G::kBM));
+    // a die's tiles are consecutive ones, expert by expert, dealt to its workgroups in turn
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
+    const uint32_t from = die * q + (die < rest ? die : rest), to = from + q + (die < rest ? 1 : 0);
+    uint32_t t = from + blockIdx.x / 8;
+    if (t >= to) return;
+    RunTile<G> g;
+    Run run;
+    uint32_t tn;
+    run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
+    begin_rows<forward>(g, p, run, tn * G::kBN, lds);
+    g.template rest<L>(lds);
+    wait_first<G>();
+    for (;;) {
+        g.template run<L, true>(lds);
+        const Run done = run;
+        const uint32_t m0 = run.from, n0 = tn * G::kBN;
+        t += gridDim.x / 8;
+        const bool more = t < to;
+        if (more) {
+            run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
+            begin_rows<forward>(g, p, run, tn * G::kBN, lds);
+        }
+        finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
+            const uint32_t m = m0 + row, n = n0 + col;
+            if (m < done.to && n < p.cols) finish_row<TO, forward>(p, done.expert, m, n, v);
+        });
+        if (!more) return;
+        g.template rest<L>(lds);
+    }
+}
+
+template <typename G, typename TO, bool kTable>
+__global__ __launch_bounds__(G::kThreads) void weights_large(GroupedProduct p) {
+    typedef WeightsLie<kTable> L;
+    extern __shared__ char lds[];
+    const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
+    const uint32_t each = tiles_m * tiles_n, all = each * p.g.experts;
+    // workgroups take tiles in turn, and so experts one after the other; of an expert's,
+    // the dies have a run of consecutive ones each
+    auto place = [&](uint32_t b, uint32_t& e, uint32_t& m0, uint32_t& n0) {
+        e = b / each;
+        const uint32_t j = b - e * each, in = j % 8 * (each / 8) + (j % 8 < each % 8 ? j % 8 : each % 8) + j / 8;
+        m0 = in / tiles_n * G::kBM;
+        n0 = in % tiles_n * G::kBN;
+    };
+    uint32_t b = blockIdx.x, e, m0, n0;
+    if (b >= all) return;
+    RunTile<G> g;
+    place(b, e, m0, n0);
+    begin_weights<kTable>(g, p, e, m0, n0, lds);
+    g.template rest<L>(lds);
+    wait_first<G>();
+    for (;;) {
+        g.template run<L, true>(lds);
+        const uint32_t e1 = e, m1 = m0, n1 = n0;
+        b += gridDim.x;
+        const bool more = b < all;
+        if (more) {
+            place(b, e, m0, n0);
+            begin_weights<kTable>(g, p, e, m0, n0, lds);
+        }
+        finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
+            const uint32_t m = m1 + row, n = n1 + col;
+            if (m < p.rows && n < p.cols)
+                store_vec((TO*)p.out + e1 * p.expert_out + m * p.ld_out + n, (int)(p.cols - n), v, p.nt);
+        });
+        if (!more) return;
+        g.template rest<L>(lds);
+    }
+}
+
+// dx's tiles and dw's, in one launch: each die's workgroups take its next tile when they
+// have done theirs, so that the end of the first product's last round is filled with
+// tiles of the second.  The product whose k is longer comes first, and of dw's tiles
+// those of the experts with the most rows.
+template <typename G, typename TO, bool kTable>
+__global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, GroupedProduct pw, uint32_t* counters) {
+    typedef RowsLie<false> LX;
+    typedef WeightsLie<kTable> LW;
+    extern __shared__ char lds[];
+    RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
+    fill_runs<G::kBM>(px.g, table);
+    sort_runs(px.g.experts, table);
+    const uint32_t die = blockIdx.x % 8, tiles_n = (px.cols + G::kBN - 1) / G::kBN;
+    const uint32_t tiles_m = min((uint32_t)__builtin_amdgcn_readfirstlane(table.tiles[px.g.experts]),
+                                 group_tiles(px.g.rows, px.g.experts, G::kBM));
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8;
+    const uint32_t from = die * q + (die < rest ? die : rest), rows_tiles = q + (die < rest ? 1 : 0);
+    const uint32_t wide = (pw.cols + G::kBN - 1) / G::kBN, each = (pw.rows + G::kBM - 1) / G::kBM * wide;
+    const uint32_t all = each * pw.g.experts, weights_tiles = all / 8 + (die < all % 8 ? 1 : 0);
+    const bool rows_first = px.k >= pw.g.rows / pw.g.experts;
+    RunTile<G> g;
+    Run run;
+    uint32_t m0, n0;
+    bool rows;
+    // takes up the die's tile i, if there is one
+    auto take = [&](uint32_t i) {
+        if (i >= rows_tiles + weights_tiles) return false;
+        rows = rows_first ? i < rows_tiles : i >= weights_tiles;
+        if (rows != rows_first) i -= rows_first ? rows_tiles : weights_tiles;
+        if (rows) {
+            uint32_t tn;
+            run_in<G::kBM>(table, px.g.experts, from + i, tiles_n, run, tn);
+            m0 = run.from;
+            n0 = tn * G::kBN;
+            begin_rows<false>(g, px, run, n0, lds);
+            return true;
+        }
+        const uint32_t b = i * 8 + die;
+        const uint32_t nth = b / each, j = b - nth * each;
+        const uint32_t in = j % 8 * (each / 8) + (j % 8 < each % 8 ? j % 8 : each % 8) + j / 8;
+        run.expert = __builtin_amdgcn_readfirstlane(table.order[nth]);
+        m0 = in / wide * G::kBM;
+        n0 = in % wide * G::kBN;
+        begin_weights<kTable>(g, pw, run.expert, m0, n0, lds);
+        return true;
+    };
+    auto ask_rest = [&]() {
+        if (rows) g.template rest<LX>(lds);
+        else g.template rest<LW>(lds);
+    };
+    if (!take(blockIdx.x / 8)) return;
+    ask_rest();
+    wait_first<G>();
+    for (;;) {
+        // (its answer comes while the tile is at work)
+        uint32_t next = 0, none = 0;
+        asm volatile("" : "+v"(none));  // (of an address that all lanes share the compiler wants the answer at once)
+        if (threadIdx.x == 0) next = atomicAdd(counters + die + none, 1u);
+        if (rows) g.template run<LX, true>(lds);
+        else g.template run<LW, true>(lds);
+        if (threadIdx.x == 0) table.next = gridDim.x / 8 + next;
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        lds_barrier();
+        const bool was_rows = rows;
+        const uint32_t e1 = run.expert, to1 = run.to, m1 = m0, n1 = n0;
+        const bool more = take(__builtin_amdgcn_readfirstlane(table.next));
+        if (was_rows)
+            finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
+                const uint32_t m = m1 + row, n = n1 + col;
+                if (m < to1 && n < px.cols) finish_row<typename G::T, false>(px, e1, m, n, v);
+            });
+        else
+            finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
+                const uint32_t m = m1 + row, n = n1 + col;
+                if (m < pw.rows && n < pw.cols)
+                    store_vec((TO*)pw.out + e1 * pw.expert_out + m * pw.ld_out + n, (int)(pw.cols - n), v, pw.nt);
+            });
+        if (!more) return;
+        ask_rest();
+    }
 }
 
 // Tile shapes, small to large.
@@ -154,6 +474,21 @@ template <> struct Tiles<float> {
 };
 
 template <typename G>
+hipError_t launch_large(const void* kernel, void** args, uint64_t tiles, hipStream_t s) {
+    static_assert(G::kStages == 2, "the strips lie where the second stage is");
+    int dev = 0;
+    DevInfo di;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess) e = device_info(dev, &di);
+    constexpr int kLds = kLargeLds<G> + (int)sizeof(RunTable);
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+    // a whole number of workgroups for each die
+    const uint32_t grid = (uint32_t)std::min<uint64_t>((tiles + 7) / 8 * 8, (uint64_t)(di.cus < 8 ? 8 : di.cus / 8 * 8));
+    return hipLaunchKernel(kernel, dim3(grid), dim3(G::kThreads), args, kLds, s);
+}
+
+template <typename G>
 hipError_t launch_tiles(const void* kernel, const GroupedProduct& p, uint64_t grid, hipStream_t s) {
     hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
     if (e != hipSuccess) return e;
@@ -164,16 +499,30 @@ hipError_t launch_tiles(const void* kernel, const GroupedProduct& p, uint64_t gr
 
 template <typename G, typename TO>
 hipError_t launch_kind(int kind, const GroupedProduct& p, hipStream_t s) {
+    constexpr bool kLarge = G::P == 1 && G::kBM == 256;
     const uint64_t across = (p.cols + G::kBN - 1) / G::kBN;
+    const uint64_t tiles = across * (kind == kGroupedWeights ? (uint64_t)p.g.experts * ((p.rows + G::kBM - 1) / G::kBM)
+                                                             : group_tiles(p.g.rows, p.g.experts, G::kBM));
     if (kind == kGroupedWeights) {
-        const uint64_t grid = (uint64_t)p.g.experts * ((p.rows + G::kBM - 1) / G::kBM) * across;
-        if (p.where) return launch_tiles<G>((const void*)weights_product<G, TO, true>, p, grid, s);
-        return launch_tiles<G>((const void*)weights_product<G, TO, false>, p, grid, s);
+        if constexpr (kLarge) {
+            void* args[] = {(void*)&p};
+            return launch_large<G>(p.where ? (const void*)weights_large<G, TO, true> : (const void*)weights_large<G, TO, false>, args,
+                                   tiles, s);
+        } else {
+            return launch_tiles<G>(p.where ? (const void*)weights_product<G, TO, true> : (const void*)weights_product<G, TO, false>,
+                                   p, tiles, s);
+        }
     }
-    const uint64_t grid = group_tiles(p.g.rows, p.g.experts, G::kBM) * across;
     if constexpr (std::is_same_v<TO, typename G::T> || G::P > 1) {
-        if (kind == kGroupedForward) return launch_tiles<G>((const void*)rows_product<G, TO, true>, p, grid, s);
-        return launch_tiles<G>((const void*)rows_product<G, TO, false>, p, grid, s);
+        const bool forward = kind == kGroupedForward;
+        if constexpr (kLarge) {
+            void* args[] = {(void*)&p};
+            return launch_large<G>(forward ? (const void*)rows_large<G, TO, true> : (const void*)rows_large<G, TO, false>, args,
+                                   tiles, s);
+        } else {
+            return launch_tiles<G>(forward ? (const void*)rows_product<G, TO, true> : (const void*)rows_product<G, TO, false>, p,
+                                   tiles, s);
+        }
     }
     return hipErrorInvalidValue;
 }
@@ -309,10 +658,10 @@ __global__ __launch_bounds__(256) void grouped_few(GroupedFew a) {
 
 // ---------------------------------------------------- what products are given
 template <typename T>
-__global__ __launch_bounds__(256) void lay_rows(LayRows a) {
+__device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint32_t blocks) {
     typedef typename PlaneOf<T>::type E;
-    const uint64_t ld = plane_cols(a.cols), across = ld / 8, step = (uint64_t)gridDim.x * 256;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < a.count * across; i += step) {
+    const uint64_t ld = plane_cols(a.cols), across = ld / 8, step = (uint64_t)blocks * 256;
+    for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < a.count * across; i += step) {
         const uint64_t r = i / across;
         const uint32_t c = (uint32_t)(i - r * across) * 8;
         uint64_t at;
@@ -331,74 +680,101 @@ __global__ __launch_bounds__(256) void lay_rows(LayRows a) {
     }
 }
 
-// A workgroup 64 rows of one expert by 64 columns.
+// A workgroup 64 rows of one expert by 128 columns; all its loads go out before the
+// first is used.  Bound by memory: TODO.
+constexpr uint32_t kSlopeCols = 128;
 template <typename T>
-__global__ __launch_bounds__(256) void grouped_slope(GroupedSlope a) {
+__device__ __forceinline__ void slope_tile(const Groups& g, const GroupedSlope& a, uint32_t block) {
     typedef typename PlaneOf<T>::type E;
-    __shared__ float sums[4][64];
+    constexpr int kPasses = 4;
+    __shared__ float sums[4][kSlopeCols];
     Run run;
     const uint64_t ld = plane_cols(a.cols);
-    const uint32_t across = (uint32_t)(ld / 64), tile = blockIdx.x / across, c0 = blockIdx.x % across * 64;
-    const bool some = run_of<64>(a.g, tile, run);
-    const uint32_t lc = threadIdx.x % 8 * 8, c = c0 + lc;
+    const uint32_t across = (uint32_t)(ld + kSlopeCols - 1) / kSlopeCols, tile = block / across, c0 = block % across * kSlopeCols;
+    const bool some = run_of<64>(g, tile, run);
+    const uint32_t lc = threadIdx.x % 16 * 8, c = c0 + lc;
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
     if (some) {
+        Raw<T, 8> v[kPasses], z[kPasses];
+        int left[kPasses];
+        auto fetch = [&](auto whole) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint64_t r = run.from + threadIdx.x / 8 + 32 * i;
-            const int left = r < run.to && c < a.cols ? (int)(a.cols - c) : 0;
-            float v[8], z[8];
-            load_vec((const T*)a.dy + (left > 0 ? r * a.ldd + c : 0), left, v);
-            if (a.z) {
-                load_vec((const T*)a.z + (left > 0 ? r * a.ldz + c : 0), left, z);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] * act_slope<sizeof(T) == 4>(a.act, z[j]) : 0.0f;
+            for (int i = 0; i < kPasses; ++i) {
+                const uint64_t r = run.from + threadIdx.x / 16 + 16 * i;
+                left[i] = r < run.to && c < a.cols ? (int)(a.cols - c) : 0;
+                v[i].template load<decltype(whole)::value>((const T*)a.dy + (left[i] > 0 ? r * a.ldd + c : 0), left[i]);
+                if (a.z) z[i].template load<decltype(whole)::value>((const T*)a.z + (left[i] > 0 ? r * a.ldz + c : 0), left[i]);
             }
-            if (a.dz && r < run.to) store_planes<T>((E*)a.dz + r * ld + c, (uint64_t)a.g.rows * ld, v);
+        };
+        if (a.cols % 8 == 0 || c0 + kSlopeCols <= a.cols) fetch(std::true_type{});
+        else fetch(std::false_type{});
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+        for (int i = 0; i < kPasses; ++i) {
+            const uint64_t r = run.from + threadIdx.x / 16 + 16 * i;
+            float d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                d[j] = (float)v[i].v[j];
+                if (a.z) d[j] = j < left[i] ? d[j] * act_slope<sizeof(T) == 4>(a.act, (float)z[i].v[j]) : 0.0f;
+                sum[j] += d[j];
+            }
+            if (a.dz && r < run.to && c < ld) store_planes<T>((E*)a.dz + r * ld + c, (uint64_t)g.rows * ld, d);
         }
     }
     if (!a.part) return;
-    // rows of the same columns: lanes eight apart, then the waves
+    // rows of the same columns: lanes sixteen apart, then the waves
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int o = 8; o < 64; o <<= 1) sum[j] += __shfl_xor(sum[j], o, 64);
-    if ((threadIdx.x & 63) < 8)
+        for (int o = 16; o < 64; o <<= 1) sum[j] += __shfl_xor(sum[j], o, 64);
+    if ((threadIdx.x & 63) < 16)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sums[threadIdx.x >> 6][lc + j] = sum[j];
     __syncthreads();
     const uint32_t col = c0 + threadIdx.x;
-    if (threadIdx.x < 64 && col < a.cols)
+    if (threadIdx.x < kSlopeCols && col < a.cols)
         a.part[(uint64_t)tile * a.cols + col] =
             (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
-template <typename TO>
-__global__ __launch_bounds__(256) void grouped_bias(GroupedSlope a, TO* out, uint64_t ld) {
-    const uint32_t c = blockIdx.x * 256 + threadIdx.x, e = blockIdx.y;
-    if (c >= a.cols) return;
-    const uint32_t first = offset_of(a.g, 0), from = offset_of(a.g, e), to = offset_of(a.g, e + 1);
-    float sum = 0.0f;
-    if (from >= first && to > from) {
-        const uint32_t t0 = tiles_before<64>(first, from, e), n = (to - from + 63) / 64;
-        for (uint32_t t = 0; t < n; ++t) sum += a.part[(uint64_t)(t0 + t) * a.cols + c];
-    }
-    out[e * ld + c] = (TO)sum;
-}
-
-__global__ __launch_bounds__(256) void grouped_where(GroupedWhere a) {
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+__device__ __forceinline__ void where_rows(const Groups& g, const GroupedWhere& a, uint32_t block) {
+    const uint32_t i = block * 256 + threadIdx.x;
     Run run;
     uint32_t at = kNowhere;
-    if (run_of<64>(a.g, i / 64, run) && run.from + i % 64 < run.to) {
+    if (run_of<64>(g, i / 64, run) && run.from + i % 64 < run.to) {
         const uint32_t row = (uint32_t)a.source[run.from + i % 64];
         if (row < a.x_rows) at = row * a.ld * 2;
     }
-    if (i < 64 * (group_tiles(a.g.rows, a.g.experts, 64) + 1)) a.where[i] = at;
+    if (i < 64 * (group_tiles(g.rows, g.experts, 64) + 1)) a.where[i] = at;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void prepare(Prepare a) {
+    const uint32_t b = blockIdx.x;
+    if (b < a.first[0]) slope_tile<T>(a.g, a.slope, b);
+    else if (b < a.first[1]) lay_rows<T>(a.lay[0], b - a.first[0], a.first[1] - a.first[0]);
+    else if (b < a.first[2]) lay_rows<T>(a.lay[1], b - a.first[1], a.first[2] - a.first[1]);
+    else if (b < a.first[3]) where_rows(a.g, a.where, b - a.first[2]);
+    else if (threadIdx.x < kGroupedCounters) a.counters[threadIdx.x] = 0;
+}
+
+// A workgroup 64 columns of an expert, whose tiles four waves share out.
+template <typename TO>
+__global__ __launch_bounds__(256) void grouped_bias(Groups g, GroupedSlope a, TO* out, uint64_t ld) {
+    __shared__ float sums[4][64];
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t c = blockIdx.x * 64 + lane, e = blockIdx.y;
+    const uint32_t first = offset_of(g, 0), from = offset_of(g, e), to = offset_of(g, e + 1);
+    float sum = 0.0f;
+    if (c < a.cols && from >= first && to > from) {
+        const uint32_t t0 = tiles_before<64>(first, from, e), n = (to - from + 63) / 64;
+        for (uint32_t t = wave; t < n; t += 4) sum += a.part[(uint64_t)(t0 + t) * a.cols + c];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < a.cols) out[e * ld + c] = (TO)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
 }  // namespace
@@ -415,6 +791,35 @@ hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProdu
     return launch_tile<bf16_t, bf16_t>(kind, t, p, s);
 }
 
+template <typename T, typename TO>
+static hipError_t pair_of(const GroupedProduct& rows, const GroupedProduct& weights, uint32_t* counters, hipStream_t s) {
+    typedef typename Tiles<T>::Large G;
+    if constexpr (G::P == 1) {
+        const uint64_t tiles = group_tiles(rows.g.rows, rows.g.experts, G::kBM) * ((uint64_t)(rows.cols + G::kBN - 1) / G::kBN) +
+                               (uint64_t)weights.g.experts * ((weights.rows + G::kBM - 1) / G::kBM) *
+                                   ((weights.cols + G::kBN - 1) / G::kBN);
+        void* args[] = {(void*)&rows, (void*)&weights, (void*)&counters};
+        return launch_large<G>(weights.where ? (const void*)grads_large<G, TO, true> : (const void*)grads_large<G, TO, false>, args,
+                               tiles, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
+                               uint32_t* counters, hipStream_t s) {
+    const bool some = rows.g.rows > 0 && rows.cols > 0 && weights.rows > 0 && weights.cols > 0;
+    if (some && dtype != BC_F32 && tile_for(kGroupedRows, dtype, rows) == 2 && tile_for(kGroupedWeights, dtype, weights) == 2) {
+        if (dtype == BC_F16) {
+            if (out_dtype == BC_F32) return pair_of<f16_t, float>(rows, weights, counters, s);
+            return pair_of<f16_t, f16_t>(rows, weights, counters, s);
+        }
+        if (out_dtype == BC_F32) return pair_of<bf16_t, float>(rows, weights, counters, s);
+        return pair_of<bf16_t, bf16_t>(rows, weights, counters, s);
+    }
+    const hipError_t e = launch_grouped(kGroupedRows, dtype, dtype, rows, s);
+    return e != hipSuccess ? e : launch_grouped(kGroupedWeights, dtype, out_dtype, weights, s);
+}
+
 template <typename T>
 static void few_of(const GroupedFew& a, hipStream_t s) {
     const dim3 grid((a.cols + 3) / 4, std::min(a.g.experts, a.g.rows));
@@ -429,35 +834,32 @@ hipError_t launch_grouped_few(int dtype, const GroupedFew& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_lay_rows(int dtype, const LayRows& a, hipStream_t s) {
-    const uint64_t n = (a.count * (plane_cols(a.cols) / 8) + 255) / 256;
+hipError_t launch_prepare(int dtype, Prepare& a, hipStream_t s) {
+    uint64_t n = 0;
+    if (a.slope.dz || a.slope.part) n += (plane_cols(a.slope.cols) + kSlopeCols - 1) / kSlopeCols * group_tiles(a.g.rows, a.g.experts, 64);
+    for (int i = 0; i < 2; ++i) {
+        a.first[i] = (uint32_t)n;
+        if (a.lay[i].out) n += std::min<uint64_t>((a.lay[i].count * (plane_cols(a.lay[i].cols) / 8) + 255) / 256, 1u << 20);
+    }
+    a.first[2] = (uint32_t)n;
+    if (a.where.where) n += (64 * (group_tiles(a.g.rows, a.g.experts, 64) + 1) + 255) / 256;
+    a.first[3] = (uint32_t)n;
+    if (a.counters) n += 1;
+    a.first[4] = (uint32_t)n;
     if (n == 0) return hipSuccess;
-    const dim3 grid((uint32_t)std::min<uint64_t>(n, 1u << 22)), block(256);
-    if (dtype == BC_F32) hipLaunchKernelGGL(lay_rows<float>, grid, block, 0, s, a);
-    else if (dtype == BC_F16) hipLaunchKernelGGL(lay_rows<f16_t>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(lay_rows<bf16_t>, grid, block, 0, s, a);
+    if (n * 256 >= (1ull << 32)) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)n), block(256);
+    if (dtype == BC_F32) hipLaunchKernelGGL(prepare<float>, grid, block, 0, s, a);
+    else if (dtype == BC_F16) hipLaunchKernelGGL(prepare<f16_t>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(prepare<bf16_t>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 
-hipError_t launch_grouped_slope(int dtype, const GroupedSlope& a, hipStream_t s) {
-    const dim3 grid((uint32_t)(plane_cols(a.cols) / 64) * group_tiles(a.g.rows, a.g.experts, 64)), block(256);
-    if (dtype == BC_F32) hipLaunchKernelGGL(grouped_slope<float>, grid, block, 0, s, a);
-    else if (dtype == BC_F16) hipLaunchKernelGGL(grouped_slope<f16_t>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(grouped_slope<bf16_t>, grid, block, 0, s, a);
-    return hipGetLastError();
-}
-
-hipError_t launch_grouped_bias(int out_dtype, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s) {
-    const dim3 grid((a.cols + 255) / 256, a.g.experts), block(256);
-    if (out_dtype == BC_F32) hipLaunchKernelGGL(grouped_bias<float>, grid, block, 0, s, a, (float*)dbias, ld);
-    else if (out_dtype == BC_F16) hipLaunchKernelGGL(grouped_bias<f16_t>, grid, block, 0, s, a, (f16_t*)dbias, ld);
-    else hipLaunchKernelGGL(grouped_bias<bf16_t>, grid, block, 0, s, a, (bf16_t*)dbias, ld);
-    return hipGetLastError();
-}
-
-hipError_t launch_grouped_where(const GroupedWhere& a, hipStream_t s) {
-    const uint32_t n = 64 * (group_tiles(a.g.rows, a.g.experts, 64) + 1);
-    hipLaunchKernelGGL(grouped_where, dim3((n + 255) / 256), dim3(256), 0, s, a);
+hipError_t launch_grouped_bias(int out_dtype, const Groups& g, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s) {
+    const dim3 grid((a.cols + 63) / 64, g.experts), block(256);
+    if (out_dtype == BC_F32) hipLaunchKernelGGL(grouped_bias<float>, grid, block, 0, s, g, a, (float*)dbias, ld);
+    else if (out_dtype == BC_F16) hipLaunchKernelGGL(grouped_bias<f16_t>, grid, block, 0, s, g, a, (f16_t*)dbias, ld);
+    else hipLaunchKernelGGL(grouped_bias<bf16_t>, grid, block, 0, s, g, a, (bf16_t*)dbias, ld);
     return hipGetLastError();
 }
 
