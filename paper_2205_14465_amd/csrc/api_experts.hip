@@ -425,10 +425,11 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
     if (c.used > 0 && rows > 0 && (!ws || ws_bytes < c.used)) return BC_E_WORKSPACE;
     // (no rows: dw and dbias are zeros)
     hipError_t e = rows > 0 ? launch_prepare(dtype, pre, s) : hipSuccess;
-    if (e == hipSuccess && dbias) e = launch_grouped_bias(gdtype, g, slope, dbias, ld_dbias, s);
+    const GroupedBias bias{g, slope.part, dbias, ld_dbias, (uint32_t)cols};
     if (e == hipSuccess && dx && dw) {
-        e = launch_grouped_pair(dtype, gdtype, px, pw, pre.counters, s);
+        e = launch_grouped_pair(dtype, gdtype, px, pw, bias, pre.counters, s);
     } else {
+        if (e == hipSuccess && dbias) e = launch_grouped_bias(gdtype, bias, s);
         if (e == hipSuccess && dx) e = launch_grouped(kGroupedRows, dtype, dtype, px, s);
         if (e == hipSuccess && dw) e = launch_grouped(kGroupedWeights, dtype, gdtype, pw, s);
     }

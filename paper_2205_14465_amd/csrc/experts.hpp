@@ -96,10 +96,21 @@ struct GroupedProduct {
     bool nt;
 };
 hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProduct& p, hipStream_t s);
-// Both gradients' products.  counters: kGroupedCounters words, zero (launch_prepare).
+// dbias [experts][cols], rows ld apart, from the sums over 64 rows each of
+// GroupedSlope.
+struct GroupedBias {
+    Groups g;
+    const float* part;
+    void* out;
+    uint64_t ld;
+    uint32_t cols;
+};
+hipError_t launch_grouped_bias(int out_dtype, const GroupedBias& a, hipStream_t s);
+// Both gradients' products, none of them empty, and the bias's gradient where
+// bias.out is given.  counters: kGroupedCounters words, zero (launch_prepare).
 constexpr uint32_t kGroupedCounters = 8;
 hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
-                               uint32_t* counters, hipStream_t s);
+                               const GroupedBias& bias, uint32_t* counters, hipStream_t s);
 
 // The forward pass for few rows in all.
 constexpr uint32_t kGroupedFewRows = 64;
@@ -150,8 +161,6 @@ struct Prepare {
     uint32_t first[5];       // workgroups before lay[0], lay[1], where and counters, and in all
 };
 hipError_t launch_prepare(int dtype, Prepare& a, hipStream_t s);
-// The experts' sums of slope.part, rows ld apart.
-hipError_t launch_grouped_bias(int out_dtype, const Groups& g, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s);
 
 // --------------------------------------------------- norm and clipping
 // One matrix of a list (device table; compared by its bytes: no padding).

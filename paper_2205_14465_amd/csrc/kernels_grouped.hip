@@ -160,13 +160,12 @@ __device__ __forceinline__ void begin_weights(R& g, const GroupedProduct& p, uin
 }
 
 template <typename G, typename TO, bool forward>
-__global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
-    extern __shared__ char lds[];
+__device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t block, char* lds) {
     const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN, tiles_m = tiles_in_all<G::kBM>(p.g);
-    if (blockIdx.x >= tiles_m * tiles_n) return;
+    if (block >= tiles_m * tiles_n) return;
     // a die's tiles are consecutive ones, expert by expert
-    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
-    const uint32_t t = die * q + (die < rest ? die : rest) + blockIdx.x / 8;
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8, die = block % 8;
+    const uint32_t t = die * q + (die < rest ? die : rest) + block / 8;
     Run run;
     uint32_t tn;
     if (!tile_run<G::kBM>(p.g, t, tiles_n, run, tn)) return;
@@ -183,11 +182,10 @@ __global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
 
 // dw: every expert's tiles, over its rows.
 template <typename G, typename TO, bool kTable>
-__global__ __launch_bounds__(G::kThreads) void weights_product(GroupedProduct p) {
-    extern __shared__ char lds[];
+__device__ __forceinline__ void weights_tile(const GroupedProduct& p, uint32_t block, char* lds) {
     const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     // an expert's tiles go to all dies, each a run of consecutive ones
-    const uint32_t each = tiles_m * tiles_n, e = blockIdx.x / each, j = blockIdx.x - e * each;
+    const uint32_t each = tiles_m * tiles_n, e = block / each, j = block - e * each;
     const uint32_t in = j % 8 * (each / 8) + (j % 8 < each % 8 ? j % 8 : each % 8) + j / 8;
     const uint32_t m0 = in / tiles_n * G::kBM, n0 = in % tiles_n * G::kBN;
     RunTile<G> g;
@@ -199,6 +197,53 @@ __global__ __launch_bounds__(G::kThreads) void weights_product(GroupedProduct p)
         if (m < p.rows && n < p.cols)
             store_vec((TO*)p.out + e * p.expert_out + m * p.ld_out + n, (int)(p.cols - n), v, p.nt);
     });
+}
+
+template <typename G, typename TO, bool forward>
+__global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
+    extern __shared__ char lds[];
+    rows_tile<G, TO, forward>(p, blockIdx.x, lds);
+}
+
+template <typename G, typename TO, bool kTable>
+__global__ __launch_bounds__(G::kThreads) void weights_product(GroupedProduct p) {
+    extern __shared__ char lds[];
+    weights_tile<G, TO, kTable>(p, blockIdx.x, lds);
+}
+
+// dbias: 64 columns of an expert, whose sums over 64 rows each the first four waves
+// share out.
+template <typename TO>
+__device__ __forceinline__ void bias_columns(const GroupedBias& a, uint32_t block, float* sums) {
+    const uint32_t across = (a.cols + 63) / 64, e = block / across;
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = block % across * 64 + lane;
+    const uint32_t first = offset_of(a.g, 0), from = offset_of(a.g, e), to = offset_of(a.g, e + 1);
+    float sum = 0.0f;
+    if (wave < 4 && c < a.cols && from >= first && to > from) {
+        const uint32_t t0 = tiles_before<64>(first, from, e), n = (to - from + 63) / 64;
+        for (uint32_t t = wave; t < n; t += 4) sum += a.part[(uint64_t)(t0 + t) * a.cols + c];
+    }
+    if (wave < 4) sums[wave * 64 + lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < a.cols)
+        ((TO*)a.out)[e * a.ld + c] = (TO)((sums[lane] + sums[64 + lane]) + (sums[128 + lane] + sums[192 + lane]));
+}
+
+// Both gradients' products where tiles of this size do not fill the chip, and dbias:
+// `split` workgroups of the first product (dx's with rows_first: the one whose k is the
+// longer), those of the second up to `end`, then the bias's.
+template <typename G, typename TO, bool kTable>
+__global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, GroupedProduct pw, GroupedBias bias, uint32_t split,
+                                                             uint32_t end, bool rows_first) {
+    extern __shared__ char lds[];
+    if (blockIdx.x >= end) {
+        bias_columns<TO>(bias, blockIdx.x - end, (float*)lds);
+        return;
+    }
+    const bool first = blockIdx.x < split;
+    const uint32_t block = first ? blockIdx.x : blockIdx.x - split;
+    if (first == rows_first) rows_tile<G, std::conditional_t<(G::P > 1), float, typename G::T>, false>(px, block, lds);
+    else weights_tile<G, TO, kTable>(pw, block, lds);
 }
 
 // ---------------------------------------------------------- large products
@@ -536,26 +581,45 @@ struct TileCost {
 constexpr TileCost kCost16[3] = {{64, 64, 0.30, 0.193, 0.5}, {128, 128, 0.60, 0.53, 2.0}, {256, 256, 1.05, 1.50, 11.0}};
 constexpr TileCost kCost32[3] = {{64, 64, 0.82, 0.95, 0.5}, {128, 128, 1.86, 2.56, 1.5}, {256, 128, 3.4, 4.68, 8.7}};
 
-int tile_for(int kind, int dtype, const GroupedProduct& p) {
+// A product in tiles of one size: rounds over the chip's 256 units, a tile's time alone
+// and on a full chip.
+struct Load {
+    double rounds, alone, full;
+};
+Load load_of(int kind, const GroupedProduct& p, const TileCost& c) {
+    const double rows = (double)p.g.rows, experts = (double)p.g.experts, across = std::ceil((double)p.cols / c.cols);
+    const bool weights = kind == kGroupedWeights;
+    // (half a tile of every run is past its end)
+    const double tiles = weights ? experts * std::ceil((double)p.rows / c.rows) * across
+                                 : (rows / c.rows + std::fmin(experts, rows) * 0.5) * across;
+    const double steps = std::ceil((weights ? rows / experts : (double)p.k) / 64.0);
+    return Load{tiles / 256.0, steps * c.alone + c.ends, steps * c.full + c.ends};
+}
+// The cheapest tile for one product; least: its time.
+int tile_for(int kind, int dtype, const GroupedProduct& p, double& least) {
     const TileCost* cost = dtype == BC_F32 ? kCost32 : kCost16;
     int best = 0;
-    double least = 1e300;
+    least = 1e300;
     for (int i = 0; i < 3; ++i) {
-        const TileCost& c = cost[i];
-        const double rows = (double)p.g.rows, experts = (double)p.g.experts;
-        const double across = std::ceil((double)p.cols / c.cols);
-        double tiles, k;
-        if (kind == kGroupedWeights) {
-            tiles = experts * std::ceil((double)p.rows / c.rows) * across;
-            k = rows / experts;
-        } else {
-            // half a tile of every run is past its end
-            tiles = (rows / c.rows + std::fmin(experts, rows) * 0.5) * across;
-            k = (double)p.k;
+        const Load l = load_of(kind, p, cost[i]);
+        const double busy = i == 2 ? std::ceil(l.rounds) * l.full : l.rounds <= 1.0 ? 0.0 : (l.rounds + 0.5) * l.full;
+        const double t = std::fmax(l.alone, busy);
+        if (t < least) {
+            least = t;
+            best = i;
         }
-        const double steps = std::ceil(k / 64.0), full = steps * c.full + c.ends, n = tiles / 256.0;
-        const double busy = i == 2 ? std::ceil(n) * full : n <= 1.0 ? 0.0 : (n + 0.5) * full;
-        const double t = std::fmax(steps * c.alone + c.ends, busy);
+    }
+    return best;
+}
+// The same for both gradients' products in one launch.
+int tile_for_both(int dtype, const GroupedProduct& rows, const GroupedProduct& weights, double& least) {
+    const TileCost* cost = dtype == BC_F32 ? kCost32 : kCost16;
+    int best = 0;
+    least = 1e300;
+    for (int i = 0; i < 3; ++i) {
+        const Load x = load_of(kGroupedRows, rows, cost[i]), w = load_of(kGroupedWeights, weights, cost[i]);
+        const double n = x.rounds + w.rounds, busy = x.rounds * x.full + w.rounds * w.full;
+        const double t = std::fmax(std::fmax(x.alone, w.alone), n <= 1.0 ? 0.0 : busy + 0.5 * std::fmin(x.full, w.full));
         if (t < least) {
             least = t;
             best = i;
@@ -760,28 +824,18 @@ __global__ __launch_bounds__(256) void prepare(Prepare a) {
     else if (threadIdx.x < kGroupedCounters) a.counters[threadIdx.x] = 0;
 }
 
-// A workgroup 64 columns of an expert, whose tiles four waves share out.
 template <typename TO>
-__global__ __launch_bounds__(256) void grouped_bias(Groups g, GroupedSlope a, TO* out, uint64_t ld) {
-    __shared__ float sums[4][64];
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint32_t c = blockIdx.x * 64 + lane, e = blockIdx.y;
-    const uint32_t first = offset_of(g, 0), from = offset_of(g, e), to = offset_of(g, e + 1);
-    float sum = 0.0f;
-    if (c < a.cols && from >= first && to > from) {
-        const uint32_t t0 = tiles_before<64>(first, from, e), n = (to - from + 63) / 64;
-        for (uint32_t t = wave; t < n; t += 4) sum += a.part[(uint64_t)(t0 + t) * a.cols + c];
-    }
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && c < a.cols) out[e * ld + c] = (TO)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+__global__ __launch_bounds__(256) void grouped_bias(GroupedBias a) {
+    __shared__ float sums[256];
+    bias_columns<TO>(a, blockIdx.x, sums);
 }
 
 }  // namespace
 
 hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProduct& p, hipStream_t s) {
     if (p.cols == 0 || (kind == kGroupedWeights ? p.rows == 0 || p.g.experts == 0 : p.g.rows == 0)) return hipSuccess;
-    const int t = tile_for(kind, dtype, p);
+    double least;
+    const int t = tile_for(kind, dtype, p, least);
     if (dtype == BC_F32) return launch_tile<float, float>(kind, t, p, s);
     if (dtype == BC_F16) {
         if (out_dtype == BC_F32) return launch_tile<f16_t, float>(kind, t, p, s);
@@ -791,33 +845,58 @@ hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProdu
     return launch_tile<bf16_t, bf16_t>(kind, t, p, s);
 }
 
-template <typename T, typename TO>
-static hipError_t pair_of(const GroupedProduct& rows, const GroupedProduct& weights, uint32_t* counters, hipStream_t s) {
-    typedef typename Tiles<T>::Large G;
-    if constexpr (G::P == 1) {
-        const uint64_t tiles = group_tiles(rows.g.rows, rows.g.experts, G::kBM) * ((uint64_t)(rows.cols + G::kBN - 1) / G::kBN) +
-                               (uint64_t)weights.g.experts * ((weights.rows + G::kBM - 1) / G::kBM) *
-                                   ((weights.cols + G::kBN - 1) / G::kBN);
-        void* args[] = {(void*)&rows, (void*)&weights, (void*)&counters};
-        return launch_large<G>(weights.where ? (const void*)grads_large<G, TO, true> : (const void*)grads_large<G, TO, false>, args,
-                               tiles, s);
+template <typename G, typename TO>
+static hipError_t pair_of(GroupedProduct x, GroupedProduct w, GroupedBias bias, uint32_t* counters, hipStream_t s) {
+    const uint64_t tiles_x = group_tiles(x.g.rows, x.g.experts, G::kBM) * ((uint64_t)(x.cols + G::kBN - 1) / G::kBN);
+    const uint64_t tiles_w = (uint64_t)w.g.experts * ((w.rows + G::kBM - 1) / G::kBM) * ((w.cols + G::kBN - 1) / G::kBN);
+    if constexpr (G::P == 1 && G::kBM == 256) {
+        if (bias.out) {
+            const hipError_t e = launch_grouped_bias(sizeof(TO) == 4 ? (int)BC_F32 : __is_same(TO, f16_t) ? (int)BC_F16 : (int)BC_BF16, bias, s);
+            if (e != hipSuccess) return e;
+        }
+        void* args[] = {&x, &w, &counters};
+        return launch_large<G>(w.where ? (const void*)grads_large<G, TO, true> : (const void*)grads_large<G, TO, false>, args,
+                               tiles_x + tiles_w, s);
+    } else {
+        bool rows_first = x.k >= w.g.rows / w.g.experts;
+        uint32_t split = (uint32_t)(rows_first ? tiles_x : tiles_w), end = (uint32_t)(tiles_x + tiles_w);
+        const uint64_t grid = end + (bias.out ? (uint64_t)bias.g.experts * ((bias.cols + 63) / 64) : 0);
+        const void* kernel = w.where ? (const void*)grads_product<G, TO, true> : (const void*)grads_product<G, TO, false>;
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
+        if (e != hipSuccess) return e;
+        if (grid * G::kThreads >= (1ull << 32)) return hipErrorInvalidValue;
+        void* args[] = {&x, &w, &bias, &split, &end, &rows_first};
+        return hipLaunchKernel(kernel, dim3((uint32_t)grid), dim3(G::kThreads), args, G::kLdsBytes, s);
     }
-    return hipErrorInvalidValue;
 }
 
-hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
+template <typename T, typename TO>
+static hipError_t pair_tile(int tile, const GroupedProduct& x, const GroupedProduct& w, const GroupedBias& bias,
+                            uint32_t* counters, hipStream_t s) {
+    if (tile == 0) return pair_of<typename Tiles<T>::Small, TO>(x, w, bias, counters, s);
+    if (tile == 1) return pair_of<typename Tiles<T>::Middle, TO>(x, w, bias, counters, s);
+    return pair_of<typename Tiles<T>::Large, TO>(x, w, bias, counters, s);
+}
+
+hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& x, const GroupedProduct& w, const GroupedBias& bias,
                                uint32_t* counters, hipStream_t s) {
-    const bool some = rows.g.rows > 0 && rows.cols > 0 && weights.rows > 0 && weights.cols > 0;
-    if (some && dtype != BC_F32 && tile_for(kGroupedRows, dtype, rows) == 2 && tile_for(kGroupedWeights, dtype, weights) == 2) {
+    double both = 0.0, tx = 0.0, tw = 0.0;
+    tile_for(kGroupedRows, dtype, x, tx);
+    tile_for(kGroupedWeights, dtype, w, tw);
+    const int tile = tile_for_both(dtype, x, w, both);
+    // (a launch of its own: 3 us, and the bias's another 3)
+    if (both < tx + tw + 3.0 + (bias.out && tile < 2 ? 3.0 : 0.0)) {
+        if (dtype == BC_F32) return pair_tile<float, float>(tile, x, w, bias, counters, s);
         if (dtype == BC_F16) {
-            if (out_dtype == BC_F32) return pair_of<f16_t, float>(rows, weights, counters, s);
-            return pair_of<f16_t, f16_t>(rows, weights, counters, s);
+            if (out_dtype == BC_F32) return pair_tile<f16_t, float>(tile, x, w, bias, counters, s);
+            return pair_tile<f16_t, f16_t>(tile, x, w, bias, counters, s);
         }
-        if (out_dtype == BC_F32) return pair_of<bf16_t, float>(rows, weights, counters, s);
-        return pair_of<bf16_t, bf16_t>(rows, weights, counters, s);
+        if (out_dtype == BC_F32) return pair_tile<bf16_t, float>(tile, x, w, bias, counters, s);
+        return pair_tile<bf16_t, bf16_t>(tile, x, w, bias, counters, s);
     }
-    const hipError_t e = launch_grouped(kGroupedRows, dtype, dtype, rows, s);
-    return e != hipSuccess ? e : launch_grouped(kGroupedWeights, dtype, out_dtype, weights, s);
+    hipError_t e = bias.out ? launch_grouped_bias(out_dtype, bias, s) : hipSuccess;
+    if (e == hipSuccess) e = launch_grouped(kGroupedRows, dtype, dtype, x, s);
+    return e != hipSuccess ? e : launch_grouped(kGroupedWeights, dtype, out_dtype, w, s);
 }
 
 template <typename T>
@@ -855,11 +934,11 @@ hipError_t launch_prepare(int dtype, Prepare& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_grouped_bias(int out_dtype, const Groups& g, const GroupedSlope& a, void* dbias, uint64_t ld, hipStream_t s) {
-    const dim3 grid((a.cols + 63) / 64, g.experts), block(256);
-    if (out_dtype == BC_F32) hipLaunchKernelGGL(grouped_bias<float>, grid, block, 0, s, g, a, (float*)dbias, ld);
-    else if (out_dtype == BC_F16) hipLaunchKernelGGL(grouped_bias<f16_t>, grid, block, 0, s, g, a, (f16_t*)dbias, ld);
-    else hipLaunchKernelGGL(grouped_bias<bf16_t>, grid, block, 0, s, g, a, (bf16_t*)dbias, ld);
+hipError_t launch_grouped_bias(int out_dtype, const GroupedBias& a, hipStream_t s) {
+    const dim3 grid((a.cols + 63) / 64 * a.g.experts), block(256);
+    if (out_dtype == BC_F32) hipLaunchKernelGGL(grouped_bias<float>, grid, block, 0, s, a);
+    else if (out_dtype == BC_F16) hipLaunchKernelGGL(grouped_bias<f16_t>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(grouped_bias<bf16_t>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 
