@@ -672,7 +672,7 @@ int bytecomp_combine_backward(int dtype, uint64_t rows, uint64_t cols, uint32_t 
  *   ws        at least bytecomp_grouped_linear_workspace_size bytes, 16-byte
  *             aligned; NULL is fine where that is 0
  * fp32 products are sums of bfloat16 products of the operands' three parts,
- * as the linear layer's; at most 64 rows are summed in fp32.
+ * as the linear layer's, or fp32 ones where there are few rows.
  * 1 <= experts <= 1024 (BC_E_COUNT); rows < 2^22, x_rows < 2^31, inner and
  * cols < 2^20, and as many elements as rows + 64 experts rows of inner or of cols,
  * and as the weights, have: less than 2^35, with inner and cols as whole 64s

@@ -106,7 +106,7 @@ size_t grouped_ws(int dtype, uint64_t rows, uint64_t x_rows, uint64_t inner, uin
     // (with or without a gather, whichever takes more)
     const size_t x = planes_bytes(dtype, std::max(rows, x_rows <= rows ? x_rows : 0), inner);
     const size_t w = planes_bytes(dtype, experts * cols, inner);
-    if (!backward) return rows <= kGroupedFewRows ? 0 : x + w;
+    if (!backward) return rows <= grouped_few_rows(dtype, experts, true) ? 0 : x + w;
     return x + w + planes_bytes(dtype, rows, cols) + part_bytes(rows, experts, cols) + where_bytes(rows, experts) +
            align256(kGroupedCounters * sizeof(uint32_t));
 }
@@ -325,7 +325,9 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
         return BC_E_ALIGN;
     hipStream_t s = (hipStream_t)stream;
     const Groups g{offsets, experts, (uint32_t)rows};
-    if (rows <= kGroupedFewRows) {
+    const bool lies = readable(dtype, x, ldx, inner) && (!source || x_rows * ldx * 2 <= kGatherBytes) &&
+                      readable(dtype, w, ldw, inner) && expert_w % 8 == 0;
+    if (rows <= grouped_few_rows(dtype, experts, !lies)) {
         const GroupedFew a{g, x, w, bias, source, y, z, ldx, ldw, expert_w, ld_bias, ldy, ldz,
                            (uint32_t)(source ? x_rows : rows), (uint32_t)inner, (uint32_t)cols, act};
         return finish_call(status_of(launch_grouped_few(dtype, a, s)), s, nullptr);

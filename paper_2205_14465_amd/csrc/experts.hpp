@@ -112,8 +112,15 @@ constexpr uint32_t kGroupedCounters = 8;
 hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
                                const GroupedBias& bias, uint32_t* counters, hipStream_t s);
 
-// The forward pass for few rows in all.
-constexpr uint32_t kGroupedFewRows = 64;
+// The forward pass for few rows, which needs no workspace: up to 64 in all, more where w
+// would be laid out first (four to ten bytes an element moved for a product that reads
+// two or four).  us, this way and by tiles: fp32, 8 experts of 1600x1600, 128 rows 28 and
+// 59, 256 50 and 74, 512 83 and 78; 64 experts 128 rows 125 and 495, 1024 205 and 526;
+// fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows 32 and 36, 1024
+// 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
+inline uint64_t grouped_few_rows(int dtype, uint32_t experts, bool laid_out) {
+    return 64 + (!laid_out ? 0 : dtype == BC_F32 ? 32ull * experts : 8ull * experts);
+}
 struct GroupedFew {
     Groups g;
     const void *x, *w, *bias;

@@ -12,6 +12,7 @@
 // kernels_linear.hip does it.
 #include "act.hpp"
 #include "experts.hpp"
+#include "few.hpp"
 #include "launch.hpp"
 #include "run_tile.hpp"
 
@@ -720,6 +721,85 @@ __global__ __launch_bounds__(256) void grouped_few(GroupedFew a) {
     }
 }
 
+// Sixteen rows of w by up to 16 kGroups of the expert's rows on the matrix cores: the
+// waves share out the inner axis and meet in LDS.
+constexpr int kFewWaves = 8;
+template <typename T, int kGroups>
+__device__ __forceinline__ void few_block(const GroupedFew& a, uint32_t e, uint32_t r0, uint32_t to, float* meet) {
+    typedef FewFrag<T> F;
+    constexpr int kEach = F::kStep / 4, kAhead = kGroups > 1 ? 2 : 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t n0 = blockIdx.x * 16, n = n0 + (lane & 15), kl = (lane >> 4) * kEach;
+    const T* w = (const T*)a.w + e * a.expert_w + (uint64_t)(n < a.cols ? n : a.cols - 1) * a.ldw;
+    const T* x[kGroups];
+    bool there[kGroups];
+    f32x4_t acc[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const uint32_t m = r0 + g * 16 + (lane & 15), r = m < to ? m : r0;
+        const uint32_t row = a.source ? (uint32_t)a.source[r] : r;
+        there[g] = row < a.x_rows;  // a row from nowhere is zeros
+        x[g] = (const T*)a.x + (uint64_t)(there[g] ? row : 0) * a.ldx;
+        acc[g] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const uint32_t steps = (a.inner + F::kStep - 1) / F::kStep, whole = a.inner / F::kStep;
+    uint32_t s = wave;
+    for (; s + (kAhead - 1) * kFewWaves < whole; s += kAhead * kFewWaves) {
+        typename F::type fw[kAhead], fx[kAhead][kGroups];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t k = (s + u * kFewWaves) * F::kStep + kl;
+            F::load(w + k, kEach, fw[u]);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) F::load(x[g] + k, there[g] ? kEach : 0, fx[u][g]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) acc[g] = F::mma(fw[u], fx[u][g], acc[g]);
+    }
+    for (; s < steps; s += kFewWaves) {
+        const uint32_t k = s * F::kStep + kl;
+        const int left = k < a.inner ? (int)(a.inner - k) : 0;
+        typename F::type fw, fx;
+        F::load(w + (left ? k : 0), left, fw);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            F::load(x[g] + (left ? k : 0), there[g] ? left : 0, fx);
+            acc[g] = F::mma(fw, fx, acc[g]);
+        }
+    }
+    // [wave][group][row][17]
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) meet[((wave * kGroups + g) * 16 + (lane & 15)) * 17 + (lane >> 4) * 4 + r] = acc[g][r];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 256 * kGroups; i += 64 * kFewWaves) {
+        const uint64_t r = r0 + i / 16;
+        const uint32_t c = n0 + i % 16;
+        if (r >= to || c >= a.cols) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kFewWaves; ++q) v += meet[(q * kGroups * 16 + i / 16) * 17 + i % 16];
+        if (a.bias) v += (float)((const T*)a.bias)[e * a.ld_bias + c];
+        if (a.z) ((T*)a.z)[r * a.ldz + c] = (T)v;
+        ((T*)a.y)[r * a.ldy + c] = (T)activate<sizeof(T) == 4>(a.act, v);
+    }
+}
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void grouped_few_tiles(GroupedFew a) {
+    __shared__ float meet[kFewWaves * 2 * 16 * 17];
+    uint32_t from, to;
+    const int e = busy_expert(a.g, blockIdx.y, from, to);
+    if (e < 0) return;
+    for (uint32_t r0 = from; r0 < to; r0 += 32) {
+        if (to - r0 <= 16) few_block<T, 1>(a, (uint32_t)e, r0, to, meet);
+        else few_block<T, 2>(a, (uint32_t)e, r0, to, meet);
+    }
+}
+
 // ---------------------------------------------------- what products are given
 template <typename T>
 __device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint32_t blocks) {
@@ -901,6 +981,10 @@ hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& x
 
 template <typename T>
 static void few_of(const GroupedFew& a, hipStream_t s) {
+    if (a.g.rows > (sizeof(T) == 4 ? 8 : 4)) {
+        hipLaunchKernelGGL(grouped_few_tiles<T>, dim3((a.cols + 15) / 16, std::min(a.g.experts, a.g.rows)), dim3(64 * kFewWaves), 0, s, a);
+        return;
+    }
     const dim3 grid((a.cols + 3) / 4, std::min(a.g.experts, a.g.rows));
     if (a.inner % kVec<T> == 0) hipLaunchKernelGGL((grouped_few<T, true>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((grouped_few<T, false>), grid, dim3(256), 0, s, a);

@@ -14,6 +14,7 @@
 // unit in the last place of one term of dx and dw, whose own results are
 // rounded once to the same type.  dbias is the fp32 sum of the unrounded dz.
 #include "act.hpp"
+#include "few.hpp"
 #include "gemm.hpp"
 #include "launch.hpp"
 #include "layers.hpp"
@@ -261,45 +262,6 @@ hipError_t launch_pair_of(int tile, const Product& p, const Product& q, hipStrea
 // loads that cols / 16 workgroups keep in flight: 16 rows in fp16, 1600 by 6400
 // 8.5 us (2.4 TB/s), 6400 by 1600 13.7; in fp32, 4096 by 4096 20 (3.4 TB/s).
 constexpr int kFewWaves = 8;
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-template <typename T>
-struct FewFrag {
-    typedef typename Frag<T>::type type;
-    static constexpr int kStep = 32;
-    static __device__ __forceinline__ void load(const T* p, int left, type& f) {
-        if (left >= 8) {
-            __builtin_memcpy(&f, p, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = i < left ? p[i] : (T)0.0f;
-        }
-    }
-    static __device__ __forceinline__ f32x4_t mma(type a, type b, f32x4_t c) {
-        if constexpr (__is_same(T, f16_t)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    }
-};
-// fp32: four 16x16x4 instructions, the k of lane group g's element i being
-// 4 g + i in both operands.
-template <>
-struct FewFrag<float> {
-    typedef f32x4_t type;
-    static constexpr int kStep = 16;
-    static __device__ __forceinline__ void load(const float* p, int left, type& f) {
-        if (left >= 4) {
-            __builtin_memcpy(&f, p, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = i < left ? p[i] : 0.0f;
-        }
-    }
-    static __device__ __forceinline__ f32x4_t mma(type a, type b, f32x4_t c) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-        return c;
-    }
-};
 
 template <typename T, int kGroups>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows(FewRows a) {

@@ -88,10 +88,12 @@ def test_grouped_linear_refusals():
     assert fwd(x=P(0x10001)) == -9 and fwd(off=ODD) == -9 and fwd(src=ODD, x_rows=5) == -9
     assert fwd(ws=P(0x40008), n=1 << 30) == -9
     assert fwd(rows=0) == 0 and fwd(cols=0) == 0
-    need = B.bytecomp_grouped_linear_workspace_size(0, 70, 70, 64, 32, 3)
-    assert need > 0 and fwd(dtype=0) == -7 and fwd(dtype=0, ws=WS, n=need - 1) == -7
-    assert fwd(inner=63) == -7 and fwd(inner=60) == -7
+    # many rows of fp32 and odd sizes are laid out first
+    need = B.bytecomp_grouped_linear_workspace_size(0, 700, 700, 64, 32, 3)
+    assert need > 0 and fwd(dtype=0, rows=700) == -7 and fwd(dtype=0, rows=700, ws=WS, n=need - 1) == -7
+    assert fwd(rows=700, inner=63) == -7 and fwd(rows=700, inner=60) == -7
     assert B.bytecomp_grouped_linear_workspace_size(0, 64, 64, 64, 32, 3) == 0
+    assert B.bytecomp_grouped_linear_workspace_size(1, 64 + 8 * 3, 9, 63, 32, 3) == 0
 
     def bwd(dtype=1, gdtype=1, rows=70, off=O, dy=Y, lddy=32, z=Y, ldz=32, act=1, x=X, ldx=64, src=None, w=W, ldw=64,
             each=2048, dx=X, lddx=64, dw=W, lddw=64, each_d=2048, db=W, lddb=32, ws=WS, n=1 << 30):

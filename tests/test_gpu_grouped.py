@@ -252,7 +252,7 @@ def test_special_values_stay_with_their_rows_and_experts():
     import torch
     from paper_2205_14465_amd import binding as B
     nan, inf = float("nan"), float("inf")
-    for counts in ([3, 2, 1], [100, 130, 60]):
+    for counts in ([3, 2, 1], [30, 30, 40], [100, 130, 60], [400, 700, 60]):
         for dtype in (torch.float16, torch.float32):
             n, off = sum(counts), torch.from_numpy(np.cumsum([0] + counts).astype(np.int32)).cuda()
             x = torch.randn(n, 64, device="cuda").to(dtype)
@@ -261,7 +261,7 @@ def test_special_values_stay_with_their_rows_and_experts():
             w[1, 7, 3] = inf
             y, ws = torch.empty(n, 96, dtype=dtype, device="cuda"), None
             if n > 64 and dtype == torch.float32:
-                ws = B.alloc_grouped_linear_workspace(x, w, n)
+                ws = B.alloc_grouped_linear_workspace(x, w, n, backward=True)
             B.bytecomp_grouped_linear_forward(x, None, off, w, None, "relu", y, None, ws)
             a, b = counts[0], counts[0] + counts[1]
             assert y[1].isnan().all() and y[0].isfinite().all() and y[2:a].isfinite().all() and y[b:].isfinite().all()
@@ -372,15 +372,15 @@ def test_other_stream_and_graph():
 def test_wrong_tensors_raise():
     import torch
     from paper_2205_14465_amd import binding as B
-    x, w = torch.randn(70, 64, device="cuda"), torch.randn(3, 32, 64, device="cuda")
-    y, off = torch.empty(70, 32, device="cuda"), torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
-    ws = B.alloc_grouped_linear_workspace(x, w, 70)
+    x, w = torch.randn(700, 64, device="cuda"), torch.randn(3, 32, 64, device="cuda")
+    y, off = torch.empty(700, 32, device="cuda"), torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
+    ws = B.alloc_grouped_linear_workspace(x, w, 700)
 
     def f(x=x, src=None, off=off, w=w, b=None, act="none", y=y, z=None, ws=ws):
         B.bytecomp_grouped_linear_forward(x, src, off, w, b, act, y, z, ws)
     f()
     for bad in (dict(w=w.half()), dict(w=w[:, :, :60]), dict(w=w[0]), dict(w=w.transpose(1, 2).contiguous().transpose(1, 2)),
-                dict(w=w[:1].expand(3, 32, 64)), dict(x=x[:69]), dict(off=off[:3]), dict(off=off.long()), dict(act="swish"),
+                dict(w=w[:1].expand(3, 32, 64)), dict(x=x[:699]), dict(off=off[:3]), dict(off=off.long()), dict(act="swish"),
                 dict(src=off), dict(b=torch.zeros(3, 31, device="cuda")), dict(w=w.cpu()), dict(y=y.half())):
         with pytest.raises(ValueError):
             f(**bad)
