@@ -671,12 +671,11 @@ int bytecomp_combine_backward(int dtype, uint64_t rows, uint64_t cols, uint32_t 
  *             behind the last are left as they were.  y comes from the unrounded z.
  *   ws        at least bytecomp_grouped_linear_workspace_size bytes, 16-byte
  *             aligned; NULL is fine where that is 0
- * fp32 products are sums of bfloat16 products of the operands' three parts,
- * as the linear layer's, or fp32 ones where there are few rows.
+ * Products and their sums are fp32's.
  * 1 <= experts <= 1024 (BC_E_COUNT); rows < 2^22, x_rows < 2^31, inner and
  * cols < 2^20, and as many elements as rows + 64 experts rows of inner or of cols,
- * and as the weights, have: less than 2^35, with inner and cols as whole 64s
- * (BC_E_SIZE).  Zero inner: the products are zero. */
+ * and as the weights, have: less than 2^35, with inner and cols as whole 64s; row
+ * strides of x, w and dy < 2^21 (BC_E_SIZE).  Zero inner: the products are zero. */
 int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, uint32_t experts,
                                     const int32_t* offsets, const void* x, uint64_t ldx, const int32_t* source,
                                     uint64_t x_rows, const void* w, uint64_t ldw, uint64_t expert_w, const void* bias,

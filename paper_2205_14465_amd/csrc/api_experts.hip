@@ -64,24 +64,29 @@ int check_grouped(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, uint3
     return BC_OK;
 }
 
-size_t planes_bytes(int dtype, uint64_t rows, uint64_t k) {
-    return align256((size_t)(rows * plane_cols(k) * 2 * (uint64_t)planes_of(dtype)));
+// Bytes of rows laid out for the tiles.
+size_t laid_bytes(int dtype, uint64_t rows, uint64_t k) {
+    return align256((size_t)(rows * plane_cols(k) * dtype_bytes(dtype)));
 }
 
-// Whether the tiles can read 16-bit rows of k where they lie.
-bool readable(int dtype, const void* p, uint64_t ld, uint64_t k) {
-    return dtype != BC_F32 && k % 8 == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1ull << 21);
+// Whether rows of k are whole 16-byte pieces.
+bool whole(int dtype, const void* p, uint64_t ld, uint64_t k) {
+    const uint64_t each = 16 / dtype_bytes(dtype);
+    return k % each == 0 && ((uintptr_t)p & 15) == 0 && ld % each == 0;
 }
-// Byte offsets of gathered rows are 32-bit.
+// Whether the tiles can read rows of k where they lie: fp32 in any pieces.
+bool readable(int dtype, const void* p, uint64_t ld, uint64_t k) {
+    return dtype == BC_F32 || whole(dtype, p, ld, k);
+}
+// Byte offsets within a tile are 32-bit: row strides below this, in elements.
+constexpr uint64_t kMaxStride = 1ull << 21;
+// So are those of gathered rows.
 constexpr uint64_t kGatherBytes = 0x7fffff00u;
 
 // x laid out: its own rows, or, where the call takes fewer or they are too many
 // for 32-bit offsets, the call's rows one after the other.
-bool lay_own_rows(bool gather, uint64_t rows, uint64_t x_rows, uint64_t inner) {
-    return !gather || (x_rows <= rows && x_rows * plane_cols(inner) * 2 <= kGatherBytes);
-}
-uint64_t laid_rows(bool gather, uint64_t rows, uint64_t x_rows, uint64_t inner) {
-    return gather && lay_own_rows(gather, rows, x_rows, inner) ? x_rows : rows;
+bool lay_own_rows(int dtype, bool gather, uint64_t rows, uint64_t x_rows, uint64_t inner) {
+    return !gather || (x_rows <= rows && x_rows * plane_cols(inner) * dtype_bytes(dtype) <= kGatherBytes);
 }
 
 struct Carver {
@@ -101,13 +106,12 @@ size_t part_bytes(uint64_t rows, uint32_t experts, uint64_t cols) {
     return align256((size_t)group_tiles((uint32_t)rows, experts, 64) * cols * 4);
 }
 
-size_t grouped_ws(int dtype, uint64_t rows, uint64_t x_rows, uint64_t inner, uint64_t cols, uint32_t experts, bool backward) {
+size_t grouped_ws(int dtype, uint64_t rows, uint64_t inner, uint64_t cols, uint32_t experts, bool backward) {
     if (rows == 0) return 0;
-    // (with or without a gather, whichever takes more)
-    const size_t x = planes_bytes(dtype, std::max(rows, x_rows <= rows ? x_rows : 0), inner);
-    const size_t w = planes_bytes(dtype, experts * cols, inner);
+    // (fp32: a gather from more than 2 GB lays x out, nothing does w)
+    const size_t x = laid_bytes(dtype, rows, inner), w = dtype == BC_F32 ? 0 : laid_bytes(dtype, experts * cols, inner);
     if (!backward) return rows <= grouped_few_rows(dtype, experts, true) ? 0 : x + w;
-    return x + w + planes_bytes(dtype, rows, cols) + part_bytes(rows, experts, cols) + where_bytes(rows, experts) +
+    return x + w + laid_bytes(dtype, rows, cols) + part_bytes(rows, experts, cols) + where_bytes(rows, experts) +
            align256(kGroupedCounters * sizeof(uint32_t));
 }
 
@@ -118,28 +122,34 @@ struct GroupedX {
     uint64_t rows, call_rows, inner;
 };
 // x for the tiles; `source` becomes NULL where its rows now follow each other.
-GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, Carver& c, LayRows& lay) {
+GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, bool& wide, Carver& c, LayRows& lay) {
     const bool gather = x.source != nullptr;
     a_rows = (uint32_t)(gather ? x.rows : x.call_rows);
-    if (readable(dtype, x.x, x.ld, x.inner) && (!gather || x.rows * x.ld * 2 <= kGatherBytes))
-        return GroupedSide{x.x, x.ld, 0, 0};
-    const uint64_t n = laid_rows(gather, x.call_rows, x.rows, x.inner), pc = plane_cols(x.inner);
-    const bool own = lay_own_rows(gather, x.call_rows, x.rows, x.inner);
-    void* to = c.take(planes_bytes(dtype, n, x.inner));
+    if (readable(dtype, x.x, x.ld, x.inner) && (!gather || x.rows * x.ld * dtype_bytes(dtype) <= kGatherBytes)) {
+        wide = wide && whole(dtype, x.x, x.ld, x.inner);
+        return GroupedSide{x.x, x.ld, 0};
+    }
+    const bool own = lay_own_rows(dtype, gather, x.call_rows, x.rows, x.inner);
+    const uint64_t n = gather && own ? x.rows : x.call_rows, pc = plane_cols(x.inner);
+    void* to = c.take(laid_bytes(dtype, n, x.inner));
     lay = LayRows{x.x, own ? nullptr : x.source, to, x.ld, 0, n, n, (uint32_t)x.inner, (uint32_t)x.rows};
     if (!own) {
         x.source = nullptr;
         a_rows = (uint32_t)x.call_rows;
     }
-    return GroupedSide{to, pc, n * pc, 0};
+    return GroupedSide{to, pc, 0};
 }
 GroupedSide side_of_w(int dtype, const void* w, uint64_t ld, uint64_t expert, uint32_t experts, uint64_t cols, uint64_t inner,
-                      Carver& c, LayRows& lay) {
-    if (readable(dtype, w, ld, inner) && expert % 8 == 0) return GroupedSide{w, ld, 0, expert};
+                      bool& wide, Carver& c, LayRows& lay) {
+    const bool aligned = whole(dtype, w, ld, inner) && expert * dtype_bytes(dtype) % 16 == 0;
+    if (readable(dtype, w, ld, inner) && (dtype == BC_F32 || aligned)) {
+        wide = wide && aligned;
+        return GroupedSide{w, ld, expert};
+    }
     const uint64_t pc = plane_cols(inner), n = experts * cols;
-    void* to = c.take(planes_bytes(dtype, n, inner));
+    void* to = c.take(laid_bytes(dtype, n, inner));
     lay = LayRows{w, nullptr, to, ld, expert, n, cols, (uint32_t)inner, 0};
-    return GroupedSide{to, pc, n * pc, cols * pc};
+    return GroupedSide{to, pc, cols * pc};
 }
 
 // ------------------------------------------------------ norm and clipping
@@ -303,7 +313,7 @@ int bytecomp_grouped_linear_workspace_size(int dtype, uint64_t rows, uint64_t x_
                                            uint32_t experts, int backward, size_t* bytes) {
     if (!bytes) return BC_E_NULL;
     if (const int rc = check_grouped(dtype, rows, inner, cols, experts, x_rows)) return rc;
-    *bytes = grouped_ws(dtype, rows, x_rows, inner, cols, experts, backward != 0);
+    *bytes = grouped_ws(dtype, rows, inner, cols, experts, backward != 0);
     return BC_OK;
 }
 
@@ -318,15 +328,14 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
     if (rows == 0 || cols == 0) return BC_OK;
     if (!offsets || !y || (inner > 0 && ((!x && (!source || x_rows > 0)) || !w))) return BC_E_NULL;
     if (ldx < inner || ldw < inner || expert_w < (cols - 1) * ldw + inner || (bias && ld_bias < cols) || ldy < cols ||
-        (z && ldz < cols))
+        (z && ldz < cols) || ldx >= kMaxStride || ldw >= kMaxStride)
         return BC_E_SIZE;
     if (misaligned(x, dtype) || misaligned(w, dtype) || misaligned(bias, dtype) || misaligned(y, dtype) ||
         misaligned(z, dtype) || misaligned4(offsets) || misaligned4(source) || ((uintptr_t)ws & 15))
         return BC_E_ALIGN;
     hipStream_t s = (hipStream_t)stream;
     const Groups g{offsets, experts, (uint32_t)rows};
-    const bool lies = readable(dtype, x, ldx, inner) && (!source || x_rows * ldx * 2 <= kGatherBytes) &&
-                      readable(dtype, w, ldw, inner) && expert_w % 8 == 0;
+    const bool lies = readable(dtype, x, ldx, inner) && readable(dtype, w, ldw, inner) && (dtype == BC_F32 || expert_w % 8 == 0);
     if (rows <= grouped_few_rows(dtype, experts, !lies)) {
         const GroupedFew a{g, x, w, bias, source, y, z, ldx, ldw, expert_w, ld_bias, ldy, ldz,
                            (uint32_t)(source ? x_rows : rows), (uint32_t)inner, (uint32_t)cols, act};
@@ -338,8 +347,9 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
     pre.g = g;
     GroupedProduct p{};
     p.g = g;
-    p.a = side_of_x(dtype, gx, p.a_rows, c, pre.lay[0]);
-    p.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, pre.lay[1]);
+    p.wide = true;
+    p.a = side_of_x(dtype, gx, p.a_rows, p.wide, c, pre.lay[0]);
+    p.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, p.wide, c, pre.lay[1]);
     if (c.used > 0 && (!ws || ws_bytes < c.used)) return BC_E_WORKSPACE;
     p.source = gx.source;
     p.cols = (uint32_t)cols;
@@ -377,7 +387,7 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
     if (lddy < cols || (act != BC_ACT_NONE && ldz < cols) || (dw && (ldx < inner || lddw < inner ||
                                                                     expert_dw < (cols - 1) * lddw + inner)) ||
         (dx && (ldw < inner || lddx < inner || (cols > 0 && expert_w < (cols - 1) * ldw + inner))) ||
-        (dbias && ld_dbias < cols))
+        (dbias && ld_dbias < cols) || lddy >= kMaxStride || (dw && ldx >= kMaxStride) || (dx && ldw >= kMaxStride))
         return BC_E_SIZE;
     if (misaligned(dy, dtype) || misaligned(z, dtype) || misaligned(x, dtype) || misaligned(w, dtype) ||
         misaligned(dx, dtype) || misaligned(dw, gdtype) || misaligned(dbias, gdtype) || misaligned4(offsets) ||
@@ -393,19 +403,21 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
     pre.g = g;
     GroupedSlope& slope = pre.slope;
     slope = GroupedSlope{dy, act != BC_ACT_NONE ? z : nullptr, nullptr, nullptr, lddy, ldz, (uint32_t)cols, act};
-    if (!same && (dx || dw)) slope.dz = c.take(planes_bytes(dtype, rows, cols));
+    if (!same && (dx || dw)) slope.dz = c.take(laid_bytes(dtype, rows, cols));
     if (dbias) slope.part = (float*)c.take(part_bytes(rows, experts, cols));
-    const GroupedSide dz = slope.dz ? GroupedSide{slope.dz, pc, rows * pc, 0} : GroupedSide{dy, lddy, 0, 0};
+    const GroupedSide dz = slope.dz ? GroupedSide{slope.dz, pc, 0} : GroupedSide{dy, lddy, 0};
     GroupedProduct px{}, pw{};
     px.g = pw.g = g;
     px.a = pw.a = dz;
+    px.wide = pw.wide = slope.dz || whole(dtype, dy, lddy, cols);
     px.a_rows = (uint32_t)rows;
     if (dw) {
         GroupedX gx{x, ldx, source, x_rows, rows, inner};
         uint32_t n = 0;
-        pw.b = side_of_x(dtype, gx, n, c, pre.lay[0]);
+        pw.b = side_of_x(dtype, gx, n, pw.wide, c, pre.lay[0]);
         if (gx.source) {
-            pre.where = GroupedWhere{gx.source, (uint32_t*)c.take(where_bytes(rows, experts)), n, (uint32_t)pw.b.ld};
+            pre.where = GroupedWhere{gx.source, (uint32_t*)c.take(where_bytes(rows, experts)), n,
+                                     (uint32_t)(pw.b.ld * dtype_bytes(dtype))};
             pw.where = pre.where.where;
         }
         pw.rows = (uint32_t)cols;
@@ -416,7 +428,7 @@ int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint6
         pw.nt = streams(experts * cols * inner * dtype_bytes(gdtype));
     }
     if (dx) {
-        px.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, c, pre.lay[1]);
+        px.b = side_of_w(dtype, w, ldw, expert_w, experts, cols, inner, px.wide, c, pre.lay[1]);
         px.cols = (uint32_t)inner;
         px.k = (uint32_t)cols;
         px.out = dx;

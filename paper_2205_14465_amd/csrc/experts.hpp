@@ -74,10 +74,10 @@ struct Groups {
 // tile's expert is found by comparisons alone; there are at most so many:
 __host__ __device__ inline uint32_t group_tiles(uint32_t rows, uint32_t experts, uint32_t high) { return rows / high + experts; }
 
-// A matrix for every expert, or one for all, as planes of 16-bit elements.
+// A matrix for every expert, or one for all.
 struct GroupedSide {
     const void* p;
-    uint64_t ld, plane, expert;   // elements from row to row, plane to plane, expert to expert
+    uint64_t ld, expert;     // elements from row to row, expert to expert
 };
 enum GroupedKind { kGroupedForward, kGroupedRows, kGroupedWeights };
 struct GroupedProduct {
@@ -94,6 +94,7 @@ struct GroupedProduct {
     uint64_t ld_bias, ld_z;
     int act;
     bool nt;
+    bool wide;               // both operands' rows are whole 16-byte pieces (16-bit ones: always)
 };
 hipError_t launch_grouped(int kind, int dtype, int out_dtype, const GroupedProduct& p, hipStream_t s);
 // dbias [experts][cols], rows ld apart, from the sums over 64 rows each of
@@ -112,14 +113,14 @@ constexpr uint32_t kGroupedCounters = 8;
 hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& rows, const GroupedProduct& weights,
                                const GroupedBias& bias, uint32_t* counters, hipStream_t s);
 
-// The forward pass for few rows, which needs no workspace: up to 64 in all, more where w
-// would be laid out first (four to ten bytes an element moved for a product that reads
-// two or four).  us, this way and by tiles: fp32, 8 experts of 1600x1600, 128 rows 28 and
-// 59, 256 50 and 74, 512 83 and 78; 64 experts 128 rows 125 and 495, 1024 205 and 526;
-// fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows 32 and 36, 1024
-// 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
+// The forward pass for few rows, which needs no workspace: up to 64 in all; more in
+// fp32, whose tiles are bound by the matrix instructions wherever rows fill them badly,
+// and where 16-bit weights would be laid out first.  us, this way and by tiles: fp32, 8
+// experts of 1600x1600, 128 rows 28 and 38, 256 50 and 57, 512 83 and 60; 64 experts 128
+// rows 125 and 177, 1024 205 and 205; fp16, 64 experts of 768x768, 64 rows 15 and 13, of
+// 1001x515 256 rows 32 and 36, 1024 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
 inline uint64_t grouped_few_rows(int dtype, uint32_t experts, bool laid_out) {
-    return 64 + (!laid_out ? 0 : dtype == BC_F32 ? 32ull * experts : 8ull * experts);
+    return 64 + (dtype == BC_F32 ? 32ull * experts : laid_out ? 8ull * experts : 0);
 }
 struct GroupedFew {
     Groups g;
@@ -133,8 +134,8 @@ struct GroupedFew {
 hipError_t launch_grouped_few(int dtype, const GroupedFew& a, hipStream_t s);
 
 // What the products need first, in one launch; a part whose output is NULL is left out.
-// Rows laid out as planes [count][plane_cols(cols)]: row r is row r % group of
-// the matrix r / group, or row source[r] of the only one (zeros where there is none).
+// Rows laid out as [count][plane_cols(cols)]: row r is row r % group of the matrix
+// r / group, or row source[r] of the only one (zeros where there is none).
 struct LayRows {
     const void* in;
     const int32_t* source;
@@ -142,7 +143,7 @@ struct LayRows {
     uint64_t ld, matrix, count, group;
     uint32_t cols, in_rows;
 };
-// dz = dy act'(z) of the experts' rows as planes [rows][plane_cols(cols)], and its
+// dz = dy act'(z) of the experts' rows as [rows][plane_cols(cols)], and its
 // sums over every tile of 64 rows.
 struct GroupedSlope {
     const void *dy, *z;      // z NULL: dz = dy
@@ -152,12 +153,12 @@ struct GroupedSlope {
     uint32_t cols;
     int act;
 };
-// Byte offsets of the rows source[r] of a matrix of row stride ld (16-bit
-// elements), every expert's from a multiple of 64 on, kNowhere in between.
+// Byte offsets of the rows source[r] of a matrix, every expert's from a multiple of 64
+// on, kNowhere in between.
 struct GroupedWhere {
     const int32_t* source;
     uint32_t* where;         // [64 (group_tiles(rows, experts, 64) + 1)]
-    uint32_t x_rows, ld;
+    uint32_t x_rows, row_bytes;
 };
 struct Prepare {
     Groups g;

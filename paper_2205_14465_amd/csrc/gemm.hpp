@@ -74,8 +74,9 @@ struct GemmTile {
     static constexpr int P = P_, kBM = BM_, kBN = BN_, kBK = BK_, kWM = WM_, kWN = WN_, kStages = STAGES_;
     static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
     static constexpr int kFM = kBM / kWM / 32, kFN = kBN / kWN / 32;     // 32x32 blocks of a wave
-    static constexpr int kRow = kBK * 2;                                // bytes of a row in LDS
-    static constexpr int kChunks = kBK / 8;                             // 16-byte chunks of a row
+    static constexpr int kElem = sizeof(T);                             // bytes of an element
+    static constexpr int kRow = kBK * kElem;                            // bytes of a row in LDS
+    static constexpr int kChunks = kRow / 16;                           // 16-byte chunks of a row
     static constexpr int kRows = 64 / kChunks;                          // rows of one load instruction
     static constexpr int kLoadA = kBM / kRows / kWaves, kLoadB = kBN / kRows / kWaves;
     static constexpr int kLoads = P * (kLoadA + kLoadB);                // a step's loads of one wave
@@ -83,7 +84,7 @@ struct GemmTile {
     static constexpr int kEpiCols = kFN * 32, kEpiLd = kEpiCols + 4;     // a wave's strip of C in the epilogue
     static constexpr int kEpiBytes = kWaves * 32 * kEpiLd * 4;
     static constexpr int kLdsBytes = kStages * kStageBytes > kEpiBytes ? kStages * kStageBytes : kEpiBytes;
-    static_assert(kBK == 32 || kBK == 64, "swizzles");
+    static_assert(kRow == 64 || kRow == 128, "swizzles");
     static_assert(kLoadA * kRows * kWaves == kBM && kLoadB * kRows * kWaves == kBN, "loads cover the tile");
 
     f32x16 acc[kFM][kFN];
@@ -92,7 +93,7 @@ struct GemmTile {
     static constexpr bool kApart = P > 1 && kFM * kFN <= 4;
     static_assert(P < 3 || kApart, "bfloat16 planes hold infinities, which lesser products must not reach");
 
-    static __device__ __forceinline__ int swizzle(int row) { return kBK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
+    static __device__ __forceinline__ int swizzle(int row) { return kRow == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
     // Products of `steps` steps of kBK into acc, which is cleared.
     __device__ __forceinline__ void multiply(const Operand<T>& a, const Operand<T>& b, int steps, char* lds) {

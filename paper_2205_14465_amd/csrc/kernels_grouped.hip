@@ -7,9 +7,11 @@
 // for every tile that there can be; a tile finds its expert among the offsets by
 // comparisons (experts.hpp), and those without rows end at once.  No operand is
 // turned in memory: dx takes w and dw takes dz and x with k down their columns
-// (run_tile.hpp).  16-bit operands are read where they lie, x through `source` if
-// it is given; fp32 ones are laid out as three bfloat16 planes, as
-// kernels_linear.hip does it.
+// (run_tile.hpp).  Operands are read where they lie, x through `source` if it is
+// given, but for 16-bit ones whose rows are no whole 16-byte pieces, which are laid
+// out first.  fp32 ones are multiplied as fp32: three bfloat16 planes of every
+// expert's weight (kernels_linear.hip) would move more bytes than their products
+// take time, and few rows share each.
 #include "act.hpp"
 #include "experts.hpp"
 #include "few.hpp"
@@ -126,42 +128,43 @@ __device__ __forceinline__ void finish_row(const GroupedProduct& p, uint32_t e, 
 
 // How the operands of a product lie: forward k along the rows of both, for dx
 // down the columns of w, for dw down those of dz and x.
-template <bool forward>
-using RowsLie = Lie<false, !forward>;
-template <bool kTable>
-using WeightsLie = Lie<true, true, kTable>;
+template <bool forward, int kPiece>
+using RowsLie = Lie<false, !forward, false, kPiece>;
+template <bool kTable, int kPiece>
+using WeightsLie = Lie<true, true, kTable, kPiece>;
 
 // Takes up the tile with rows `run` and columns n0 on of the experts' rows times
 // their weight.
-template <bool forward, typename R>
+template <typename L, bool forward, typename R>
 __device__ __forceinline__ void begin_rows(R& g, const GroupedProduct& p, const Run& run, uint32_t n0, char* lds) {
     typedef typename R::T T;
     const bool gather = forward && p.source;
     const uint32_t m0 = run.from;
-    const Side<T> a{(const T*)p.a.p + (gather ? 0 : m0 * p.a.ld), p.a.plane, (uint32_t)p.a.ld, run.to - m0};
-    const Side<T> b{(const T*)p.b.p + run.expert * p.b.expert + (forward ? n0 * p.b.ld : n0), p.b.plane, (uint32_t)p.b.ld,
-                    p.cols - n0};
-    g.template begin<RowsLie<forward>>(a, b, p.k, nullptr, lds, [&](int r) -> uint32_t {
-        if (!gather) return (uint32_t)r * (uint32_t)p.a.ld * 2;
+    const uint32_t ld = (uint32_t)p.a.ld;
+    const Side<T> a{(const T*)p.a.p + (gather ? 0 : m0 * p.a.ld), ld, run.to - m0};
+    const Side<T> b{(const T*)p.b.p + run.expert * p.b.expert + (forward ? n0 * p.b.ld : n0), (uint32_t)p.b.ld, p.cols - n0};
+    g.template begin<L>(a, b, p.k, nullptr, lds, [&](int r) -> uint32_t {
+        if (!gather) return (uint32_t)r * ld * (uint32_t)sizeof(T);
         const uint32_t row = (uint32_t)p.source[m0 + r];
-        return row < p.a_rows ? row * (uint32_t)p.a.ld * 2 : kNowhere;
+        return row < p.a_rows ? row * ld * (uint32_t)sizeof(T) : kNowhere;
     });
 }
 
 // The same for rows m0 and columns n0 on of expert e's dw.
-template <bool kTable, typename R>
+template <typename L, typename R>
 __device__ __forceinline__ void begin_weights(R& g, const GroupedProduct& p, uint32_t e, uint32_t m0, uint32_t n0, char* lds) {
     typedef typename R::T T;
     const uint32_t first = offset_of(p.g, 0), from = offset_of(p.g, e), to = offset_of(p.g, e + 1);
-    const Side<T> a{(const T*)p.a.p + (uint64_t)from * p.a.ld + m0, p.a.plane, (uint32_t)p.a.ld, p.rows - m0};
-    const Side<T> b{(const T*)p.b.p + (kTable ? 0 : (uint64_t)from * p.b.ld) + n0, p.b.plane, (uint32_t)p.b.ld, p.cols - n0};
-    const uint32_t* where = kTable ? p.where + (uint64_t)tiles_before<64>(first, from, e) * 64 : nullptr;
+    const Side<T> a{(const T*)p.a.p + (uint64_t)from * p.a.ld + m0, (uint32_t)p.a.ld, p.rows - m0};
+    const Side<T> b{(const T*)p.b.p + (L::kTable ? 0 : (uint64_t)from * p.b.ld) + n0, (uint32_t)p.b.ld, p.cols - n0};
+    const uint32_t* where = L::kTable ? p.where + (uint64_t)tiles_before<64>(first, from, e) * 64 : nullptr;
     // (offsets that do not ascend: no rows)
-    g.template begin<WeightsLie<kTable>>(a, b, to > from && from >= first ? to - from : 0, where, lds, [](int) { return 0u; });
+    g.template begin<L>(a, b, to > from && from >= first ? to - from : 0, where, lds, [](int) { return 0u; });
 }
 
-template <typename G, typename TO, bool forward>
+template <typename G, typename TO, bool forward, int kPiece>
 __device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t block, char* lds) {
+    typedef RowsLie<forward, kPiece> L;
     const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN, tiles_m = tiles_in_all<G::kBM>(p.g);
     if (block >= tiles_m * tiles_n) return;
     // a die's tiles are consecutive ones, expert by expert
@@ -171,10 +174,10 @@ __device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t bloc
     uint32_t tn;
     if (!tile_run<G::kBM>(p.g, t, tiles_n, run, tn)) return;
     const uint32_t m0 = run.from, n0 = tn * G::kBN;
-    RunTile<G> g;
-    begin_rows<forward>(g, p, run, n0, lds);
-    g.template rest<RowsLie<forward>>(lds);
-    g.template run<RowsLie<forward>>(lds);
+    RunTile<G, kPiece> g;
+    begin_rows<L, forward>(g, p, run, n0, lds);
+    g.template rest<L>(lds);
+    g.template run<L>(lds);
     g.finish(lds, [&](int row, int col, float (&v)[8]) {
         const uint32_t m = m0 + row, n = n0 + col;
         if (m < run.to && n < p.cols) finish_row<TO, forward>(p, run.expert, m, n, v);
@@ -182,17 +185,18 @@ __device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t bloc
 }
 
 // dw: every expert's tiles, over its rows.
-template <typename G, typename TO, bool kTable>
+template <typename G, typename TO, bool kTable, int kPiece>
 __device__ __forceinline__ void weights_tile(const GroupedProduct& p, uint32_t block, char* lds) {
+    typedef WeightsLie<kTable, kPiece> L;
     const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     // an expert's tiles go to all dies, each a run of consecutive ones
     const uint32_t each = tiles_m * tiles_n, e = block / each, j = block - e * each;
     const uint32_t in = j % 8 * (each / 8) + (j % 8 < each % 8 ? j % 8 : each % 8) + j / 8;
     const uint32_t m0 = in / tiles_n * G::kBM, n0 = in % tiles_n * G::kBN;
-    RunTile<G> g;
-    begin_weights<kTable>(g, p, e, m0, n0, lds);
-    g.template rest<WeightsLie<kTable>>(lds);
-    g.template run<WeightsLie<kTable>>(lds);
+    RunTile<G, kPiece> g;
+    begin_weights<L>(g, p, e, m0, n0, lds);
+    g.template rest<L>(lds);
+    g.template run<L>(lds);
     g.finish(lds, [&](int row, int col, float (&v)[8]) {
         const uint32_t m = m0 + row, n = n0 + col;
         if (m < p.rows && n < p.cols)
@@ -200,16 +204,16 @@ __device__ __forceinline__ void weights_tile(const GroupedProduct& p, uint32_t b
     });
 }
 
-template <typename G, typename TO, bool forward>
+template <typename G, typename TO, bool forward, int kPiece>
 __global__ __launch_bounds__(G::kThreads) void rows_product(GroupedProduct p) {
     extern __shared__ char lds[];
-    rows_tile<G, TO, forward>(p, blockIdx.x, lds);
+    rows_tile<G, TO, forward, kPiece>(p, blockIdx.x, lds);
 }
 
-template <typename G, typename TO, bool kTable>
+template <typename G, typename TO, bool kTable, int kPiece>
 __global__ __launch_bounds__(G::kThreads) void weights_product(GroupedProduct p) {
     extern __shared__ char lds[];
-    weights_tile<G, TO, kTable>(p, blockIdx.x, lds);
+    weights_tile<G, TO, kTable, kPiece>(p, blockIdx.x, lds);
 }
 
 // dbias: 64 columns of an expert, whose sums over 64 rows each the first four waves
@@ -233,7 +237,7 @@ __device__ __forceinline__ void bias_columns(const GroupedBias& a, uint32_t bloc
 // Both gradients' products where tiles of this size do not fill the chip, and dbias:
 // `split` workgroups of the first product (dx's with rows_first: the one whose k is the
 // longer), those of the second up to `end`, then the bias's.
-template <typename G, typename TO, bool kTable>
+template <typename G, typename TO, bool kTable, int kPiece>
 __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, GroupedProduct pw, GroupedBias bias, uint32_t split,
                                                              uint32_t end, bool rows_first) {
     extern __shared__ char lds[];
@@ -243,8 +247,8 @@ __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, 
     }
     const bool first = blockIdx.x < split;
     const uint32_t block = first ? blockIdx.x : blockIdx.x - split;
-    if (first == rows_first) rows_tile<G, std::conditional_t<(G::P > 1), float, typename G::T>, false>(px, block, lds);
-    else weights_tile<G, TO, kTable>(pw, block, lds);
+    if (first == rows_first) rows_tile<G, typename G::T, false, kPiece>(px, block, lds);
+    else weights_tile<G, TO, kTable, kPiece>(pw, block, lds);
 }
 
 // ---------------------------------------------------------- large products
@@ -346,7 +350,7 @@ __device__ __forceinline__ void finish_large(R& g, char* lds, const E& epi) {
 
 template <typename G, typename TO, bool forward>
 __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
-    typedef RowsLie<forward> L;
+    typedef RowsLie<forward, 16> L;
     extern __shared__ char lds[];
     RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
     fill_runs<G::kBM>(p.g, table);
@@ -359,11 +363,11 @@ __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
     const uint32_t from = die * q + (die < rest ? die : rest), to = from + q + (die < rest ? 1 : 0);
     uint32_t t = from + blockIdx.x / 8;
     if (t >= to) return;
-    RunTile<G> g;
+    RunTile<G, 16> g;
     Run run;
     uint32_t tn;
     run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
-    begin_rows<forward>(g, p, run, tn * G::kBN, lds);
+    begin_rows<L, forward>(g, p, run, tn * G::kBN, lds);
     g.template rest<L>(lds);
     wait_first<G>();
     for (;;) {
@@ -374,7 +378,7 @@ __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
         const bool more = t < to;
         if (more) {
             run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
-            begin_rows<forward>(g, p, run, tn * G::kBN, lds);
+            begin_rows<L, forward>(g, p, run, tn * G::kBN, lds);
         }
         finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
             const uint32_t m = m0 + row, n = n0 + col;
@@ -387,7 +391,7 @@ __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
 
 template <typename G, typename TO, bool kTable>
 __global__ __launch_bounds__(G::kThreads) void weights_large(GroupedProduct p) {
-    typedef WeightsLie<kTable> L;
+    typedef WeightsLie<kTable, 16> L;
     extern __shared__ char lds[];
     const uint32_t tiles_m = (p.rows + G::kBM - 1) / G::kBM, tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     const uint32_t each = tiles_m * tiles_n, all = each * p.g.experts;
@@ -401,9 +405,9 @@ __global__ __launch_bounds__(G::kThreads) void weights_large(GroupedProduct p) {
     };
     uint32_t b = blockIdx.x, e, m0, n0;
     if (b >= all) return;
-    RunTile<G> g;
+    RunTile<G, 16> g;
     place(b, e, m0, n0);
-    begin_weights<kTable>(g, p, e, m0, n0, lds);
+    begin_weights<L>(g, p, e, m0, n0, lds);
     g.template rest<L>(lds);
     wait_first<G>();
     for (;;) {
@@ -413,7 +417,7 @@ __global__ __launch_bounds__(G::kThreads) void weights_large(GroupedProduct p) {
         const bool more = b < all;
         if (more) {
             place(b, e, m0, n0);
-            begin_weights<kTable>(g, p, e, m0, n0, lds);
+            begin_weights<L>(g, p, e, m0, n0, lds);
         }
         finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
             const uint32_t m = m1 + row, n = n1 + col;
@@ -431,8 +435,8 @@ __global__ __launch_bounds__(G::kThreads) void weights_large(GroupedProduct p) {
 // those of the experts with the most rows.
 template <typename G, typename TO, bool kTable>
 __global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, GroupedProduct pw, uint32_t* counters) {
-    typedef RowsLie<false> LX;
-    typedef WeightsLie<kTable> LW;
+    typedef RowsLie<false, 16> LX;
+    typedef WeightsLie<kTable, 16> LW;
     extern __shared__ char lds[];
     RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
     fill_runs<G::kBM>(px.g, table);
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, Gr
     const uint32_t wide = (pw.cols + G::kBN - 1) / G::kBN, each = (pw.rows + G::kBM - 1) / G::kBM * wide;
     const uint32_t all = each * pw.g.experts, weights_tiles = all / 8 + (die < all % 8 ? 1 : 0);
     const bool rows_first = px.k >= pw.g.rows / pw.g.experts;
-    RunTile<G> g;
+    RunTile<G, 16> g;
     Run run;
     uint32_t m0, n0;
     bool rows;
@@ -459,7 +463,7 @@ __global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, Gr
             run_in<G::kBM>(table, px.g.experts, from + i, tiles_n, run, tn);
             m0 = run.from;
             n0 = tn * G::kBN;
-            begin_rows<false>(g, px, run, n0, lds);
+            begin_rows<LX, false>(g, px, run, n0, lds);
             return true;
         }
         const uint32_t b = i * 8 + die;
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, Gr
         run.expert = __builtin_amdgcn_readfirstlane(table.order[nth]);
         m0 = in / wide * G::kBM;
         n0 = in % wide * G::kBN;
-        begin_weights<kTable>(g, pw, run.expert, m0, n0, lds);
+        begin_weights<LW>(g, pw, run.expert, m0, n0, lds);
         return true;
     };
     auto ask_rest = [&]() {
@@ -513,10 +517,12 @@ template <typename T> struct Tiles {
     typedef GemmTile<T, 1, 128, 128, 64, 2, 4, 2> Middle;
     typedef GemmTile<T, 1, 256, 256, 64, 2, 4, 2> Large;
 };
+// (fp32's matrix instructions take so long that a tile needs few bytes a step: the
+// middle ones are large enough)
 template <> struct Tiles<float> {
-    typedef GemmTile<bf16_t, 3, 64, 64, 32, 2, 2, 3> Small;
-    typedef GemmTile<bf16_t, 3, 128, 128, 32, 2, 4, 3> Middle;
-    typedef GemmTile<bf16_t, 3, 256, 128, 32, 4, 2, 2> Large;
+    typedef GemmTile<float, 1, 64, 64, 32, 2, 2, 2> Small;
+    typedef GemmTile<float, 1, 128, 128, 32, 2, 4, 2> Middle;
+    typedef Middle Large;
 };
 
 template <typename G>
@@ -543,9 +549,30 @@ hipError_t launch_tiles(const void* kernel, const GroupedProduct& p, uint64_t gr
     return hipLaunchKernel(kernel, dim3((uint32_t)grid), dim3(G::kThreads), args, G::kLdsBytes, s);
 }
 
+// The kernel for pieces of 4 bytes exists for fp32 alone.
+template <typename G, typename TO, bool forward>
+const void* rows_kernel(const GroupedProduct& p) {
+    if constexpr (G::kElem == 4)
+        if (!p.wide) return (const void*)rows_product<G, TO, forward, 4>;
+    return (const void*)rows_product<G, TO, forward, 16>;
+}
+template <typename G, typename TO>
+const void* weights_kernel(const GroupedProduct& p) {
+    if constexpr (G::kElem == 4)
+        if (!p.wide) return p.where ? (const void*)weights_product<G, TO, true, 4> : (const void*)weights_product<G, TO, false, 4>;
+    return p.where ? (const void*)weights_product<G, TO, true, 16> : (const void*)weights_product<G, TO, false, 16>;
+}
+template <typename G, typename TO>
+const void* grads_kernel(const GroupedProduct& x, const GroupedProduct& w) {
+    if constexpr (G::kElem == 4)
+        if (!x.wide || !w.wide)
+            return w.where ? (const void*)grads_product<G, TO, true, 4> : (const void*)grads_product<G, TO, false, 4>;
+    return w.where ? (const void*)grads_product<G, TO, true, 16> : (const void*)grads_product<G, TO, false, 16>;
+}
+
 template <typename G, typename TO>
 hipError_t launch_kind(int kind, const GroupedProduct& p, hipStream_t s) {
-    constexpr bool kLarge = G::P == 1 && G::kBM == 256;
+    constexpr bool kLarge = G::kBM == 256;
     const uint64_t across = (p.cols + G::kBN - 1) / G::kBN;
     const uint64_t tiles = across * (kind == kGroupedWeights ? (uint64_t)p.g.experts * ((p.rows + G::kBM - 1) / G::kBM)
                                                              : group_tiles(p.g.rows, p.g.experts, G::kBM));
@@ -555,19 +582,17 @@ hipError_t launch_kind(int kind, const GroupedProduct& p, hipStream_t s) {
             return launch_large<G>(p.where ? (const void*)weights_large<G, TO, true> : (const void*)weights_large<G, TO, false>, args,
                                    tiles, s);
         } else {
-            return launch_tiles<G>(p.where ? (const void*)weights_product<G, TO, true> : (const void*)weights_product<G, TO, false>,
-                                   p, tiles, s);
+            return launch_tiles<G>(weights_kernel<G, TO>(p), p, tiles, s);
         }
     }
-    if constexpr (std::is_same_v<TO, typename G::T> || G::P > 1) {
+    if constexpr (std::is_same_v<TO, typename G::T>) {
         const bool forward = kind == kGroupedForward;
         if constexpr (kLarge) {
             void* args[] = {(void*)&p};
             return launch_large<G>(forward ? (const void*)rows_large<G, TO, true> : (const void*)rows_large<G, TO, false>, args,
                                    tiles, s);
         } else {
-            return launch_tiles<G>(forward ? (const void*)rows_product<G, TO, true> : (const void*)rows_product<G, TO, false>, p,
-                                   tiles, s);
+            return launch_tiles<G>(forward ? rows_kernel<G, TO, true>(p) : rows_kernel<G, TO, false>(p), p, tiles, s);
         }
     }
     return hipErrorInvalidValue;
@@ -580,7 +605,7 @@ struct TileCost {
     double alone, full, ends;
 };
 constexpr TileCost kCost16[3] = {{64, 64, 0.30, 0.193, 0.5}, {128, 128, 0.60, 0.53, 2.0}, {256, 256, 1.05, 1.50, 11.0}};
-constexpr TileCost kCost32[3] = {{64, 64, 0.82, 0.95, 0.5}, {128, 128, 1.86, 2.56, 1.5}, {256, 128, 3.4, 4.68, 8.7}};
+constexpr TileCost kCost32[3] = {{64, 64, 1.0, 0.95, 1.0}, {128, 128, 3.6, 3.6, 2.0}, {128, 128, 1e9, 1e9, 0.0}};
 
 // A product in tiles of one size: rounds over the chip's 256 units, a tile's time alone
 // and on a full chip.
@@ -803,7 +828,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void grouped_few_tiles(GroupedFew a
 // ---------------------------------------------------- what products are given
 template <typename T>
 __device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint32_t blocks) {
-    typedef typename PlaneOf<T>::type E;
     const uint64_t ld = plane_cols(a.cols), across = ld / 8, step = (uint64_t)blocks * 256;
     for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < a.count * across; i += step) {
         const uint64_t r = i / across;
@@ -820,7 +844,7 @@ __device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint3
         }
         float v[8];
         load_vec((const T*)a.in + (there ? at + c : 0), there ? (int)(a.cols - c) : 0, v);
-        store_planes<T>((E*)a.out + r * ld + c, a.count * ld, v);
+        store_vec((T*)a.out + r * ld + c, 8, v);
     }
 }
 
@@ -829,7 +853,6 @@ __device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint3
 constexpr uint32_t kSlopeCols = 128;
 template <typename T>
 __device__ __forceinline__ void slope_tile(const Groups& g, const GroupedSlope& a, uint32_t block) {
-    typedef typename PlaneOf<T>::type E;
     constexpr int kPasses = 4;
     __shared__ float sums[4][kSlopeCols];
     Run run;
@@ -864,7 +887,7 @@ __device__ __forceinline__ void slope_tile(const Groups& g, const GroupedSlope& 
                 if (a.z) d[j] = j < left[i] ? d[j] * act_slope<sizeof(T) == 4>(a.act, (float)z[i].v[j]) : 0.0f;
                 sum[j] += d[j];
             }
-            if (a.dz && r < run.to && c < ld) store_planes<T>((E*)a.dz + r * ld + c, (uint64_t)g.rows * ld, d);
+            if (a.dz && r < run.to && c < ld) store_vec((T*)a.dz + r * ld + c, 8, d);
         }
     }
     if (!a.part) return;
@@ -889,7 +912,7 @@ __device__ __forceinline__ void where_rows(const Groups& g, const GroupedWhere& 
     uint32_t at = kNowhere;
     if (run_of<64>(g, i / 64, run) && run.from + i % 64 < run.to) {
         const uint32_t row = (uint32_t)a.source[run.from + i % 64];
-        if (row < a.x_rows) at = row * a.ld * 2;
+        if (row < a.x_rows) at = row * a.row_bytes;
     }
     if (i < 64 * (group_tiles(g.rows, g.experts, 64) + 1)) a.where[i] = at;
 }
@@ -929,7 +952,7 @@ template <typename G, typename TO>
 static hipError_t pair_of(GroupedProduct x, GroupedProduct w, GroupedBias bias, uint32_t* counters, hipStream_t s) {
     const uint64_t tiles_x = group_tiles(x.g.rows, x.g.experts, G::kBM) * ((uint64_t)(x.cols + G::kBN - 1) / G::kBN);
     const uint64_t tiles_w = (uint64_t)w.g.experts * ((w.rows + G::kBM - 1) / G::kBM) * ((w.cols + G::kBN - 1) / G::kBN);
-    if constexpr (G::P == 1 && G::kBM == 256) {
+    if constexpr (G::kBM == 256) {
         if (bias.out) {
             const hipError_t e = launch_grouped_bias(sizeof(TO) == 4 ? (int)BC_F32 : __is_same(TO, f16_t) ? (int)BC_F16 : (int)BC_BF16, bias, s);
             if (e != hipSuccess) return e;
@@ -941,7 +964,7 @@ static hipError_t pair_of(GroupedProduct x, GroupedProduct w, GroupedBias bias, 
         bool rows_first = x.k >= w.g.rows / w.g.experts;
         uint32_t split = (uint32_t)(rows_first ? tiles_x : tiles_w), end = (uint32_t)(tiles_x + tiles_w);
         const uint64_t grid = end + (bias.out ? (uint64_t)bias.g.experts * ((bias.cols + 63) / 64) : 0);
-        const void* kernel = w.where ? (const void*)grads_product<G, TO, true> : (const void*)grads_product<G, TO, false>;
+        const void* kernel = grads_kernel<G, TO>(x, w);
         const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
         if (e != hipSuccess) return e;
         if (grid * G::kThreads >= (1ull << 32)) return hipErrorInvalidValue;

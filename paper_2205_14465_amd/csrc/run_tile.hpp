@@ -1,14 +1,16 @@
 // run_tile.hpp -- the tile of gemm.hpp for operands that lie either way: each of
 // the two has the contracted axis k along its rows, as there, or down its columns
-// (an operand that a product takes transposed).
+// (an operand that a product takes transposed); and for fp32 on the fp32 matrix
+// instruction (32x32x2), two elements of k at a time.
 //
 // An operand with k down its columns goes to LDS as it lies, a step's kBK rows of
-// it, and the transposing LDS read hands each lane four consecutive k of one
-// column: within 16 lanes, lane 4 j + q reads 8 bytes of row j, columns 4 q on, and
-// lane i receives column i of rows 0 to 3.  Rows are a multiple of 128 bytes apart,
-// so the 16-byte chunks of row r are swizzled by kTurn[r mod 4]: the four rows
-// of a read, and the next sixteen columns, then lie in eight different pieces of 32
-// bytes of 256.
+// it.  16-bit ones come back by the transposing LDS read, which hands each lane four
+// consecutive k of one column: within 16 lanes, lane 4 j + q reads 8 bytes of row j,
+// columns 4 q on, and lane i receives column i of rows 0 to 3.  Rows are a multiple
+// of 128 bytes apart, so the 16-byte chunks of row r are swizzled by kTurn[r mod 4]:
+// the four rows of a read, and the next sixteen columns, then lie in eight different
+// pieces of 32 bytes of 256.  fp32 ones are read word by word, 32 columns of a row
+// at a time.
 //
 // What is past an operand's end is loaded as zero: a lane's offset past the
 // buffer's size reads 0.
@@ -20,33 +22,61 @@ namespace bc {
 
 constexpr uint32_t kNowhere = 0x80000000u;   // a byte offset that reads zero
 
+// A fragment: 16 bytes of a row of k for each lane, those of the upper half of the
+// wave after those of the lower.
+template <typename T>
+struct RunFrag {
+    typedef typename Frag<T>::type type;
+    static constexpr int kProducts = 1;      // matrix instructions
+    static __device__ __forceinline__ f32x16 mma(type a, type b, f32x16 c) { return Frag<T>::mma(a, b, c); }
+};
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+template <>
+struct RunFrag<float> {
+    typedef f32x4v type;
+    static constexpr int kProducts = 4;
+    // (element i of both halves: two of the fragment's eight k, the same in both operands)
+    static __device__ __forceinline__ f32x16 mma(type a, type b, f32x16 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
 // One operand.  Rows (or columns) of the tile past `count` read zero.
 template <typename T>
 struct Side {
     const T* p;         // the tile's first row (column), first k
-    uint64_t plane;     // elements from plane to plane
     uint32_t ld;        // elements from row to row in memory, < 2^21
     uint32_t count;     // rows (columns) there are from the tile's first on
 };
 
-// How a product's operands lie: whether k runs down A's and B's columns, and
-// whether B's rows are wherever a table of byte offsets says.
-template <bool TA_, bool TB_, bool kTable_ = false>
+// How a product's operands lie: whether k runs down A's and B's columns, whether B's
+// rows are wherever a table of byte offsets says, and the bytes that a lane loads at a
+// time: 16, where every row is made of whole such pieces, or 4 (fp32 only).
+template <bool TA_, bool TB_, bool kTable_, int kPiece_>
 struct Lie {
     static constexpr bool TA = TA_, TB = TB_, kTable = kTable_;
+    static constexpr int kPiece = kPiece_;
 };
 
-template <typename B_>
+template <typename B_, int kPiece>
 struct RunTile : B_ {
     typedef B_ B;
     typedef typename B::T T;
-    using B::P; using B::kBM; using B::kBN; using B::kBK; using B::kWN; using B::kStages; using B::kWaves;
-    using B::kFM; using B::kFN; using B::kRow; using B::kChunks; using B::kRows; using B::kLoadA; using B::kLoadB;
-    using B::kLoads; using B::kStageBytes; using B::kApart; using B::acc;
-    typedef typename Frag<T>::type frag;
+    using B::kBM; using B::kBN; using B::kBK; using B::kWN; using B::kStages; using B::kWaves; using B::kElem;
+    using B::kFM; using B::kFN; using B::kRow; using B::kStageBytes; using B::acc;
+    typedef RunFrag<T> F;
+    typedef typename F::type frag;
     typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-    static_assert((kBM & (kBM - 1)) == 0 && (kBN & (kBN - 1)) == 0 && kBM <= 512 && kBN <= 512, "whole rows in a load");
+    static_assert(B::P == 1 && (kPiece == 16 || (kPiece == 4 && kElem == 4)), "pieces");
+    static_assert((kBM & (kBM - 1)) == 0 && (kBN & (kBN - 1)) == 0, "whole rows in a load");
+    // Load instructions of a wave and step.
+    static constexpr int kLoadA = kBM * kRow / (64 * kPiece) / kWaves, kLoadB = kBN * kRow / (64 * kPiece) / kWaves;
+    static constexpr int kLoads = kLoadA + kLoadB;
+    static_assert(kLoadA * kWaves * 64 * kPiece == kBM * kRow && kLoadB * kWaves * 64 * kPiece == kBN * kRow, "loads cover the tile");
+    static_assert((kStages - 1) * kLoads < 64, "the count of loads in flight has six bits");
 
     // What a lane loads of the tile at hand.
     Side<T> a, b;
@@ -54,22 +84,24 @@ struct RunTile : B_ {
     const uint32_t* where;
     uint32_t offa[kLoadA], offb[kLoadB], from_b[kLoadB];
 
-    // Chunks' swizzle of row r in LDS, for rows of `width` elements.
+    // Chunks' swizzle of row r in LDS, for rows of `width` elements of k down columns.
     template <int width>
     static __device__ __forceinline__ int turn(int r) {
-        return 2 * ((r & 3) | (width > 64 ? (r & 1) << 2 : 0));
+        return kElem == 4 ? 0 : 2 * ((r & 3) | (width > 64 ? (r & 1) << 2 : 0));
     }
-    // Row (or k) within the tile's step that load i of this wave brings to this
-    // lane, and the lane's chunk of it.
+    // Load i of this wave brings to LDS, from `index` x 64 pieces on, to this lane: row
+    // (or k within the step) `row`, elements `at` on of it.
+    template <bool down, int loads>
+    static __device__ __forceinline__ int index_of(int i, int wave) { return down ? wave * loads + i : i * kWaves + wave; }
+    struct Spot {
+        int row, at;
+    };
     template <bool down, int width, int loads>
-    static __device__ __forceinline__ int row_of(int i, int wave, int lane) {
-        if constexpr (down) return (wave * loads + i) * (512 / width) + lane / (width / 8);
-        else return (i * kWaves + wave) * kRows + lane / kChunks;
-    }
-    template <bool down, int width>
-    static __device__ __forceinline__ int chunk_of(int r, int lane) {
-        if constexpr (down) return lane % (width / 8) ^ turn<width>(r);
-        else return lane % kChunks ^ B::swizzle(r);
+    static __device__ __forceinline__ Spot spot_of(int i, int wave, int lane) {
+        constexpr int kLong = down ? width * kElem : kRow;
+        const int byte = (index_of<down, loads>(i, wave) * 64 + lane) * kPiece, row = byte / kLong, in = byte % kLong;
+        const int chunk = in / 16 ^ (down ? turn<width>(row) : B::swizzle(row));
+        return Spot{row, chunk * (16 / kElem) + in % 16 / kElem};
     }
     __device__ __forceinline__ int steps() const { return (int)((k + kBK - 1) / kBK); }
     static __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -88,22 +120,22 @@ struct RunTile : B_ {
         const int lane = threadIdx.x & 63, wave = wave_index();
 #pragma unroll
         for (int i = 0; i < kLoadA; ++i) {
-            const int r = row_of<L::TA, kBM, kLoadA>(i, wave, lane), c = chunk_of<L::TA, kBM>(r, lane);
+            const Spot s = spot_of<L::TA, kBM, kLoadA>(i, wave, lane);
             if constexpr (L::TA) {
-                offa[i] = (uint32_t)c * 8 < a.count ? (uint32_t)r * a.ld * 2 + c * 16 : kNowhere;
+                offa[i] = (uint32_t)s.at < a.count ? ((uint32_t)s.row * a.ld + s.at) * kElem : kNowhere;
             } else {
-                const uint32_t at = (uint32_t)r < a.count ? row_a(r) : kNowhere;
-                offa[i] = at == kNowhere ? kNowhere : at + c * 16;
+                const uint32_t at = (uint32_t)s.row < a.count ? row_a(s.row) : kNowhere;
+                offa[i] = at == kNowhere ? kNowhere : at + s.at * kElem;
             }
         }
 #pragma unroll
         for (int i = 0; i < kLoadB; ++i) {
-            const int r = row_of<L::TB, kBN, kLoadB>(i, wave, lane), c = chunk_of<L::TB, kBN>(r, lane);
+            const Spot s = spot_of<L::TB, kBN, kLoadB>(i, wave, lane);
             if constexpr (L::TB) {
-                offb[i] = (uint32_t)c * 8 < b.count ? (L::kTable ? 0 : (uint32_t)r * b.ld * 2) + c * 16 : kNowhere;
-                if (L::kTable && k > 0) from_b[i] = where[r];
+                offb[i] = (uint32_t)s.at < b.count ? ((L::kTable ? 0 : (uint32_t)s.row * b.ld) + s.at) * kElem : kNowhere;
+                if (L::kTable && k > 0) from_b[i] = where[s.row];
             } else {
-                offb[i] = (uint32_t)r < b.count ? (uint32_t)r * b.ld * 2 + c * 16 : kNowhere;
+                offb[i] = (uint32_t)s.row < b.count ? ((uint32_t)s.row * b.ld + s.at) * kElem : kNowhere;
             }
         }
         ask<L>(lds, 0, 1);
@@ -132,45 +164,24 @@ struct RunTile : B_ {
 #pragma unroll
         for (int m = 0; m < kFM; ++m) fa[m] = lds + place<L::TA, kBM>(wm * kFM + m, lane);
 #pragma unroll
-        for (int n = 0; n < kFN; ++n) fb[n] = lds + P * kBM * kRow + place<L::TB, kBN>(wn * kFN + n, lane);
-        frag va[2][P][kFM], vb[2][P][kFN];
+        for (int n = 0; n < kFN; ++n) fb[n] = lds + kBM * kRow + place<L::TB, kBN>(wn * kFN + n, lane);
+        frag va[2][kFM], vb[2][kFN];
         const int sw = B::swizzle(l31);
         auto read = [&](int set, int stage, int kk) {
             const int along = ((kk * 2 + hi) ^ sw) * 16;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
+            for (int n = 0; n < kFN; ++n) vb[set][n] = fetch<L::TB, kBN * kElem>(fb[n] + stage * kStageBytes, kk, along);
 #pragma unroll
-                for (int n = 0; n < kFN; ++n)
-                    vb[set][p][n] = fetch<L::TB, kBN * 2>(fb[n] + stage * kStageBytes + p * kBN * kRow, kk, along);
-#pragma unroll
-                for (int m = 0; m < kFM; ++m)
-                    va[set][p][m] = fetch<L::TA, kBM * 2>(fa[m] + stage * kStageBytes + p * kBM * kRow, kk, along);
-            }
+            for (int m = 0; m < kFM; ++m) va[set][m] = fetch<L::TA, kBM * kElem>(fa[m] + stage * kStageBytes, kk, along);
         };
-        f32x16 lesser[kApart ? kFM : 1][kApart ? kFN : 1];
-        if constexpr (kApart) {
+        auto mma = [&](int set) {
 #pragma unroll
             for (int m = 0; m < kFM; ++m)
 #pragma unroll
-                for (int n = 0; n < kFN; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) lesser[m][n][r] = 0.0f;
-        }
-        auto mma = [&](int set) {
-#pragma unroll
-            for (int pa = 0; pa < P; ++pa)
-#pragma unroll
-                for (int pb = 0; pb + pa < P; ++pb)
-#pragma unroll
-                    for (int m = 0; m < kFM; ++m)
-#pragma unroll
-                        for (int n = 0; n < kFN; ++n) {
-                            f32x16& to = kApart && pa + pb > 0 ? lesser[kApart ? m : 0][kApart ? n : 0] : acc[m][n];
-                            to = Frag<T>::mma(vb[set][pb][n], va[set][pa][m], to);
-                        }
+                for (int n = 0; n < kFN; ++n) acc[m][n] = F::mma(vb[set][n], va[set][m], acc[m][n]);
         };
-        constexpr int kKK = kBK / 16, kMma = P * (P + 1) / 2 * kFM * kFN;
-        constexpr int kReads = P * (kFM * (L::TA ? 2 : 1) + kFN * (L::TB ? 2 : 1)), kEachRead = (kReads + kMma - 1) / kMma;
+        constexpr int kKK = kRow / 32, kMma = F::kProducts * kFM * kFN, kDown = kElem == 4 ? 4 : 2;
+        constexpr int kReads = kFM * (L::TA ? kDown : 1) + kFN * (L::TB ? kDown : 1), kEachRead = (kReads + kMma - 1) / kMma;
         static_assert(kKK % 2 == 0, "fragment sets alternate");
         if (steps > 0) {
             if constexpr (!kLanded) {
@@ -224,17 +235,6 @@ struct RunTile : B_ {
             work(typename B::Yes{}, step++);
         }
         for (; step < steps; ++step) work(typename B::No{}, step);
-        if constexpr (kApart) {
-#pragma unroll
-            for (int m = 0; m < kFM; ++m)
-#pragma unroll
-                for (int n = 0; n < kFN; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float x = acc[m][n][r];
-                        acc[m][n][r] = P < 3 || fabsf(x) < INFINITY ? x + lesser[m][n][r] : x;
-                    }
-        }
         lds_barrier();  // every wave has read its last fragments: LDS is free
     }
 
@@ -279,61 +279,64 @@ struct RunTile : B_ {
         const uint32_t left = k - (uint32_t)(steps() - 1) * kBK;
 #pragma unroll
         for (int i = 0; i < kLoadA; ++i) {
-            const int r = row_of<L::TA, kBM, kLoadA>(i, wave, lane), c = chunk_of<L::TA, kBM>(r, lane);
-            if ((L::TA ? (uint32_t)r : (uint32_t)c * 8) >= left) offa[i] = kNowhere;
+            const Spot s = spot_of<L::TA, kBM, kLoadA>(i, wave, lane);
+            if ((uint32_t)(L::TA ? s.row : s.at) >= left) offa[i] = kNowhere;
         }
 #pragma unroll
         for (int i = 0; i < kLoadB; ++i) {
-            const int r = row_of<L::TB, kBN, kLoadB>(i, wave, lane), c = chunk_of<L::TB, kBN>(r, lane);
-            if ((L::TB ? (uint32_t)r : (uint32_t)c * 8) >= left) offb[i] = kNowhere;
+            const Spot s = spot_of<L::TB, kBN, kLoadB>(i, wave, lane);
+            if ((uint32_t)(L::TB ? s.row : s.at) >= left) offb[i] = kNowhere;
         }
     }
     template <typename L>
     __device__ __forceinline__ void load(char* lds, int stage, int step) {
         const int lane = threadIdx.x & 63, wave = wave_index();
         char* to = lds + stage * kStageBytes;
-        uint32_t next[kLoadB];
+        uint32_t at[kLoadB];
+#pragma unroll
+        for (int i = 0; i < kLoadB; ++i) at[i] = L::kTable ? either(from_b[i], offb[i]) : offb[i];
+        // the next step's rows, into the registers that have just been read and before this
+        // step's loads, so that they are there when those still are not
         if constexpr (L::kTable) {
-#pragma unroll
-            for (int i = 0; i < kLoadB; ++i) next[i] = where[(uint32_t)(step + 1) * kBK + row_of<L::TB, kBN, kLoadB>(i, wave, lane)];
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const __amdgpu_buffer_rsrc_t from = resource(a.p + p * a.plane + (L::TA ? (uint64_t)step * kBK * a.ld : 0));
-#pragma unroll
-            for (int i = 0; i < kLoadA; ++i)
-                B::copy16(from, offa[i], L::TA ? 0 : step * kRow,
-                          to + p * kBM * kRow + (L::TA ? wave * kLoadA + i : i * kWaves + wave) * 1024);
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const __amdgpu_buffer_rsrc_t from =
-                resource(b.p + p * b.plane + (L::TB && !L::kTable ? (uint64_t)step * kBK * b.ld : 0));
 #pragma unroll
             for (int i = 0; i < kLoadB; ++i)
-                B::copy16(from, L::kTable ? either(from_b[i], offb[i]) : offb[i], L::TB ? 0 : step * kRow,
-                          to + (P * kBM + p * kBN) * kRow + (L::TB ? wave * kLoadB + i : i * kWaves + wave) * 1024);
+                from_b[i] = where[(uint32_t)(step + 1) * kBK + spot_of<L::TB, kBN, kLoadB>(i, wave, lane).row];
         }
-        if constexpr (L::kTable) {
+        const __amdgpu_buffer_rsrc_t from_a = resource(a.p + (L::TA ? (uint64_t)step * kBK * a.ld : 0));
 #pragma unroll
-            for (int i = 0; i < kLoadB; ++i) from_b[i] = next[i];
-        }
+        for (int i = 0; i < kLoadA; ++i)
+            copy(from_a, offa[i], L::TA ? 0 : step * kRow, to + index_of<L::TA, kLoadA>(i, wave) * 64 * kPiece);
+        const __amdgpu_buffer_rsrc_t rows_b = resource(b.p + (L::TB && !L::kTable ? (uint64_t)step * kBK * b.ld : 0));
+#pragma unroll
+        for (int i = 0; i < kLoadB; ++i)
+            copy(rows_b, at[i], L::TB ? 0 : step * kRow, to + kBM * kRow + index_of<L::TB, kLoadB>(i, wave) * 64 * kPiece);
+    }
+    static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t from, uint32_t off, int step, char* to) {
+        auto* lds = (__attribute__((address_space(3))) void*)to;
+        if constexpr (kPiece == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, (int)off, step, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, (int)off, step, 0, 0);
     }
     static __device__ __forceinline__ uint32_t either(uint32_t row, uint32_t chunk) {
         return row == kNowhere || chunk == kNowhere ? kNowhere : row + chunk;
     }
+    // (p is the same in all lanes, which the compiler does not see everywhere: a load for
+    // each different pointer would be a loop)
     static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const T* p) {
-        return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000);
+        const uint64_t at = (uint64_t)p;
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = __builtin_amdgcn_readfirstlane((int)(at >> 32));
+        return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, 0x7fffffff, 0x00020000);
     }
     // Where a lane's fragments of block `block` (32 rows or columns) begin in a stage's operand.
     template <bool down, int width>
     static __device__ __forceinline__ int place(int block, int lane) {
-        if constexpr (down) {
+        if constexpr (!down) {
+            return (block * 32 + (lane & 31)) * kRow;
+        } else if constexpr (kElem == 4) {
+            return (lane >> 5) * 4 * width * 4 + (block * 32 + (lane & 31)) * 4;
+        } else {
             const int r = (lane >> 5) * 8 + ((lane & 15) >> 2);   // its k
             const int chunk = block * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
             return r * width * 2 + (chunk ^ turn<width>(r)) * 16 + (lane & 1) * 8;
-        } else {
-            return (block * 32 + (lane & 31)) * kRow;
         }
     }
     // The transposing read.  Its pointer is restrict, which says no more than that it
@@ -342,17 +345,22 @@ struct RunTile : B_ {
     static __device__ __forceinline__ s16x4 turned(const char* __restrict__ p) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
     }
-    // A fragment of 16 along k, from `at` of the lane's block; along: the swizzled
-    // chunk of an operand with k along its rows.
+    // Fragment kk of a step, from `at` of the lane's block; along: the swizzled chunk of an
+    // operand with k along its rows; row: bytes of one with k down its columns.
     template <bool down, int row>
     static __device__ __forceinline__ frag fetch(const char* at, int kk, int along) {
-        if constexpr (down) {
+        if constexpr (!down) {
+            return *(const frag*)(at + along);
+        } else if constexpr (kElem == 4) {
+            frag f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = *(const float*)(at + (kk * 8 + i) * row);
+            return f;
+        } else {
             const s16x4 v[2] = {turned(at + kk * 16 * row), turned(at + (kk * 16 + 4) * row)};
             frag f;
             __builtin_memcpy(&f, v, sizeof(f));
             return f;
-        } else {
-            return *(const frag*)(at + along);
         }
     }
 };

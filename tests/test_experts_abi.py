@@ -88,10 +88,12 @@ def test_grouped_linear_refusals():
     assert fwd(x=P(0x10001)) == -9 and fwd(off=ODD) == -9 and fwd(src=ODD, x_rows=5) == -9
     assert fwd(ws=P(0x40008), n=1 << 30) == -9
     assert fwd(rows=0) == 0 and fwd(cols=0) == 0
-    # many rows of fp32 and odd sizes are laid out first
-    need = B.bytecomp_grouped_linear_workspace_size(0, 700, 700, 64, 32, 3)
-    assert need > 0 and fwd(dtype=0, rows=700) == -7 and fwd(dtype=0, rows=700, ws=WS, n=need - 1) == -7
-    assert fwd(rows=700, inner=63) == -7 and fwd(rows=700, inner=60) == -7
+    assert fwd(ldx=1 << 21) == -5 and fwd(ldw=1 << 21, each=1 << 30) == -5
+    # many 16-bit rows of odd sizes are laid out first, fp32 ones that a gather's offsets do not reach
+    need = B.bytecomp_grouped_linear_workspace_size(1, 700, 700, 63, 32, 3)
+    assert need > 0 and fwd(rows=700, inner=63) == -7 and fwd(rows=700, inner=63, ws=WS, n=need - 257) == -7
+    assert fwd(rows=700, inner=60) == -7
+    assert fwd(dtype=0, rows=700, src=S, x_rows=1 << 30) == -7
     assert B.bytecomp_grouped_linear_workspace_size(0, 64, 64, 64, 32, 3) == 0
     assert B.bytecomp_grouped_linear_workspace_size(1, 64 + 8 * 3, 9, 63, 32, 3) == 0
 

@@ -384,6 +384,6 @@ def test_wrong_tensors_raise():
                 dict(src=off), dict(b=torch.zeros(3, 31, device="cuda")), dict(w=w.cpu()), dict(y=y.half())):
         with pytest.raises(ValueError):
             f(**bad)
-    with pytest.raises(B.BytecompError) as err:
-        f(ws=None)
+    with pytest.raises(B.BytecompError) as err:  # rows that are laid out first
+        f(x=x.half()[:, :60], w=w.half()[:, :, :60], y=y.half(), ws=None)
     assert err.value.code == -7
