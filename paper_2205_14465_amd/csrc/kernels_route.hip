@@ -26,6 +26,11 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Threads of a workgroup that chooses experts, G lanes a row: 64 rows at a time where
+// that is at most 1024.
+template <int G>
+constexpr int kGate = G <= 16 ? 64 * G : 1024;
+
 // Order of logits as unsigned numbers: -inf 0, then ascending; zeros are equal, a
 // NaN is the largest.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -52,84 +57,102 @@ __device__ __forceinline__ float group_sum(float x) {
     for (int o = G / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
     return x;
 }
+// The logit of an order, but for a NaN's payload.
+__device__ __forceinline__ float of_order(uint32_t o) {
+    if (o == 0xffffffffu) return NAN;
+    o += 0x007fffffu;
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+
+// The largest x of G lanes, in all of them.  Within 16 lanes by the moves that cost no
+// trip through LDS: neighbours, pairs, then halves and rows mirrored.
 template <int G>
-__device__ __forceinline__ uint64_t group_max(uint64_t x) {
-#pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) {
-        const uint64_t y = __shfl_xor(x, o, 64);
-        x = x > y ? x : y;
-    }
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+    auto with = [&](uint32_t y) { x = x > y ? x : y; };
+    with(__builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));                      // lane ^ 1
+    with(__builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));                      // lane ^ 2
+    with(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));                     // 7 - lane
+    if constexpr (G > 8) with(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));  // 15 - lane
+    if constexpr (G > 16) with(__shfl_xor(x, 16, 64));
+    if constexpr (G > 32) with(__shfl_xor(x, 32, 64));
     return x;
 }
 
 // exp(x - top), 0 for a logit that is masked out (also where all of them are).
 __device__ __forceinline__ float chance(float x, float top) { return x == -INFINITY ? 0.0f : expf(x - top); }
 
-// Writes a block's choices: weight and expert of its rows, their ranks (slot),
-// and, in LDS, the mask of the rows of each expert.
+// Writes a block's choices: weight and expert of its rows, and, in LDS, the mask of the
+// rows of each expert.  A choice is the largest order over a row's lanes, of equals that
+// of the first lane (lanes hold consecutive experts): each lane keeps its own largest at
+// hand and looks for the next when it has lost it.
 template <typename T, int G, int V>
 __device__ __forceinline__ void gate_rows(const Route& a, uint64_t row0, uint32_t rows, uint32_t words, uint32_t* mask) {
-    constexpr uint32_t kRows = kThreads / G;
-    const uint32_t lane = threadIdx.x % G;
+    constexpr uint32_t kRows = kGate<G> / G;
+    constexpr int kMine = (kMaxChoices + G - 1) / G;   // choices that a lane keeps
+    const uint32_t lane = threadIdx.x % G, first = (threadIdx.x & 63) / G * G;
     for (uint32_t r0 = 0; r0 < rows; r0 += kRows) {
         const uint32_t r = r0 + threadIdx.x / G;
         const bool there = r < rows;
         const uint64_t row = row0 + (there ? r : 0);
         float x[V];
         load_logits<T, V>((const T*)a.logits + row * a.ld, a.experts, lane, there, x);
-        uint32_t left = (1u << V) - 1;  // not chosen yet
-        float top = 0.0f, chosen = 0.0f, all = 1.0f, mine = 0.0f;
-        int32_t e_mine = -1;
-        for (uint32_t j = 0; j < a.k; ++j) {
-            uint64_t best = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const uint32_t o = order_of(x[i]);
-                const uint64_t key = (uint64_t)o << 32 | (0xffffffffu - (lane * V + i));
-                if ((left >> i & 1) && o != 0 && key > best) best = key;
-            }
-            best = group_max<G>(best);
-            const uint32_t e = 0xffffffffu - (uint32_t)best;
-            const bool found = best != 0;
-            // the chosen logit, from the lane that holds it
-            float value = 0.0f;
+        uint32_t o[V], best = 0, at = 0;
+        auto look = [&]() {
+            best = 0;
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (found && e == lane * V + i) {
-                    value = x[i];
-                    left &= ~(1u << i);
+                if (o[i] > best) {
+                    best = o[i];
+                    at = i;
                 }
-            value = __shfl(value, (int)((threadIdx.x & 63) / G * G + (found ? e / V : 0)), 64);
-            if (j == 0) {
-                top = value;
-                float sum = 0.0f;
+        };
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum += chance(x[i], top);
-                all = group_sum<G>(sum);
-            }
-            const float p = found ? expf(value - top) : 0.0f;
-            chosen += p;
-            if (lane == j % G) {
-                mine = p;
-                e_mine = found ? (int32_t)e : -1;
-            }
-            if (j % G == G - 1 || j + 1 == a.k) {
-                // G choices, one a lane (a lane's weight is divided when the sum is known)
-                const uint32_t at = j - j % G + lane;
-                if (there && at <= j) {
-                    a.weight[row * a.k + at] = mine;
-                    a.expert[row * a.k + at] = e_mine;
-                    if (e_mine >= 0) atomicOr(&mask[(uint32_t)e_mine * words + r / 32], 1u << (r % 32));
+        for (int i = 0; i < V; ++i) o[i] = order_of(x[i]);
+        look();
+        float top = 0.0f, chosen = 0.0f, all = 1.0f, mine[kMine];
+        int32_t e_mine[kMine];
+#pragma unroll
+        for (int s = 0; s < kMine; ++s) {
+            mine[s] = 0.0f;
+            e_mine[s] = -1;
+            for (uint32_t jj = 0; jj < G && s * G + jj < a.k; ++jj) {
+                const uint32_t most = group_max<G>(best);
+                const bool found = most != 0;
+                const uint64_t equal = __ballot(found && best == most) >> first & (G == 64 ? ~0ull : (1ull << (G & 63)) - 1);
+                const uint32_t owner = found ? (uint32_t)__builtin_ctzll(equal) : 0;
+                const uint32_t e = owner * V + (uint32_t)__shfl((int)at, (int)(first + owner), 64);
+                const float value = of_order(most);
+                if (s == 0 && jj == 0) {
+                    top = found ? value : 0.0f;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum += chance(x[i], top);
+                    all = group_sum<G>(sum);
+                }
+                const float p = found ? expf(value - top) : 0.0f;
+                chosen += p;
+                if (lane == jj) {
+                    mine[s] = p;
+                    e_mine[s] = found ? (int32_t)e : -1;
+                }
+                if (found && lane == owner) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (i == (int)at) o[i] = 0;
+                    look();
                 }
             }
         }
         // a row without a chosen expert has weights of 0 and nothing to divide by
         const float by = a.normalise ? chosen : all;
-        if (there)
-            for (uint32_t j = lane; j < a.k; j += G) {
-                const float p = a.weight[row * a.k + j];
-                a.weight[row * a.k + j] = by == 0.0f ? 0.0f : p / by;
-            }
+#pragma unroll
+        for (int s = 0; s < kMine; ++s) {
+            const uint32_t j = s * G + lane;
+            if (!there || j >= a.k) continue;
+            a.weight[row * a.k + j] = e_mine[s] < 0 ? 0.0f : mine[s] / by;
+            a.expert[row * a.k + j] = e_mine[s];
+            if (e_mine[s] >= 0) atomicOr(&mask[(uint32_t)e_mine[s] * words + r / 32], 1u << (r % 32));
+        }
     }
 }
 
@@ -141,7 +164,8 @@ __device__ __forceinline__ uint32_t rank_of(const uint32_t* mask, uint32_t r) {
 }
 
 template <typename T, int G, int V>
-__global__ __launch_bounds__(kThreads) void route_gate(Route a) {
+__global__ __launch_bounds__(kGate<G>) void route_gate(Route a) {
+    constexpr uint32_t kThreads = kGate<G>;
     extern __shared__ uint32_t mask[];
     const uint64_t row0 = (uint64_t)blockIdx.x * a.block_rows;
     const uint32_t rows = a.rows - row0 < a.block_rows ? (uint32_t)(a.rows - row0) : a.block_rows;
@@ -162,6 +186,7 @@ __global__ __launch_bounds__(kThreads) void route_gate(Route a) {
 }
 
 // Exclusive sums of x over a workgroup; *total: the sum.
+template <uint32_t kThreads>
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* total) {
     __shared__ uint32_t sh[kThreads / 64];
     const uint32_t lane = threadIdx.x & 63;
@@ -191,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void route_scan(Route a) {
     for (uint32_t b0 = 0; b0 < a.blocks; b0 += kThreads) {
         const uint32_t b = b0 + threadIdx.x;
         uint32_t total;
-        const uint32_t before = block_scan(b < a.blocks ? c[b] : 0, &total);
+        const uint32_t before = block_scan<kThreads>(b < a.blocks ? c[b] : 0, &total);
         if (b < a.blocks) c[b] = sum + before;
         sum += total;
     }
@@ -199,13 +224,13 @@ __global__ __launch_bounds__(kThreads) void route_scan(Route a) {
 }
 
 // Offsets of the experts from their totals, into LDS.
-template <typename F>
+template <uint32_t kThreads, typename F>
 __device__ __forceinline__ void offsets_of(uint32_t experts, uint32_t* offsets, F total_of) {
     uint32_t sum = 0;
     for (uint32_t e0 = 0; e0 < experts; e0 += kThreads) {
         const uint32_t e = e0 + threadIdx.x;
         uint32_t total;
-        const uint32_t before = block_scan(e < experts ? total_of(e) : 0, &total);
+        const uint32_t before = block_scan<kThreads>(e < experts ? total_of(e) : 0, &total);
         if (e < experts) offsets[e] = sum + before;
         sum += total;
     }
@@ -217,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void route_place(Route a) {
     __shared__ uint32_t offsets[kMaxExperts + 1];
     const uint64_t row0 = (uint64_t)blockIdx.x * a.block_rows;
     const uint32_t rows = a.rows - row0 < a.block_rows ? (uint32_t)(a.rows - row0) : a.block_rows;
-    offsets_of(a.experts, offsets, [&](uint32_t e) { return a.count[(uint64_t)a.experts * a.blocks + e]; });
+    offsets_of<kThreads>(a.experts, offsets, [&](uint32_t e) { return a.count[(uint64_t)a.experts * a.blocks + e]; });
     if (blockIdx.x == 0)
         for (uint32_t e = threadIdx.x; e <= a.experts; e += kThreads) a.offsets[e] = (int32_t)offsets[e];
     for (uint32_t i = threadIdx.x; i < rows * a.k; i += kThreads) {
@@ -232,7 +257,8 @@ __global__ __launch_bounds__(kThreads) void route_place(Route a) {
 
 // All of it in one workgroup.
 template <typename T, int G, int V>
-__global__ __launch_bounds__(kThreads) void route_small(Route a) {
+__global__ __launch_bounds__(kGate<G>) void route_small(Route a) {
+    constexpr uint32_t kThreads = kGate<G>;
     extern __shared__ uint32_t mask[];
     __shared__ uint32_t offsets[kMaxExperts + 1];
     const uint32_t rows = (uint32_t)a.rows, words = a.block_rows / 32;
@@ -240,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void route_small(Route a) {
     __syncthreads();
     gate_rows<T, G, V>(a, 0, rows, words, mask);
     __syncthreads();
-    offsets_of(a.experts, offsets, [&](uint32_t e) {
+    offsets_of<kThreads>(a.experts, offsets, [&](uint32_t e) {
         uint32_t n = 0;
         for (uint32_t w = 0; w < words; ++w) n += __popc(mask[e * words + w]);
         return n;
@@ -359,38 +385,41 @@ __global__ __launch_bounds__(kThreads) void combine(Combine a, uint32_t lanes) {
         combine_row<T, kWhole>(a, row, threadIdx.x % lanes * 8, lanes * 8);
 }
 
-// dy[slot_j] = weight_j dout, dweight_j = <dout, y[slot_j]>: a wave a row, its
-// part of dout read once for each choice (from the caches after the first).
+// dy[slot_j] = weight_j dout, dweight_j = <dout, y[slot_j]>: `lanes` lanes of a wave a
+// row, its part of dout read once for each choice (from the caches after the first).
 template <typename T, bool kWhole>
-__global__ __launch_bounds__(kThreads) void combine_grad(CombineGrad a) {
-    const uint32_t lane = threadIdx.x & 63;
-    constexpr uint32_t kRows = kThreads / 64;
-    const uint64_t first = (uint64_t)blockIdx.x * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (uint64_t row = first; row < a.rows; row += (uint64_t)gridDim.x * kRows)
-    for (uint32_t j = 0; j < a.k; ++j) {
-        const uint32_t slot = (uint32_t)a.slot[row * a.k + j];
-        float dot = 0.0f;
-        if (slot < a.slots) {
-            const float w = a.weight ? a.weight[row * a.k + j] : 1.0f;
-            for (uint32_t c = lane * 8; c < a.cols; c += 64 * 8) {
-                const int left = (int)(a.cols - c);
-                float d[8], y[8];
-                load_vec<kWhole>((const T*)a.dout + row * a.ldd + c, left, d);
-                if (a.dweight) {
-                    load_vec<kWhole>((const T*)a.y + slot * a.ldy + c, left, y);
+__global__ __launch_bounds__(kThreads) void combine_grad(CombineGrad a, uint32_t lanes) {
+    const uint32_t lane = threadIdx.x % lanes;
+    const uint64_t step = (uint64_t)gridDim.x * kThreads / lanes;
+    const uint64_t first = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / lanes;
+    // (the lanes of a wave go round together: the sums need every one of them)
+    for (uint64_t r = first; r < a.rows + first % (64 / lanes); r += step) {
+        const bool there = r < a.rows;
+        for (uint32_t j = 0; j < a.k; ++j) {
+            const uint32_t slot = there ? (uint32_t)a.slot[r * a.k + j] : 0xffffffffu;
+            float dot = 0.0f;
+            if (slot < a.slots) {
+                const float w = a.weight ? a.weight[r * a.k + j] : 1.0f;
+                for (uint32_t c = lane * 8; c < a.cols; c += lanes * 8) {
+                    const int left = (int)(a.cols - c);
+                    float d[8], y[8];
+                    load_vec<kWhole>((const T*)a.dout + r * a.ldd + c, left, d);
+                    if (a.dweight) {
+                        load_vec<kWhole>((const T*)a.y + slot * a.ldy + c, left, y);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) dot = fmaf(d[i], y[i], dot);
-                }
-                if (a.dy) {
+                        for (int i = 0; i < 8; ++i) dot = fmaf(d[i], y[i], dot);
+                    }
+                    if (a.dy) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] *= w;
-                    store_vec((T*)a.dy + slot * a.lddy + c, left, d, a.nt);
+                        for (int i = 0; i < 8; ++i) d[i] *= w;
+                        store_vec((T*)a.dy + slot * a.lddy + c, left, d, a.nt);
+                    }
                 }
             }
-        }
-        if (a.dweight) {
-            dot = wave_sum(dot);
-            if (lane == 0) a.dweight[row * a.k + j] = dot;
+            if (a.dweight) {
+                for (uint32_t o = lanes / 2; o > 0; o >>= 1) dot += __shfl_xor(dot, (int)o, 64);
+                if (lane == 0 && there) a.dweight[r * a.k + j] = dot;
+            }
         }
     }
 }
@@ -418,10 +447,10 @@ hipError_t route_of(const Route& a, hipStream_t s) {
         constexpr int G = decltype(g)::value, V = decltype(v)::value;
         const size_t lds = (size_t)a.experts * (a.block_rows / 32) * 4;
         if (a.blocks == 1) {
-            hipLaunchKernelGGL((route_small<T, G, V>), dim3(1), dim3(kThreads), lds, s, a);
+            hipLaunchKernelGGL((route_small<T, G, V>), dim3(1), dim3(kGate<G>), lds, s, a);
             return hipGetLastError();
         }
-        hipLaunchKernelGGL((route_gate<T, G, V>), dim3(a.blocks), dim3(kThreads), lds, s, a);
+        hipLaunchKernelGGL((route_gate<T, G, V>), dim3(a.blocks), dim3(kGate<G>), lds, s, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(route_scan, dim3(a.experts), dim3(kThreads), 0, s, a);
@@ -452,9 +481,10 @@ hipError_t combine_of(const Combine& a, hipStream_t s) {
 
 template <typename T>
 hipError_t combine_grad_of(const CombineGrad& a, hipStream_t s) {
-    const uint64_t blocks = (a.rows + kThreads / 64 - 1) / (kThreads / 64);
-    if (a.cols % 8 == 0) hipLaunchKernelGGL((combine_grad<T, true>), dim3(capped(blocks)), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((combine_grad<T, false>), dim3(capped(blocks)), dim3(kThreads), 0, s, a);
+    const uint32_t lanes = std::min(64u, row_lanes(a.cols));
+    const uint64_t blocks = (a.rows * lanes + kThreads - 1) / kThreads;
+    if (a.cols % 8 == 0) hipLaunchKernelGGL((combine_grad<T, true>), dim3(capped(blocks)), dim3(kThreads), 0, s, a, lanes);
+    else hipLaunchKernelGGL((combine_grad<T, false>), dim3(capped(blocks)), dim3(kThreads), 0, s, a, lanes);
     return hipGetLastError();
 }
 
