@@ -182,7 +182,7 @@ struct ClipDesc {
     uint32_t dtype;
 };
 static_assert(sizeof(ClipDesc) == 64, "ClipDesc layout");
-constexpr uint32_t kClipChunk = 1024, kClipParts = 2048;
+constexpr uint32_t kClipChunk = 256, kClipParts = 2048;
 struct Clip {
     const ClipDesc* d;
     uint32_t T;

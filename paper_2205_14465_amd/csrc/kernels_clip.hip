@@ -6,9 +6,15 @@
 // launch the workgroups' in a fixed order.  The maximum is taken over the
 // magnitudes' bits, so that a NaN is the largest.
 //
-// Both passes are bound by memory.  A workgroup takes a run of consecutive chunks
-// and finds its first matrix by a search of the table with all its threads; the
-// second pass walks its run backwards and meets what the caches kept of the first.
+// Both passes are bound by memory (1.56e9 fp32 elements: 1015 us for the norm, 6.1
+// TB/s, and 2740 for the scaling to another place, 4.5, a copy's rate; in bfloat16
+// 524 and 1280; ResNet-50's 161 gradients of 25.6e6 elements: 26 and, with nothing
+// to scale, 3.4).  A workgroup takes a run of consecutive chunks and finds its
+// first matrix by a search of the table with all its threads; the second pass walks
+// its run backwards and meets what the caches kept of the first.  A thread has 128
+// bytes of loads in flight whatever the type (with 64 of the 16-bit types the norm
+// took 722 us in place of 524), and rows' ends are left to a loop of their own,
+// whose registers would cost a quarter of the waves in flight.
 #include "common.hpp"
 #include "experts.hpp"
 
@@ -19,7 +25,11 @@ namespace bc {
 
 namespace {
 
-constexpr int kThreads = 256, kEach = kClipChunk / kThreads;
+constexpr int kThreads = 256;
+static_assert(kClipChunk == kThreads, "a piece of a chunk for every thread");
+// Chunks whose loads are in flight at once: 128 bytes a thread.
+template <typename T>
+constexpr int kGroup = 16 / (int)sizeof(T);
 
 // The last matrix whose first chunk is c or before, empty ones (which share their
 // first chunk with the next) passed over.  All threads call it.
@@ -36,48 +46,72 @@ __device__ __forceinline__ uint32_t matrix_of_chunk(const ClipDesc* __restrict__
     return lo;
 }
 
-// fn(descriptor, chunk of its own) for chunks [from, to), in order or backwards.
+// fn(descriptor, first chunk of its own, chunks) for the chunks [from, to), matrix
+// by matrix, in order or backwards.
 template <bool kBack, typename F>
-__device__ __forceinline__ void for_chunks(const ClipDesc* __restrict__ d, uint32_t T, uint64_t from, uint64_t to, F fn) {
+__device__ __forceinline__ void for_matrices(const ClipDesc* __restrict__ d, uint32_t T, uint64_t from, uint64_t to, F fn) {
     if (from >= to) return;
     uint32_t t = matrix_of_chunk(d, T, kBack ? to - 1 : from);
-    for (uint64_t i = from; i < to; ++i) {
-        const uint64_t c = kBack ? to - 1 - (i - from) : i;
-        if constexpr (kBack) {
-            while (d[t].chunk0 > c) --t;
-        } else {
-            while (t + 1 < T && d[t + 1].chunk0 <= c) ++t;
+    if constexpr (kBack) {
+        while (true) {
+            const uint64_t first = max(from, d[t].chunk0);
+            if (first < to) fn(d[t], first - d[t].chunk0, to - first);
+            if (first <= from) break;
+            to = first;
+            --t;
         }
-        fn(d[t], c - d[t].chunk0);
+    } else {
+        while (true) {
+            const uint64_t end = t + 1 < T ? min(to, d[t + 1].chunk0) : to;
+            if (from < end) fn(d[t], from - d[t].chunk0, end - from);
+            if (end >= to) break;
+            from = end;
+            ++t;
+        }
     }
 }
 
 struct Piece {
     uint64_t in, out;       // element offsets
-    int left;               // elements of it, 0: none
+    uint32_t left;          // elements of it, 0: none
 };
-__device__ __forceinline__ Piece piece_of(const ClipDesc& d, uint64_t chunk, int i) {
-    const uint64_t p = chunk * kClipChunk + (uint32_t)i * kThreads + threadIdx.x;
+__device__ __forceinline__ Piece piece_of(const ClipDesc& d, uint64_t chunk) {
+    const uint64_t p = chunk * kClipChunk + threadIdx.x;
     if (p >= d.pieces) return Piece{0, 0, 0};
     if (d.row_pieces == 0) {
         const uint64_t at = p * 8;
-        return Piece{at, at, (int)(d.cols - at < 8 ? d.cols - at : 8)};
+        return Piece{at, at, (uint32_t)min(d.cols - at, (uint64_t)8)};
     }
-    const uint64_t row = p / d.row_pieces, at = (p - row * d.row_pieces) * 8;
-    return Piece{row * d.ld_in + at, row * d.ld_out + at, (int)(d.cols - at < 8 ? d.cols - at : 8)};
+    const uint64_t row = d.pieces >> 32 ? p / d.row_pieces : (uint32_t)p / d.row_pieces;
+    const uint64_t at = (p - row * d.row_pieces) * 8;
+    return Piece{row * d.ld_in + at, row * d.ld_out + at, (uint32_t)min(d.cols - at, (uint64_t)8)};
 }
 
+// The whole pieces of chunks [chunk, chunk + n), n no more than a group, all loads
+// in flight at once; zeros in place of others.
 template <typename T>
-__device__ __forceinline__ void fetch(const ClipDesc& d, uint64_t chunk, Raw<T, 8> (&v)[kEach], Piece (&p)[kEach]) {
+__device__ __forceinline__ void fetch(const ClipDesc& d, uint64_t chunk, uint32_t n, Raw<T, 8> (&v)[kGroup<T>]) {
+    if (d.row_pieces == 0 && n == kGroup<T> && (chunk + n) * kClipChunk * 8 <= d.cols) {
+        const T* at = (const T*)d.in + chunk * kClipChunk * 8;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) p[i] = piece_of(d, chunk, i);
-    // (whole pieces without a branch for parts, so that all loads are in flight at once)
-    if ((d.cols & 7) == 0 || (d.row_pieces == 0 && (chunk + 1) * kClipChunk * 8 <= d.cols)) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i].template load<true>((const T*)d.in + p[i].in, p[i].left);
+        for (int i = 0; i < kGroup<T>; ++i) v[i].template load<true>(at + ((uint32_t)i * kThreads + threadIdx.x) * 8, 8);
     } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i].load((const T*)d.in + p[i].in, p[i].left);
+        for (int i = 0; i < kGroup<T>; ++i) {
+            const Piece p = (uint32_t)i < n ? piece_of(d, chunk + i) : Piece{0, 0, 0};
+            v[i].template load<true>((const T*)d.in + p.in, p.left == 8);
+        }
+    }
+}
+
+// fn(piece) for the chunks' pieces of fewer than eight elements, the ends of rows.
+template <typename F>
+__device__ __forceinline__ void for_ends(const ClipDesc& d, uint64_t chunk, uint32_t n, F fn) {
+    if ((d.cols & 7) == 0 || (d.row_pieces == 0 && (chunk + n) * kClipChunk * 8 <= d.cols)) return;
+#pragma unroll 1
+    for (uint32_t i = 0; i < n; ++i) {
+        const Piece p = piece_of(d, chunk + i);
+        if (p.left > 0 && p.left < 8) fn(p);
     }
 }
 
@@ -109,9 +143,16 @@ __device__ __forceinline__ double block_reduce(double x, int kind) {
 __device__ __forceinline__ double norm_of(const Clip& a) {
     if (a.given) return *a.given;
     double x = 0.0;
-    for (uint32_t i = threadIdx.x; i < a.parts; i += kThreads)
-        x = a.kind == BC_NORM_MAX ? __longlong_as_double(max(__double_as_longlong(x), __double_as_longlong(a.part[i])))
-                                  : x + a.part[i];
+    double part[kClipParts / kThreads];  // (all loads at once)
+#pragma unroll
+    for (uint32_t i = 0; i < kClipParts / kThreads; ++i) {
+        const uint32_t at = threadIdx.x + i * kThreads;
+        part[i] = at < a.parts ? a.part[at] : 0.0;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kClipParts / kThreads; ++i)
+        x = a.kind == BC_NORM_MAX ? __longlong_as_double(max(__double_as_longlong(x), __double_as_longlong(part[i])))
+                                  : x + part[i];
     x = block_reduce(x, a.kind);
     return a.kind == BC_NORM_MAX ? x : sqrt(x);
 }
@@ -120,24 +161,35 @@ __global__ __launch_bounds__(kThreads) void clip_norm(Clip a) {
     const uint64_t from = a.chunks * blockIdx.x / gridDim.x, to = a.chunks * (blockIdx.x + 1) / gridDim.x;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     uint32_t most = 0;
-    for_chunks<false>(a.d, a.T, from, to, [&](const ClipDesc& d, uint64_t chunk) {
+    for_matrices<false>(a.d, a.T, from, to, [&](const ClipDesc& d, uint64_t chunk, uint64_t n) {
         with_type(d.dtype, [&](auto of) {
-            Raw<decltype(of), 8> v[kEach];
-            Piece p[kEach];
-            fetch(d, chunk, v, p);
-            if (a.kind == BC_NORM_MAX) {
+            typedef decltype(of) E;
+            for (uint64_t at = 0; at < n; at += kGroup<E>) {
+                const uint32_t m = (uint32_t)min(n - at, (uint64_t)kGroup<E>);
+                Raw<E, 8> v[kGroup<E>];
+                fetch(d, chunk + at, m, v);
+                if (a.kind == BC_NORM_MAX) {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i)
+                    for (int i = 0; i < kGroup<E>; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint((float)v[i].v[j]) & 0x7fffffffu);
-            } else {
+                        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint((float)v[i].v[j]) & 0x7fffffffu);
+                } else {
 #pragma unroll
-                for (int i = 0; i < kEach; ++i)
+                    for (int i = 0; i < kGroup<E>; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const double x = (double)(float)v[i].v[j];
-                        sum[j & 3] = fma(x, x, sum[j & 3]);
+                        for (int j = 0; j < 8; ++j) {
+                            const double x = (double)(float)v[i].v[j];
+                            sum[j & 3] = fma(x, x, sum[j & 3]);
+                        }
+                }
+                for_ends(d, chunk + at, m, [&](const Piece& p) {
+#pragma unroll 1
+                    for (uint32_t j = 0; j < p.left; ++j) {
+                        const float x = (float)((const E*)d.in)[p.in + j];
+                        if (a.kind == BC_NORM_MAX) most = max(most, __float_as_uint(x) & 0x7fffffffu);
+                        else sum[0] = fma((double)x, (double)x, sum[0]);
                     }
+                });
             }
         });
     });
@@ -160,19 +212,29 @@ __global__ __launch_bounds__(kThreads) void clip_scale(Clip a) {
         if (a.factor) *a.factor = c;
     }
     const uint64_t from = a.chunks * blockIdx.x / gridDim.x, to = a.chunks * (blockIdx.x + 1) / gridDim.x;
-    for_chunks<true>(a.d, a.T, from, to, [&](const ClipDesc& d, uint64_t chunk) {
+    for_matrices<true>(a.d, a.T, from, to, [&](const ClipDesc& d, uint64_t chunk, uint64_t n) {
         if (c == 1.0f && d.in == d.out) return;
         with_type(d.dtype, [&](auto of) {
             typedef decltype(of) E;
-            Raw<E, 8> v[kEach];
-            Piece p[kEach];
-            fetch(d, chunk, v, p);
+            for (uint64_t end = n; end > 0;) {
+                const uint32_t m = (uint32_t)min(end, (uint64_t)kGroup<E>);
+                end -= m;
+                Raw<E, 8> v[kGroup<E>];
+                fetch(d, chunk + end, m, v);
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                float f[8];
+                for (int i = 0; i < kGroup<E>; ++i) {
+                    const Piece p = (uint32_t)i < m ? piece_of(d, chunk + end + i) : Piece{0, 0, 0};
+                    if (p.left != 8) continue;
+                    float f[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = c * (float)v[i].v[j];
-                store_vec((E*)d.out + p[i].out, p[i].left, f, a.nt);
+                    for (int j = 0; j < 8; ++j) f[j] = c * (float)v[i].v[j];
+                    store_vec((E*)d.out + p.out, 8, f, a.nt);
+                }
+                for_ends(d, chunk + end, m, [&](const Piece& p) {
+#pragma unroll 1
+                    for (uint32_t j = 0; j < p.left; ++j)
+                        ((E*)d.out)[p.out + j] = (E)(c * (float)((const E*)d.in)[p.in + j]);
+                });
             }
         });
     });
@@ -189,7 +251,10 @@ __global__ __launch_bounds__(kThreads) void write_table(uint32_t* to, TableWords
 
 }  // namespace
 
-uint32_t clip_parts(uint64_t chunks) { return (uint32_t)std::min<uint64_t>(chunks, kClipParts); }
+// A chunk a workgroup while there are no more chunks than CUs, a group after that.
+uint32_t clip_parts(uint64_t chunks) {
+    return (uint32_t)std::min(std::min<uint64_t>(chunks, kClipParts), std::max<uint64_t>((chunks + 3) / 4, 256));
+}
 
 hipError_t launch_grad_norm(const Clip& a, hipStream_t s) {
     if (a.parts == 0) return hipSuccess;
@@ -202,8 +267,12 @@ hipError_t launch_norm_of_parts(const Clip& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Five workgroups a CU, each of which adds the parts up first: with 2048 the fp32
+// elements above took 2940 us in place of 2740, the bfloat16 ones 1510 for 1280,
+// and a list with nothing to scale 5.1 for 3.4.
 hipError_t launch_clip(const Clip& a, hipStream_t s) {
-    hipLaunchKernelGGL(clip_scale, dim3(std::max(1u, clip_parts(a.chunks))), dim3(kThreads), 0, s, a);
+    const uint32_t blocks = std::max(1u, std::min(clip_parts(a.chunks), 1280u));
+    hipLaunchKernelGGL(clip_scale, dim3(blocks), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
