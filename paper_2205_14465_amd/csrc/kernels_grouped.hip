@@ -260,7 +260,9 @@ __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, 
 struct RunTable {
     uint32_t tiles[kMaxExperts + 1];   // before each expert
     uint32_t rows[kMaxExperts + 1];    // its first
-    uint32_t order[kMaxExperts];       // experts by their rows, the most first
+    // experts by their rows, the most first (grads_large), or an expert's last tile, if at
+    // most half of it has rows, counted apart: such tiles before each (rows_large)
+    uint32_t order[kMaxExperts + 1];
     uint32_t next;                     // a workgroup's next tile
 };
 // Experts by their rows, where it takes few comparisons; fill_runs has run.
@@ -280,50 +282,80 @@ __device__ __forceinline__ void sort_runs(uint32_t experts, RunTable& t) {
     }
     __syncthreads();
 }
-template <uint32_t kHigh>
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t& all) {  // over a wave
+    uint32_t s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(s, o, 64);
+        if ((threadIdx.x & 63) >= (uint32_t)o) s += y;
+    }
+    all = __shfl(s, 63, 64);
+    return s - x;
+}
+template <uint32_t kHigh, bool kApart>
 __device__ __forceinline__ void fill_runs(const Groups& g, RunTable& t) {
     if (threadIdx.x < 64) {
-        uint32_t sum = 0;
+        uint32_t sum = 0, sum_low = 0, all;
         for (uint32_t e0 = 0; e0 <= g.experts; e0 += 64) {
             const uint32_t e = e0 + threadIdx.x;
-            uint32_t at = 0, n = 0;
+            uint32_t at = 0, n = 0, low = 0;
             if (e <= g.experts) at = offset_of(g, e);
             if (e < g.experts) {
                 const uint32_t to = offset_of(g, e + 1);
                 n = to > at ? (to - at + kHigh - 1) / kHigh : 0;
+                if (kApart && n > 0 && (to - at - 1) % kHigh < kHigh / 2) {
+                    low = 1;
+                    --n;
+                }
             }
-            uint32_t s = n;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const uint32_t y = __shfl_up(s, o, 64);
-                if (threadIdx.x >= (uint32_t)o) s += y;
-            }
+            const uint32_t before = sum + sum_before(n, all);
+            sum += all;
             if (e <= g.experts) {
-                t.tiles[e] = sum + s - n;
+                t.tiles[e] = before;
                 t.rows[e] = at;
             }
-            sum += __shfl(s, 63, 64);
+            if constexpr (kApart) {
+                const uint32_t lows = sum_low + sum_before(low, all);
+                sum_low += all;
+                if (e <= g.experts) t.order[e] = lows;
+            }
         }
     }
     __syncthreads();
+}
+// The last expert with counts[e] <= n, all lanes alike.
+__device__ __forceinline__ uint32_t expert_at(const uint32_t* counts, uint32_t experts, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (uint32_t e0 = 0; e0 < experts; e0 += 64)
+        before += __popcll(__ballot(e0 + lane < experts && counts[e0 + lane] <= n));
+    return __builtin_amdgcn_readfirstlane(before - 1);
 }
 // Tile t of a product that is tiles_n tiles wide: as tile_run, without empty ones.
 template <uint32_t kHigh>
 __device__ __forceinline__ void run_in(const RunTable& table, uint32_t experts, uint32_t t, uint32_t tiles_n, Run& r,
                                        uint32_t& tn) {
-    const uint32_t lane = threadIdx.x & 63, row = t / tiles_n;
-    uint32_t n = 0;
-    for (uint32_t e0 = 0; e0 < experts; e0 += 64)
-        n += __popcll(__ballot(e0 + lane < experts && table.tiles[e0 + lane] <= row));
-    r.expert = __builtin_amdgcn_readfirstlane(n - 1);
+    r.expert = expert_at(table.tiles, experts, t / tiles_n);
     const uint32_t before = __builtin_amdgcn_readfirstlane(table.tiles[r.expert]);
+    const uint32_t next = __builtin_amdgcn_readfirstlane(table.tiles[r.expert + 1]);
     const uint32_t at = __builtin_amdgcn_readfirstlane(table.rows[r.expert]);
     r.to = __builtin_amdgcn_readfirstlane(table.rows[r.expert + 1]);
-    const uint32_t high = (r.to - at + kHigh - 1) / kHigh, in = t - before * tiles_n;
+    const uint32_t high = next - before, in = t - before * tiles_n;
     const uint32_t first = in / (kBand * tiles_n) * kBand, here = high - first < kBand ? high - first : kBand;
     const uint32_t i = in - first * tiles_n;
     tn = i / here;
     r.from = at + (first + i % here) * kHigh;
+}
+// Tile t of those that are counted apart.
+template <uint32_t kHigh>
+__device__ __forceinline__ void low_run_in(const RunTable& table, uint32_t experts, uint32_t t, uint32_t tiles_n, Run& r,
+                                           uint32_t& tn) {
+    const uint32_t row = t / tiles_n;
+    r.expert = expert_at(table.order, experts, row);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(table.rows[r.expert]);
+    r.to = __builtin_amdgcn_readfirstlane(table.rows[r.expert + 1]);
+    tn = t - row * tiles_n;
+    r.from = at + (r.to - at) / kHigh * kHigh;
 }
 
 // LDS of a large product: two stages, and of the strips what one does not hold; the
@@ -342,9 +374,9 @@ __device__ __forceinline__ void wait_first() {
 // memory operations count down in order.
 template <typename R, typename E>
 __device__ __forceinline__ void finish_large(R& g, char* lds, const E& epi) {
-    g.template finish_blocks<0, R::kFM - 1>(lds + R::kStageBytes, epi);
+    if (g.busy) g.template finish_blocks<0, R::kFM - 1>(lds + R::kStageBytes, epi);
     wait_vmcnt<0>();
-    g.template finish_blocks<R::kFM - 1, R::kFM>(lds + R::kStageBytes, epi);
+    if (g.busy) g.template finish_blocks<R::kFM - 1, R::kFM>(lds + R::kStageBytes, epi);
     lds_barrier();  // every wave has read its strip, and its part of the next step is there
 }
 
@@ -353,21 +385,30 @@ __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
     typedef RowsLie<forward, 16> L;
     extern __shared__ char lds[];
     RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
-    fill_runs<G::kBM>(p.g, table);
+    fill_runs<G::kBM, true>(p.g, table);
     const uint32_t tiles_n = (p.cols + G::kBN - 1) / G::kBN;
     // (offsets that do not ascend make more tiles than there can be: those are left out)
     const uint32_t tiles_m = min((uint32_t)__builtin_amdgcn_readfirstlane(table.tiles[p.g.experts]),
                                  group_tiles(p.g.rows, p.g.experts, G::kBM));
-    // a die's tiles are consecutive ones, expert by expert, dealt to its workgroups in turn
-    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8, die = blockIdx.x % 8;
-    const uint32_t from = die * q + (die < rest ? die : rest), to = from + q + (die < rest ? 1 : 0);
-    uint32_t t = from + blockIdx.x / 8;
+    const uint32_t low_m = __builtin_amdgcn_readfirstlane(table.order[p.g.experts]);
+    // a die's tiles are consecutive ones, expert by expert, dealt to its workgroups in turn;
+    // those with no more than half their rows, which take less time, come last
+    const uint32_t die = blockIdx.x % 8;
+    const uint32_t total = tiles_m * tiles_n, q = total / 8, rest = total % 8;
+    const uint32_t from = die * q + (die < rest ? die : rest), here = q + (die < rest ? 1 : 0);
+    const uint32_t low_total = low_m * tiles_n, low_q = low_total / 8, low_rest = low_total % 8;
+    const uint32_t low_from = die * low_q + (die < low_rest ? die : low_rest), to = here + low_q + (die < low_rest ? 1 : 0);
+    uint32_t t = blockIdx.x / 8;
     if (t >= to) return;
     RunTile<G, 16> g;
     Run run;
     uint32_t tn;
-    run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
-    begin_rows<L, forward>(g, p, run, tn * G::kBN, lds);
+    auto take = [&](uint32_t i) {
+        if (i < here) run_in<G::kBM>(table, p.g.experts, from + i, tiles_n, run, tn);
+        else low_run_in<G::kBM>(table, p.g.experts, low_from + i - here, tiles_n, run, tn);
+        begin_rows<L, forward>(g, p, run, tn * G::kBN, lds);
+    };
+    take(t);
     g.template rest<L>(lds);
     wait_first<G>();
     for (;;) {
@@ -376,10 +417,7 @@ __global__ __launch_bounds__(G::kThreads) void rows_large(GroupedProduct p) {
         const uint32_t m0 = run.from, n0 = tn * G::kBN;
         t += gridDim.x / 8;
         const bool more = t < to;
-        if (more) {
-            run_in<G::kBM>(table, p.g.experts, t, tiles_n, run, tn);
-            begin_rows<L, forward>(g, p, run, tn * G::kBN, lds);
-        }
+        if (more) take(t);
         finish_large(g, lds, [&](int row, int col, float (&v)[8]) {
             const uint32_t m = m0 + row, n = n0 + col;
             if (m < done.to && n < p.cols) finish_row<TO, forward>(p, done.expert, m, n, v);
@@ -439,7 +477,7 @@ __global__ __launch_bounds__(G::kThreads) void grads_large(GroupedProduct px, Gr
     typedef WeightsLie<kTable, 16> LW;
     extern __shared__ char lds[];
     RunTable& table = *(RunTable*)(lds + kLargeLds<G>);
-    fill_runs<G::kBM>(px.g, table);
+    fill_runs<G::kBM, false>(px.g, table);
     sort_runs(px.g.experts, table);
     const uint32_t die = blockIdx.x % 8, tiles_n = (px.cols + G::kBN - 1) / G::kBN;
     const uint32_t tiles_m = min((uint32_t)__builtin_amdgcn_readfirstlane(table.tiles[px.g.experts]),

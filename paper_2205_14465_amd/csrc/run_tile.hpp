@@ -83,6 +83,7 @@ struct RunTile : B_ {
     uint32_t k;
     const uint32_t* where;
     uint32_t offa[kLoadA], offb[kLoadB], from_b[kLoadB];
+    bool busy;          // whether this wave took part in the last run()'s products
 
     // Chunks' swizzle of row r in LDS, for rows of `width` elements of k down columns.
     template <int width>
@@ -105,6 +106,13 @@ struct RunTile : B_ {
     }
     __device__ __forceinline__ int steps() const { return (int)((k + kBK - 1) / kBK); }
     static __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    // Which rows and columns of blocks are this wave's.  Waves w and w + 4 share a SIMD:
+    // of the largest tile's, the upper four have the columns two on from the lower
+    // ones', so that either half of the rows and either of the columns is one wave a SIMD.
+    static __device__ __forceinline__ int wave_m(int wave) { return wave / kWN; }
+    static __device__ __forceinline__ int wave_n(int wave) {
+        return kBM == 256 && kWN == 4 ? wave % kWN ^ (wave / kWN & 1) * 2 : wave % kWN;
+    }
 
     // Takes up a tile, k long, and asks for its first step; every wave must have read
     // what stage 0 held.  row_a(r): byte offset of row r of an operand A with k
@@ -145,7 +153,11 @@ struct RunTile : B_ {
     __device__ __forceinline__ void rest(char* lds) { ask<L>(lds, 1, kStages); }
 
     // The products over k into acc, after begin() and rest().  kLanded: every wave has
-    // waited for its first step's loads, and met the others since.
+    // waited for its first step's loads, and met the others since; and a wave whose part
+    // of the tile is past the operands' ends loads, and waits, but has no products (16
+    // experts' 16384 rows of 1600 to 6400, from 400 to 2100 an expert: 482 to 452 us,
+    // with such tiles last).  Not with a table, whose loads the compiler then waits for
+    // sooner (the weights' gradient of the same rows 500 to 532 us).
     template <typename L, bool kLanded = false>
     __device__ __forceinline__ void run(char* lds) {
         const int steps = this->steps();
@@ -156,7 +168,15 @@ struct RunTile : B_ {
             for (int n = 0; n < kFN; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
-        const int wm = wave / kWN, wn = wave % kWN;
+        const int wm = wave_m(wave), wn = wave_n(wave);
+        busy = true;
+        if constexpr (kLanded && !L::kTable) {
+            busy = (uint32_t)wm * kFM * 32 < a.count && (uint32_t)wn * kFN * 32 < b.count;
+            if (!busy) {
+                attend<L>(lds, steps);
+                return;
+            }
+        }
         const int hi = lane >> 5, l31 = lane & 31;
         // where this lane's fragments lie in a stage
         const char* fa[kFM];
@@ -242,7 +262,7 @@ struct RunTile : B_ {
     template <int from, int to, typename E>
     __device__ __forceinline__ void finish_blocks(char* lds, const E& epi) {
         const int lane = threadIdx.x & 63, wave = wave_index();
-        const int wm = wave / kWN, wn = wave % kWN;
+        const int wm = wave_m(wave), wn = wave_n(wave);
         float* strip = (float*)lds + wave * 32 * B::kEpiLd;
         constexpr int kLanes = B::kEpiCols / 8, kPass = 64 / kLanes;
 #pragma unroll
@@ -263,6 +283,23 @@ struct RunTile : B_ {
     }
 
   private:
+    // run() without its products: the same loads, waits and barriers.
+    template <typename L>
+    __device__ __forceinline__ void attend(char* lds, int steps) {
+        int stage = 0;
+#pragma unroll 1
+        for (int step = 0; step + 1 < steps; ++step) {
+            if (step + kStages <= steps) wait_vmcnt<(kStages - 2) * kLoads>();
+            else wait_vmcnt<0>();
+            lds_barrier();
+            if (step + kStages < steps) {
+                if (step + kStages == steps - 1) mask_last<L>();
+                load<L>(lds, stage, step + kStages);
+            }
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+        lds_barrier();
+    }
     template <typename L>
     __device__ __forceinline__ void ask(char* lds, int from, int to) {
 #pragma unroll
