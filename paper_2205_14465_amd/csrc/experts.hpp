@@ -115,12 +115,13 @@ hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& r
 
 // The forward pass for few rows, which needs no workspace: up to 64 in all; more in
 // fp32, whose tiles are bound by the matrix instructions wherever rows fill them badly,
-// and where 16-bit weights would be laid out first.  us, this way and by tiles: fp32, 8
-// experts of 1600x1600, 128 rows 28 and 38, 256 50 and 57, 512 83 and 60; 64 experts 128
-// rows 125 and 177, 1024 205 and 205; fp16, 64 experts of 768x768, 64 rows 15 and 13, of
-// 1001x515 256 rows 32 and 36, 1024 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
+// and where 16-bit weights would be laid out first.  us, this way and by tiles, with rows
+// spread evenly (all with one expert): fp32, 8 experts of 1600x1600, 100 rows 25 (34) and
+// 34 (32), 192 34 (55) and 34 (32); 64 experts 128 rows 133 (44) and 189 (32), 500 164
+// (144) and 189 (36); fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows
+// 32 and 36, 1024 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
 inline uint64_t grouped_few_rows(int dtype, uint32_t experts, bool laid_out) {
-    return 64 + (dtype == BC_F32 ? 32ull * experts : laid_out ? 8ull * experts : 0);
+    return 64 + (dtype == BC_F32 || laid_out ? 8ull * experts : 0);
 }
 struct GroupedFew {
     Groups g;
