@@ -69,9 +69,10 @@ struct Groups {
     const int32_t* offsets;  // [experts + 1], ascending
     uint32_t experts, rows;
 };
-// Tiles of `high` rows: expert e has those from offsets[e] / high - offsets[0] /
-// high + e on up to its successor's first, the last of which may be empty.  So a
-// tile's expert is found by comparisons alone; there are at most so many:
+// Pieces of `high` rows: expert e has those from offsets[e] / high - offsets[0] /
+// high + e on up to its successor's first, the last of which may be empty, so that a
+// piece's expert is found by comparisons alone.  There are at most so many, which
+// bounds the tiles with rows as well:
 __host__ __device__ inline uint32_t group_tiles(uint32_t rows, uint32_t experts, uint32_t high) { return rows / high + experts; }
 
 // A matrix for every expert, or one for all.

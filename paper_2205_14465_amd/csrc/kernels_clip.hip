@@ -240,7 +240,8 @@ __global__ __launch_bounds__(kThreads) void clip_scale(Clip a) {
     });
 }
 
-// 960 words of a table as arguments.
+// 960 words of a table as arguments: a captured graph holds them itself, where a copy
+// from the host would leave it with a pointer.
 constexpr uint32_t kTableWords = 960;
 struct TableWords {
     uint32_t w[kTableWords];

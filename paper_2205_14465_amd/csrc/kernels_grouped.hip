@@ -4,8 +4,8 @@
 //   dx = dz w_e,  dw_e = dz_e^T x_e,  dbias_e = sum over the expert's rows of dz.
 //
 // Where the runs begin is known to the device alone.  A launch has a workgroup
-// for every tile that there can be; a tile finds its expert among the offsets by
-// comparisons (experts.hpp), and those without rows end at once.  No operand is
+// for every tile that there can be; a workgroup finds its tile's expert by counting the
+// experts' tiles, and those without a tile end at once.  No operand is
 // turned in memory: dx takes w and dw takes dz and x with k down their columns
 // (run_tile.hpp).  Operands are read where they lie, x through `source` if it is
 // given, but for 16-bit ones whose rows are no whole 16-byte pieces, which are laid
@@ -189,6 +189,10 @@ __device__ __forceinline__ void begin_weights(R& g, const GroupedProduct& p, uin
     g.template begin<L>(a, b, to > from && from >= first ? to - from : 0, where, lds, [](int) { return 0u; });
 }
 
+// The experts' rows times their weight in tiles that leave room for others on a
+// compute unit.  fp32, 2474 rows of 1001 to 515: 43 us, 60 TFLOP/s of 152: 387 tiles
+// of 64x64 on 256 units, where the second round leaves half of them idle; whole
+// 16-byte pieces or single words make no difference.
 template <typename G, typename TO, bool forward, int kPiece>
 __device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t block, char* lds) {
     typedef RowsLie<forward, kPiece> L;
@@ -257,7 +261,9 @@ __device__ __forceinline__ void bias_columns(const GroupedBias& a, uint32_t bloc
         ((TO*)a.out)[e * a.ld + c] = (TO)((sums[lane] + sums[64 + lane]) + (sums[128 + lane] + sums[192 + lane]));
 }
 
-// Both gradients' products where tiles of this size do not fill the chip, and dbias:
+// Both gradients' products where tiles of this size do not fill the chip, and dbias
+// (8 experts' 2048 rows of 768 to 768 in fp32: 62 us, 78 TFLOP/s of 152, with the tiles'
+// first loads and epilogues in the open; apart they took 5 us more):
 // `split` workgroups of the first product (dx's with rows_first: the one whose k is the
 // longer), those of the second up to `end`, then the bias's.
 template <typename G, typename TO, bool kTable, int kPiece>
@@ -278,6 +284,14 @@ __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, 
 // The largest tiles fill a compute unit, so nothing runs beside one's epilogue.
 // Workgroups stay: before a tile's epilogue a workgroup takes up its next tile and
 // asks for its first step, the other stage of LDS serves as the strips.
+//
+// They are bound by the matrix units at the clock that the power limit leaves (1.8 to
+// 2.0 GHz, those units busy 37 to 52 % of all cycles) and by the epilogues between
+// them: 16 experts' 16384 rows of 1600 to 6400 in bfloat16, y and z written, 443 to 480
+// us, without z and activation 400; 6400 to 1600 355, 940 TFLOP/s; both gradients of
+// the first 765.  Half tiles with two workgroups a unit (128x256, 256x128, 32 along k),
+// three stages of 32, reading ahead into the L2 and other heights of a band (2 to 16)
+// were as fast or slower.
 
 // The experts' tiles and rows, in LDS.
 struct RunTable {
@@ -743,6 +757,8 @@ __device__ __forceinline__ int busy_expert(const Groups& g, uint32_t i, uint32_t
 }
 
 // A wave a row of w, kRows of the expert's rows at a time: products and sums in fp32.
+// Bound by memory, w being read once (one token through two experts of 6400x1600 in
+// fp16: 8.6 us for 41 MB, 4.8 TB/s).
 constexpr int kFewAtOnce = 4;
 template <typename T, bool kWhole>
 __global__ __launch_bounds__(256) void grouped_few(GroupedFew a) {
@@ -803,7 +819,8 @@ __global__ __launch_bounds__(256) void grouped_few(GroupedFew a) {
 }
 
 // Sixteen rows of w by up to 16 kGroups of the expert's rows on the matrix cores: the
-// waves share out the inner axis and meet in LDS.
+// waves share out the inner axis and meet in LDS.  w is read once for every 32 rows of
+// its expert (64 rows of 8 experts 1600x6400 in fp16: 34 us for 164 MB, 4.8 TB/s).
 constexpr int kFewWaves = 8;
 template <typename T, int kGroups>
 __device__ __forceinline__ void few_block(const GroupedFew& a, uint32_t e, uint32_t r0, uint32_t to, float* meet) {
@@ -905,7 +922,8 @@ __device__ __forceinline__ void lay_rows(const LayRows& a, uint32_t block, uint3
 }
 
 // A workgroup 64 rows of one expert by 128 columns; all its loads go out before the
-// first is used.  Bound by memory: TODO.
+// first is used.  Bound by memory: 16384 rows of 6400 in bfloat16, with z, 109 us, 5.8
+// TB/s (as part of prepare).
 constexpr uint32_t kSlopeCols = 128;
 template <typename T>
 __device__ __forceinline__ void slope_tile(const Groups& g, const GroupedSlope& a, uint32_t block) {
@@ -1040,11 +1058,12 @@ static hipError_t pair_tile(int tile, const GroupedProduct& x, const GroupedProd
 hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& x, const GroupedProduct& w, const GroupedBias& bias,
                                uint32_t* counters, hipStream_t s) {
     double both = 0.0, tx = 0.0, tw = 0.0;
-    tile_for(kGroupedRows, dtype, x, tx);
-    tile_for(kGroupedWeights, dtype, w, tw);
+    const int of_x = tile_for(kGroupedRows, dtype, x, tx), of_w = tile_for(kGroupedWeights, dtype, w, tw);
     const int tile = tile_for_both(dtype, x, w, both);
-    // (a launch of its own: 3 us, and the bias's another 3)
-    if (both < tx + tw + 3.0 + (bias.out && tile < 2 ? 3.0 : 0.0)) {
+    // (a launch of its own: 3 us, and the bias's another 3.  Where both products want the
+    // largest tiles, as the experts' runs leave their rounds more ragged than the costs
+    // say: 16 experts' 16384 rows of 1600 to 6400 872 to 847 us, all with 1024 rows 793 to 776)
+    if ((tile == 2 && of_x == 2 && of_w == 2) || both < tx + tw + 3.0 + (bias.out && tile < 2 ? 3.0 : 0.0)) {
         if (dtype == BC_F32) return pair_tile<float, float>(tile, x, w, bias, counters, s);
         if (dtype == BC_F16) {
             if (out_dtype == BC_F32) return pair_tile<f16_t, float>(tile, x, w, bias, counters, s);

@@ -11,9 +11,14 @@
 // expert, so that the rank is a count of bits and no order of atomics shows),
 // route_scan adds the blocks' counts up, route_place adds what lies before.
 //
+// Few bytes: what costs is the chain of launches and, within the first, of choices
+// (16384 rows of 64 experts, k 2, bfloat16: 4.9, 2.5 and 3.3 us; 32768 of 1024, k 8, 99
+// in all).  Up to 64 rows go in one launch and workgroup (one row, k 8: 5.6 us).
+//
 // Combination: out = residual + sum_j weight_j y[slot_j], the sum in fp32 in the
 // order of j, and its gradient.  Bound by memory: a row's results are k whole
-// rows elsewhere.
+// rows elsewhere (8192x1600, k 2, bfloat16, with residual: 17.2 us, 6.1 TB/s; its
+// gradient at 8000x1001 in fp16, in rows that are no whole pieces: 16.6, 4.8 TB/s).
 #include "common.hpp"
 #include "experts.hpp"
 
@@ -286,7 +291,8 @@ __global__ __launch_bounds__(kGate<G>) void route_small(Route a) {
 
 // dlogits: normalised over the chosen, w_e (dw_e - sum_j w_j dw_j) for them;
 // otherwise p_e ([chosen] dw_e - sum_j p_j dw_j).  Logits of -inf get 0, whatever
-// the sum is.
+// the sum is.  Bound by memory, behind three round trips to it (8191 rows of 129, k 4,
+// fp32: 7.4 us for 8.7 MB).
 template <typename T, int G, int V>
 __device__ __forceinline__ void grad_row(const RouteGrad& a, uint64_t row, uint32_t lane) {
     const bool there = row < a.rows;
