@@ -717,7 +717,8 @@ enum bc_norm { BC_NORM_L2 = 0, BC_NORM_MAX = 1 };
 
 /* One gradient [rows, cols] of element type dtype (any mix in a list); out
  * [rows, cols], of the same type, receives the clipped one and may be grad itself
- * (same stride); the norm alone does not look at it. */
+ * (same stride); the norm alone does not look at it.  A gradient given twice counts
+ * twice in the norm; no out may overlap another out or another gradient. */
 typedef struct bc_grad {
     const void* grad;
     void* out;

@@ -191,8 +191,8 @@ __device__ __forceinline__ void begin_weights(R& g, const GroupedProduct& p, uin
 
 // The experts' rows times their weight in tiles that leave room for others on a
 // compute unit.  fp32, 2474 rows of 1001 to 515: 43 us, 60 TFLOP/s of 152: 387 tiles
-// of 64x64 on 256 units, where the second round leaves half of them idle; whole
-// 16-byte pieces or single words make no difference.
+// of 64x64 on 256 units, where the second round leaves half of them idle, and loads of
+// single words (1004 to 516, whole pieces: 39).
 template <typename G, typename TO, bool forward, int kPiece>
 __device__ __forceinline__ void rows_tile(const GroupedProduct& p, uint32_t block, char* lds) {
     typedef RowsLie<forward, kPiece> L;
@@ -262,8 +262,9 @@ __device__ __forceinline__ void bias_columns(const GroupedBias& a, uint32_t bloc
 }
 
 // Both gradients' products where tiles of this size do not fill the chip, and dbias
-// (8 experts' 2048 rows of 768 to 768 in fp32: 62 us, 78 TFLOP/s of 152, with the tiles'
-// first loads and epilogues in the open; apart they took 5 us more):
+// (8 experts' 2048 rows of 768 to 768 in fp32: 50 us with 256 rows each, 96 TFLOP/s of
+// 152, with the tiles' first loads and epilogues in the open; 62 with 200 to 300, whose
+// ends fill tiles badly):
 // `split` workgroups of the first product (dx's with rows_first: the one whose k is the
 // longer), those of the second up to `end`, then the bias's.
 template <typename G, typename TO, bool kTable, int kPiece>
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, 
 // They are bound by the matrix units at the clock that the power limit leaves (1.8 to
 // 2.0 GHz, those units busy 37 to 52 % of all cycles) and by the epilogues between
 // them: 16 experts' 16384 rows of 1600 to 6400 in bfloat16, y and z written, 443 to 480
-// us, without z and activation 400; 6400 to 1600 355, 940 TFLOP/s; both gradients of
+// us, without z 410; 6400 to 1600 355, 940 TFLOP/s; both gradients of
 // the first 765.  Half tiles with two workgroups a unit (128x256, 256x128, 32 along k),
 // three stages of 32, reading ahead into the L2 and other heights of a band (2 to 16)
 // were as fast or slower.
