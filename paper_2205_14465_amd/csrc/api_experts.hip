@@ -253,7 +253,7 @@ int bytecomp_route_forward(int dtype, uint64_t rows, uint32_t experts, uint32_t 
     if (need > 0 && (!ws || ws_bytes < need)) return BC_E_WORKSPACE;
     const uint32_t blocks = route_blocks(rows, experts);
     const Route a{logits, ld, rows, experts, k, normalise != 0, weight, expert, slot, source, offsets, (uint32_t*)ws,
-                  blocks > 0 ? blocks : 1, route_block_rows(rows, experts)};
+                  blocks > 0 ? blocks : 1, route_block_rows(rows, experts), false};
     hipStream_t s = (hipStream_t)stream;
     return finish_call(status_of(launch_route(dtype, a, s)), s, nullptr);
 }

@@ -20,12 +20,13 @@ struct Route {
     int normalise;
     float* weight;
     int32_t *expert, *slot, *source, *offsets;
-    uint32_t* count;         // [experts][blocks], then [experts] totals
+    uint32_t* count;         // [experts][blocks], then [experts] totals; or [blocks][experts] (add)
     uint32_t blocks;         // workgroups of route_gate
     uint32_t block_rows;     // rows of each, a multiple of 64
+    bool add;                // set by launch_route: the last launch adds the counts up
 };
 uint32_t route_block_rows(uint64_t rows, uint32_t experts);
-hipError_t launch_route(int dtype, const Route& a, hipStream_t s);
+hipError_t launch_route(int dtype, Route a, hipStream_t s);
 
 struct RouteGrad {
     const void* logits;

@@ -11,6 +11,12 @@ from tests.test_gpu_layernorm import F32, close, f64
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def seeded():
+    import torch
+    torch.manual_seed(17)
+
+
 def tensors(experts, n, inner, cols, dtype, seed, x_rows=None):
     import torch
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -269,3 +275,32 @@ def test_graphs_that_share_workspaces():
             for a, b in zip(sides[j].out, alone.out):
                 assert torch.equal(a, b)
         alone.run(shared)
+
+
+@pytest.mark.parametrize("rows,experts,k", [(65, 5, 5), (100, 512, 8), (128, 300, 32), (190, 257, 3), (1000, 64, 2), (1024, 64, 8),
+                                            (1025, 64, 2), (4000, 64, 1), (5000, 3, 2)])
+def test_order_of_the_choices(rows, experts, k):
+    """Blocks of rows few enough that the last launch adds their counts up, and more:
+    the slots are a stable sort by expert of the choices that there are."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    logits = torch.randn(rows, experts, device="cuda")
+    logits[torch.rand(rows, experts, device="cuda") < 0.3] = -torch.inf
+    weight = torch.empty(rows, k, device="cuda")
+    expert, slot = (torch.empty(rows, k, dtype=torch.int32, device="cuda") for _ in range(2))
+    src = torch.full((rows * k,), -7, dtype=torch.int32, device="cuda")
+    off = torch.empty(experts + 1, dtype=torch.int32, device="cuda")
+    ws = B.alloc_route_workspace(rows, experts, k)
+    ws.fill_(255)
+    B.bytecomp_route_forward(logits, weight, expert, slot, src, off, ws)
+    e = expert.view(-1).long().cpu()
+    there = (e >= 0).nonzero()[:, 0]
+    order = there[torch.sort(e[there], stable=True)[1]]
+    want = torch.full_like(e, -1)
+    want[order] = torch.arange(len(order))
+    assert torch.equal(slot.view(-1).long().cpu(), want)
+    assert torch.equal(src[:len(order)].long().cpu(), order // k) and bool((src[len(order):] == -7).all())
+    counts = torch.bincount(e[there], minlength=experts)
+    assert torch.equal(off.long().cpu(), torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)]))
+    best = [t[:, :k] for t in logits.sort(dim=1, descending=True, stable=True)]  # of equals the lower
+    assert torch.equal(expert, torch.where(best[0] == -torch.inf, -1, best[1]).int())

@@ -8,6 +8,12 @@ pytestmark = pytest.mark.gpu
 WIDTH, HIDDEN = 96, 160
 
 
+@pytest.fixture(autouse=True)
+def seeded():
+    import torch
+    torch.manual_seed(17)
+
+
 def plain(params, x, expert):
     """The block's output in 64 bits, each row's experts given."""
     import torch
