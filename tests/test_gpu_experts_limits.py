@@ -304,3 +304,41 @@ def test_order_of_the_choices(rows, experts, k):
     assert torch.equal(off.long().cpu(), torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)]))
     best = [t[:, :k] for t in logits.sort(dim=1, descending=True, stable=True)]  # of equals the lower
     assert torch.equal(expert, torch.where(best[0] == -torch.inf, -1, best[1]).int())
+
+
+@pytest.mark.parametrize("inner,cols,n", [(264, 392, 900), (1800, 376, 2889)])
+def test_two_calls_at_once(inner, cols, n):
+    """The same calls on two streams, on other tensors and workspaces of their own, with
+    nothing between them: each as by itself."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    counts = [n // 8 + (i == 3) * 50 - (i == 4) * 50 for i in range(8)]
+    counts[7] += n - sum(counts)
+    off, sides = offsets_of(counts), []
+    for i in range(2):
+        x, w, dy, dt = tensors(8, n, inner, cols, "bfloat16", 40 + i)
+        out = (torch.empty(n, cols, dtype=dt, device="cuda"), torch.empty(n, inner, dtype=dt, device="cuda"), torch.empty_like(w),
+               torch.empty(8, cols, dtype=dt, device="cuda"), torch.empty(1, dtype=torch.float64, device="cuda"))
+        sides.append((x, w, dy, out, B.alloc_grouped_linear_workspace(x, w, n, backward=True),
+                      B.alloc_grad_norm_workspace([w, w]), torch.cuda.Stream()))
+
+    def run(x, w, dy, out, ws, norm_ws, stream):
+        y, dx, dw, db, norm = out
+        B.bytecomp_grouped_linear_forward(x, None, off, w, None, "gelu", y, None, ws, stream=stream)
+        B.bytecomp_grouped_linear_backward(dy, None, x, None, off, w, "none", dx, dw, db, ws, stream=stream)
+        B.bytecomp_grad_norm([dw, db], norm, norm_ws, stream=stream)
+    want = []
+    for s in sides:
+        run(*s)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in s[3]])
+        for t in s[3]:
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s in sides:
+            run(*s)
+    torch.cuda.synchronize()
+    for s, ws in zip(sides, want):
+        for a, b in zip(s[3], ws):
+            assert torch.equal(a, b)
