@@ -6,10 +6,10 @@
 // launch the workgroups' in a fixed order.  The maximum is taken over the
 // magnitudes' bits, so that a NaN is the largest.
 //
-// Both passes are bound by memory (1.56e9 fp32 elements: 1015 us for the norm, 6.1
-// TB/s, and 2740 for the scaling to another place, 4.5, a copy's rate; in bfloat16
-// 524 and 1280; ResNet-50's 161 gradients of 25.6e6 elements: 26 and, with nothing
-// to scale, 3.4).  A workgroup takes a run of consecutive chunks and finds its
+// Both passes are bound by memory (1.56e9 fp32 elements: 1010 us for the norm, 6.2
+// TB/s, and 2490 for the scaling to another place, 5.0, where a copy reaches 4.3 and an
+// elementwise product of one array 5.9; in bfloat16 521 and 1250; ResNet-50's 161
+// gradients of 25.6e6 elements: 26 and, with nothing to scale, 3.4).  A workgroup takes a run of consecutive chunks and finds its
 // first matrix by a search of the table with all its threads; the second pass walks
 // its run backwards and meets what the caches kept of the first.  A thread has 128
 // bytes of loads in flight whatever the type (with 64 of the 16-bit types the norm
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void clip_scale(Clip a) {
                 end -= m;
                 if (whole_group<E>(d, chunk + end, m)) {
                     // 16 bytes a lane, side by side: of 32 bytes in two instructions, fp32's
-                    // lines are written in halves (the elements above 2740 us in place of 2470)
+                    // lines are written in halves (the elements above 2740 us in place of 2490)
                     constexpr int kEach = 16 / (int)sizeof(E), kLoads = 8;
                     const uint64_t at = (chunk + end) * kClipChunk * 8 + threadIdx.x * kEach;
                     Raw<E, kEach> v[kLoads];
@@ -291,9 +291,9 @@ hipError_t launch_norm_of_parts(const Clip& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Five workgroups a CU, each of which adds the parts up first: with 2048 the fp32
-// elements above took 2940 us in place of 2740, the bfloat16 ones 1510 for 1280,
-// and a list with nothing to scale 5.1 for 3.4.
+// Five workgroups a CU, each of which adds the parts up first: from 768 to 2048 the
+// elements above take the same time, ResNet-50's to another place 36 us but 41 with 1024,
+// and a list with nothing to scale 3.4 but 5.1 with 2048.
 hipError_t launch_clip(const Clip& a, hipStream_t s) {
     const uint32_t blocks = std::max(1u, std::min(clip_parts(a.chunks), 1280u));
     hipLaunchKernelGGL(clip_scale, dim3(blocks), dim3(kThreads), 0, s, a);

@@ -286,8 +286,8 @@ __global__ __launch_bounds__(G::kThreads) void grads_product(GroupedProduct px, 
 // Workgroups stay: before a tile's epilogue a workgroup takes up its next tile and
 // asks for its first step, the other stage of LDS serves as the strips.
 //
-// They are bound by the matrix units at the clock that the power limit leaves (1.8 to
-// 2.0 GHz, those units busy 37 to 52 % of all cycles) and by the epilogues between
+// They are bound by the matrix units at the clock that the power limit leaves (1.7 to
+// 2.0 GHz, those units busy 35 to 52 % of all cycles) and by the epilogues between
 // them: 16 experts' 16384 rows of 1600 to 6400 in bfloat16, y and z written, 443 to 480
 // us, without z 410; 6400 to 1600 355, 940 TFLOP/s; both gradients of
 // the first 765.  Half tiles with two workgroups a unit (128x256, 256x128, 32 along k),
