@@ -82,6 +82,9 @@ bool readable(int dtype, const void* p, uint64_t ld, uint64_t k) {
 constexpr uint64_t kMaxStride = 1ull << 21;
 // So are those of gathered rows.
 constexpr uint64_t kGatherBytes = 0x7fffff00u;
+bool in_reach(int dtype, bool gather, uint64_t x_rows, uint64_t ldx) {
+    return !gather || x_rows * ldx * dtype_bytes(dtype) <= kGatherBytes;
+}
 
 // x laid out: its own rows, or, where the call takes fewer or they are too many
 // for 32-bit offsets, the call's rows one after the other.
@@ -125,7 +128,7 @@ struct GroupedX {
 GroupedSide side_of_x(int dtype, GroupedX& x, uint32_t& a_rows, bool& wide, Carver& c, LayRows& lay) {
     const bool gather = x.source != nullptr;
     a_rows = (uint32_t)(gather ? x.rows : x.call_rows);
-    if (readable(dtype, x.x, x.ld, x.inner) && (!gather || x.rows * x.ld * dtype_bytes(dtype) <= kGatherBytes)) {
+    if (readable(dtype, x.x, x.ld, x.inner) && in_reach(dtype, gather, x.rows, x.ld)) {
         wide = wide && whole(dtype, x.x, x.ld, x.inner);
         return GroupedSide{x.x, x.ld, 0};
     }
@@ -335,7 +338,8 @@ int bytecomp_grouped_linear_forward(int dtype, uint64_t rows, uint64_t inner, ui
         return BC_E_ALIGN;
     hipStream_t s = (hipStream_t)stream;
     const Groups g{offsets, experts, (uint32_t)rows};
-    const bool lies = readable(dtype, x, ldx, inner) && readable(dtype, w, ldw, inner) && (dtype == BC_F32 || expert_w % 8 == 0);
+    const bool lies = readable(dtype, x, ldx, inner) && in_reach(dtype, source, x_rows, ldx) && readable(dtype, w, ldw, inner) &&
+                      (dtype == BC_F32 || expert_w % 8 == 0);
     if (rows <= grouped_few_rows(dtype, experts, !lies)) {
         const GroupedFew a{g, x, w, bias, source, y, z, ldx, ldw, expert_w, ld_bias, ldy, ldz,
                            (uint32_t)(source ? x_rows : rows), (uint32_t)inner, (uint32_t)cols, act};

@@ -117,7 +117,8 @@ hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& r
 
 // The forward pass for few rows, which needs no workspace: up to 64 in all; more in
 // fp32, whose tiles are bound by the matrix instructions wherever rows fill them badly,
-// and where 16-bit weights would be laid out first.  us, this way and by tiles, with rows
+// and where 16-bit operands would be laid out first (weights in rows of no whole pieces, a
+// gather from more than 2 GB).  us, this way and by tiles, with rows
 // spread evenly (all with one expert): fp32, 8 experts of 1600x1600, 100 rows 25 (34) and
 // 34 (32), 192 34 (55) and 34 (32); 64 experts 128 rows 133 (44) and 189 (32), 500 164
 // (144) and 189 (36); fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows

@@ -117,6 +117,33 @@ def test_grouped_linear_refusals():
     assert e.value.code == -3
 
 
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("experts", [1, 3, 64, 1024])
+@pytest.mark.parametrize("x_rows,ldx", [(1 << 25, 64), (1 << 10, 1 << 20), ((1 << 31) - 1, 65), (90, 64), (0, 64)])
+def test_a_workspace_of_the_size_asked_for_is_enough(x_rows, ldx, experts, dtype):
+    """Also where a source reads from more than 2 GB, on either side of the most rows that
+    need none; the calls then get as far as the launch, which fails (-8) without a device."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would launch on addresses that are no memory")
+    L = B.lib()
+    few = 64 + 8 * experts
+    for rows in (1, 64, 65, few - 1, few, few + 1, few + 700):
+        for src, x, inner in ((S, X, 64), (S, X, 63), (None, X, 64), (S, ODD, 64), (S, X, 8)):
+            if dtype == 0 and x is ODD:
+                continue
+            for backward in (False, True):
+                need = B.bytecomp_grouped_linear_workspace_size(dtype, rows, x_rows if src else rows, inner, 32, experts, backward)
+                ws = WS if need else None
+                if backward:
+                    rc = L.bytecomp_grouped_linear_backward(dtype, dtype, rows, inner, 32, experts, O, Y, 32, Y, 32, 1, x, ldx,
+                                                            src, x_rows, W, 64, 2048, X, 64, W, 64, 2048, W, 32, ws, need, None)
+                else:
+                    rc = L.bytecomp_grouped_linear_forward(dtype, rows, inner, 32, experts, O, x, ldx, src, x_rows, W, 64, 2048,
+                                                           None, 32, 0, Y, 32, None, 32, ws, need, None)
+                assert rc == -8, (rows, inner, backward, need, rc)
+
+
 def test_clip_refusals():
     L = B.lib()
 

@@ -104,6 +104,31 @@ def test_rows_from_more_than_2gb(dtype):
         check_product(dw[e], dy[r].T, X[r], dtype)
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("counts", [[25, 0, 40], [60, 1, 27]])
+def test_some_rows_from_more_than_2gb(counts, dtype):
+    """So few (65, and 64 + 8 experts) that the forward pass asks for no workspace."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    inner, cols, n, dt = 264, 72, sum(counts), getattr(torch, dtype)
+    x_rows = (5 << 30) // (inner * dt.itemsize)
+    x = torch.empty(x_rows, inner, dtype=dt, device="cuda")
+    src = torch.randint(0, x_rows, (n,), device="cuda")
+    src[:3] = torch.tensor([x_rows - 1, 0, x_rows // 2])
+    x[src] = torch.randn(n, inner, device="cuda").to(dt)
+    X = x[src]
+    w = torch.randn(3, cols, inner, device="cuda").mul(inner ** -0.5).to(dt)
+    y = torch.empty(n, cols, dtype=dt, device="cuda")
+    ws = B.alloc_grouped_linear_workspace(x, w, n)
+    assert ws.numel() == 0
+    B.bytecomp_grouped_linear_forward(x, src.int(), offsets_of(counts), w, None, "none", y, None, ws)
+    at = 0
+    for e, c in enumerate(counts):
+        if c:
+            check_product(y[at:at + c], X[at:at + c], w[e].T, dtype)
+        at += c
+
+
 @pytest.mark.parametrize("dtype,counts", [("float16", [3, 2, 4]), ("float32", [20, 31, 200]), ("bfloat16", [700, 1, 300])])
 def test_experts_further_apart_than_32_bits(dtype, counts):
     import torch
