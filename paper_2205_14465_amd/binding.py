@@ -1026,6 +1026,8 @@ class CombineGradCall(_Call):
         import torch
         rows, cols = dout.shape
         k = slot.shape[1]
+        if y is None and dweight is not None:
+            raise ValueError("y: needed for dweight, got None")
         like = next((t for t in (dy, y) if t is not None), None)
         slots = 0 if like is None else like.shape[0]
         pd, ldd = _matrix("dout", dout, rows, cols, dout.dtype)

@@ -197,3 +197,20 @@ def test_grad_list_of_strided_and_contiguous():
         B._grad_list([dev(torch.zeros(2, 3, 4)).transpose(0, 1)], None)
     with pytest.raises(ValueError):
         B._grad_list([torch.zeros(3)], None)
+
+
+def test_combination_gradient_wants_what_it_reads():
+    """Without y there is nothing to take dweight from, also where no dy tells the slots."""
+    import torch
+
+    class Dev(torch.Tensor):
+        is_cuda = True
+
+    def dev(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(Dev)
+    dout, slot, weight, y = dev(4, 8), dev(4, 2, dtype=torch.int32), dev(4, 2), dev(8, 8)
+    for dy in (None, dev(8, 8)):
+        with pytest.raises(ValueError, match="y:"):
+            B.CombineGradCall(dout, None, slot, weight, dy, dev(4, 2))
+    for given, dy, dweight in ((None, dev(8, 8), None), (None, None, None), (y, None, dev(4, 2)), (dev(0, 8), None, dev(4, 2))):
+        B.CombineGradCall(dout, given, slot, weight, dy, dweight)
