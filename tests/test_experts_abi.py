@@ -208,9 +208,11 @@ def test_combination_gradient_wants_what_it_reads():
 
     def dev(*shape, dtype=torch.float32):
         return torch.zeros(*shape, dtype=dtype).as_subclass(Dev)
+    class Stream:
+        cuda_stream = 0
     dout, slot, weight, y = dev(4, 8), dev(4, 2, dtype=torch.int32), dev(4, 2), dev(8, 8)
     for dy in (None, dev(8, 8)):
         with pytest.raises(ValueError, match="y:"):
-            B.CombineGradCall(dout, None, slot, weight, dy, dev(4, 2))
+            B.CombineGradCall(dout, None, slot, weight, dy, dev(4, 2), Stream)
     for given, dy, dweight in ((None, dev(8, 8), None), (None, None, None), (y, None, dev(4, 2)), (dev(0, 8), None, dev(4, 2))):
-        B.CombineGradCall(dout, given, slot, weight, dy, dweight)
+        B.CombineGradCall(dout, given, slot, weight, dy, dweight, Stream)
