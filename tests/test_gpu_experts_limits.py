@@ -367,3 +367,44 @@ def test_two_calls_at_once(inner, cols, n):
     for s, ws in zip(sides, want):
         for a, b in zip(s[3], ws):
             assert torch.equal(a, b)
+
+
+# few rows, small tiles of both kinds, rows that are laid out, and the sizes above at
+# which the largest tiles take the forward pass, dx and both gradients
+@pytest.mark.parametrize("experts,n,inner,cols,dtype", [
+    (3, 20, 64, 64, "float32"), (70, 900, 64, 72, "float32"), (200, 1700, 33, 19, "float32"), (200, 2100, 40, 24, "float16"),
+    (130, 1900, 33, 19, "bfloat16"), (4, 5441, 264, 2568, "bfloat16"), (3, 8951, 1544, 264, "float16"),
+    (8, 2889, 1800, 376, "bfloat16"), (300, 9257, 520, 640, "float16")])
+def test_offsets_of_any_kind_leave_what_is_beside(experts, n, inner, cols, dtype):
+    """Offsets that do not ascend or pass the rows: results are unspecified, but nothing
+    around an output or the workspace is written."""
+    import torch
+    from paper_2205_14465_amd import binding as B
+    beside = 1 << 16
+    bufs = []
+
+    def guarded(*shape, of):
+        size = int(np.prod(shape))
+        buf = torch.full((size + 2 * beside,), 7, dtype=of, device="cuda")
+        bufs.append((buf, size))
+        return buf[beside:beside + size].view(shape)
+    x, w, dy, dt = tensors(experts, n, inner, cols, dtype, n)
+    src = torch.randint(-2, n + 2, (n,), device="cuda").int()
+    y, z, dx = (guarded(n, c, of=dt) for c in (cols, cols, inner))
+    dw, db = guarded(experts, cols, inner, of=dt), guarded(experts, cols, of=dt)
+    sizes = [B.alloc_grouped_linear_workspace(x, w, n, backward=b).numel() for b in (False, True)]
+    ws = [guarded(size, of=torch.uint8) for size in sizes]
+    rng = np.random.default_rng(n)
+    up = np.sort(rng.integers(0, n + 1, experts + 1))
+    ends = np.array([-(1 << 31), (1 << 31) - 1, 0, n, n - 1, 1, n // 2])
+    for values in (up[::-1], rng.permutation(up), rng.integers(-5, n + 6, experts + 1), rng.choice(ends, experts + 1)):
+        off = torch.from_numpy(values.astype(np.int32)).cuda()
+        for source in (src, None):
+            B.bytecomp_grouped_linear_forward(x, source, off, w, None, "gelu_tanh", y, z, ws[0] if sizes[0] else None)
+            for act, pre in (("none", None), ("silu", z)):
+                B.bytecomp_grouped_linear_backward(dy, pre, x, source, off, w, act, dx, dw, db, ws[1])
+                B.bytecomp_grouped_linear_backward(dy, pre, x, source, off, w, act, dx, None, None, ws[1])
+                B.bytecomp_grouped_linear_backward(dy, pre, x, source, off, w, act, None, dw, db, ws[1])
+        torch.cuda.synchronize()
+        for buf, size in bufs:
+            assert bool((buf[:beside] == 7).all()) and bool((buf[beside + size:] == 7).all())
