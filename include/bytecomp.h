@@ -698,7 +698,8 @@ int bytecomp_grouped_linear_workspace_size(int dtype, uint64_t rows, uint64_t x_
  *           elements apart.  An expert without rows has dw and dbias of zeros; rows
  *           of dx before the first offset and behind the last are left as they were.
  * In fp16 and bfloat16, dz is rounded to dtype for the products, as in the linear
- * layer; dbias sums it unrounded. */
+ * layer, also where dw is fp32 (half a unit of dtype in each term of its sums);
+ * dbias sums it unrounded. */
 int bytecomp_grouped_linear_backward(int dtype, int gdtype, uint64_t rows, uint64_t inner, uint64_t cols,
                                      uint32_t experts, const int32_t* offsets, const void* dy, uint64_t lddy,
                                      const void* z, uint64_t ldz, int act, const void* x, uint64_t ldx,

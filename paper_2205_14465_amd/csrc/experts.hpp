@@ -117,12 +117,16 @@ hipError_t launch_grouped_pair(int dtype, int out_dtype, const GroupedProduct& r
 
 // The forward pass for few rows, which needs no workspace: up to 64 in all; more in
 // fp32, whose tiles are bound by the matrix instructions wherever rows fill them badly,
-// and where 16-bit operands would be laid out first (weights in rows of no whole pieces, a
-// gather from more than 2 GB).  us, this way and by tiles, with rows
-// spread evenly (all with one expert): fp32, 8 experts of 1600x1600, 100 rows 25 (34) and
-// 34 (32), 192 34 (55) and 34 (32); 64 experts 128 rows 133 (44) and 189 (32), 500 164
-// (144) and 189 (36); fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows
-// 32 and 36, 1024 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.
+// and where 16-bit operands would be laid out first (weights in rows of no whole pieces,
+// a gather from more than 2 GB).  us, this way and by tiles, with rows spread evenly (all
+// with one expert): fp32, 8 experts of 1600x1600, 100 rows 25 (34) and 34 (32), 192 34
+// (55) and 34 (32); 64 experts 128 rows 133 (44) and 189 (32), 500 164 (144) and 189
+// (36); fp16, 64 experts of 768x768, 64 rows 15 and 13, of 1001x515 256 rows 32 and 36,
+// 1024 47 and 38, 8 experts 128 rows 12 and 20, 256 19 and 20.  The limit goes by all
+// experts, an expert's rows by one workgroup for 16 columns, 32 at a time: with very many
+// experts, and the more so where one has all the rows, it is too high (at the limit, fp32,
+// 128 experts of 768x768, 1088 rows 77 (167) and 86 (19); 1024 of 256x256, 8256 rows 147
+// (582) and 99 (45); fp16, 128 of 769x769 99 (269) and 93 (69)).
 inline uint64_t grouped_few_rows(int dtype, uint32_t experts, bool laid_out) {
     return 64 + (dtype == BC_F32 || laid_out ? 8ull * experts : 0);
 }

@@ -9,12 +9,15 @@
 // Both passes are bound by memory (1.56e9 fp32 elements: 1010 us for the norm, 6.2
 // TB/s, and 2490 for the scaling to another place, 5.0, where a copy reaches 4.3 and an
 // elementwise product of one array 5.9; in bfloat16 521 and 1250; ResNet-50's 161
-// gradients of 25.6e6 elements: 26 and, with nothing to scale, 3.4).  A workgroup takes a run of consecutive chunks and finds its
+// gradients of 25.6e6 elements: 20.9 us and 37.6, with nothing to scale 5.6; in bfloat16
+// 18.2, 25.4 and 5.6).  A workgroup takes a run of consecutive chunks and finds its
 // first matrix by a search of the table with all its threads; the second pass walks
-// its run backwards and meets what the caches kept of the first.  A thread has 128
-// bytes of loads in flight whatever the type (with 64 of the 16-bit types the norm
-// took 722 us in place of 524), and rows' ends are left to a loop of their own,
-// whose registers would cost a quarter of the waves in flight.
+// its run backwards and meets what the caches kept of the first.  Over a whole group of
+// chunks a thread has 128 bytes of loads in flight whatever the type (with 64 of the
+// 16-bit types the norm of the large list took 722 us in place of 524); of a 16-bit list
+// of less than 33e6 elements a workgroup's run is shorter than a group (clip_parts), so
+// that its chunks go by pieces, fewer in flight.  Rows' ends are left to a loop of their
+// own, whose registers would cost a quarter of the waves in flight.
 #include "common.hpp"
 #include "experts.hpp"
 
@@ -275,7 +278,8 @@ __global__ __launch_bounds__(kThreads) void write_table(uint32_t* to, TableWords
 
 }  // namespace
 
-// A chunk a workgroup while there are no more chunks than CUs, a group after that.
+// A chunk a workgroup while there are no more chunks than CUs, then four (a group of
+// fp32's, half of a 16-bit one) until there are kClipParts workgroups.
 uint32_t clip_parts(uint64_t chunks) {
     return (uint32_t)std::min(std::min<uint64_t>(chunks, kClipParts), std::max<uint64_t>((chunks + 3) / 4, 256));
 }
@@ -292,8 +296,9 @@ hipError_t launch_norm_of_parts(const Clip& a, hipStream_t s) {
 }
 
 // Five workgroups a CU, each of which adds the parts up first: from 768 to 2048 the
-// elements above take the same time, ResNet-50's to another place 36 us but 41 with 1024,
-// and a list with nothing to scale 3.4 but 5.1 with 2048.
+// 1.56e9 elements take the same time, ResNet-50's to another place 40.6 us with 768, 41.9
+// with 1024, 37.6 with 1280 and 37.3 with 2048 (in bfloat16 31.0, 28.4, 25.4, 24.0), and
+// with nothing to scale 5.9, 6.0, 5.6 and 7.5.
 hipError_t launch_clip(const Clip& a, hipStream_t s) {
     const uint32_t blocks = std::max(1u, std::min(clip_parts(a.chunks), 1280u));
     hipLaunchKernelGGL(clip_scale, dim3(blocks), dim3(kThreads), 0, s, a);
